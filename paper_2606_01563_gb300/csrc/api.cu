@@ -10,7 +10,7 @@
 
 using namespace mkv;
 
-namespace {
+namespace mkv {
 
 int num_sms_current() {
   static int cache[64] = {0};
@@ -22,6 +22,10 @@ int num_sms_current() {
   if (dev >= 0 && dev < 64) cache[dev] = n;
   return n;
 }
+
+}  // namespace mkv
+
+namespace {
 
 int protected_count_host(int T, int W, int sink, int keep_window) {
   const int s = sink < T ? sink : T;

@@ -10,6 +10,9 @@
 
 namespace mkv {
 
+// SMs of the current device (api.cu)
+int num_sms_current();
+
 // ------------------------------------------------------------------ decode
 struct DecodeArgs {
   const void* q;      // bf16 [b, Hkv*G, D]

@@ -1,4 +1,4 @@
-"""Python binding of the MomentKV C ABI (include/mkv.h).
+"""Python binding of the MomentKV C ABI (include/mkv.h, include/mkv_tree.h).
 
 Argument marshalling only: every function forwards to the function of the
 same name in libmkv.so, passing device pointers of torch tensors; all work
@@ -48,6 +48,25 @@ class mkv_decode_params(ctypes.Structure):
                 ("early_load", c_i32), ("C_split", c_vp)]
 
 
+class mkv_tree(ctypes.Structure):
+    _fields_ = [("n_nodes", c_i32), ("count", c_vp), ("mask", c_vp), ("q_node", ctypes.c_int64),
+                ("q_batch", ctypes.c_int64), ("kv_node", ctypes.c_int64), ("kv_batch", ctypes.c_int64)]
+
+
+class mkv_tree_layer(ctypes.Structure):
+    _fields_ = [("cache", mkv_cache), ("k", c_vp), ("v", c_vp)]
+
+
+class mkv_rope_params(ctypes.Structure):
+    _fields_ = [("rot_dim", c_i32), ("neighbours", c_i32), ("inverse", c_i32), ("n_axes", c_i32),
+                ("inv_freq", ctypes.c_float * 64), ("axis", c_i32 * 64)]
+
+
+class mkv_rope_tensor(ctypes.Structure):
+    _fields_ = [("in_", c_vp), ("out", c_vp), ("heads", c_i32)] + [
+        (n, ctypes.c_int64) for n in ("in_batch", "in_token", "in_head", "out_batch", "out_token", "out_head")]
+
+
 STATUS = {0: "MKV_OK", 1: "MKV_ERR_INVALID_ARG", 2: "MKV_ERR_SHAPE", 3: "MKV_ERR_CAPACITY",
           4: "MKV_ERR_CUDA", 5: "MKV_ERR_TIMEOUT", 6: "MKV_ERR_UNSUPPORTED", 7: "MKV_ERR_WORKSPACE"}
 
@@ -55,6 +74,8 @@ EXPORTS = ("mkv_status_str", "mkv_version", "mkv_compress_workspace_size", "mkv_
            "mkv_decode_workspace_size", "mkv_decode_step", "mkv_evict_workspace_size",
            "mkv_evict_append", "mkv_get_device_error", "mkv_decode_step_noalloc", "mkv_moments_pack_bf16",
            "mkv_decode_evict_workspace_size", "mkv_decode_evict_step", "mkv_moments_pack_split")
+# declared in include/mkv_tree.h
+TREE_EXPORTS = ("mkv_tree_build", "mkv_tree_workspace_size", "mkv_tree_step", "mkv_tree_commit", "mkv_rope")
 # test hooks declared in include/mkv_debug.h
 DEBUG_EXPORTS = ("mkv_debug_set_poll_limit", "mkv_debug_force_ticket_merge")
 
@@ -110,6 +131,21 @@ def lib():
         L.mkv_moments_pack_bf16.argtypes = [mkv_geom, ctypes.POINTER(mkv_moments), c_vp, c_vp]
         L.mkv_moments_pack_split.restype = c_i32
         L.mkv_moments_pack_split.argtypes = [mkv_geom, ctypes.POINTER(mkv_moments), ctypes.c_float, c_vp, c_vp]
+        c_i64 = ctypes.c_int64
+        L.mkv_tree_build.restype = c_i32
+        L.mkv_tree_build.argtypes = [c_i32, c_i32, c_vp, c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
+        L.mkv_tree_workspace_size.restype = ctypes.c_size_t
+        L.mkv_tree_workspace_size.argtypes = [mkv_geom, c_i32, c_i32]
+        L.mkv_tree_step.restype = c_i32
+        L.mkv_tree_step.argtypes = [mkv_geom, ctypes.POINTER(mkv_tree), c_vp, c_vp, c_vp, ctypes.POINTER(mkv_cache),
+                                    ctypes.POINTER(mkv_moments), ctypes.POINTER(mkv_decode_params), c_vp, c_vp, c_vp,
+                                    ctypes.c_size_t, c_vp]
+        L.mkv_tree_commit.restype = c_i32
+        L.mkv_tree_commit.argtypes = [mkv_geom, ctypes.POINTER(mkv_tree), c_i32, ctypes.POINTER(mkv_tree_layer), c_vp,
+                                      c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
+        L.mkv_rope.restype = c_i32
+        L.mkv_rope.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params), c_i32,
+                               ctypes.POINTER(mkv_rope_tensor), c_vp]
         L.mkv_debug_set_poll_limit.restype = ctypes.c_int64
         L.mkv_debug_set_poll_limit.argtypes = [ctypes.c_int64]
         L.mkv_debug_force_ticket_merge.restype = c_i32
@@ -177,6 +213,23 @@ class Moments:
 
     def c(self):
         return mkv_moments(self.n.data_ptr(), self.mu_k.data_ptr(), self.mu_v.data_ptr(), self.C.data_ptr())
+
+
+@dataclass
+class Tree:
+    """Drafted nodes (mkv_tree): mask int32 [b, N, ceil(N / 32)], the words of mkv_tree_build; count int32 [b],
+    the nodes in use (None: all N)."""
+    mask: torch.Tensor
+    count: torch.Tensor | None = None
+
+
+@dataclass
+class TreeLayers:
+    """The layers of a commit (tree_layers): what mkv_tree_commit takes, with the tensors it points into."""
+    array: ctypes.Array
+    tree: mkv_tree
+    batch: int
+    held: list
 
 
 def geom(batch, n_kv_heads, group, head_dim):
@@ -289,6 +342,125 @@ def mkv_moments_pack_split(g, mom: Moments, tau, C_split, stream=None):
     m = mom.c()
     _check(lib().mkv_moments_pack_split(g, m, float(tau), _ptr(C_split), _stream(stream)),
            "mkv_moments_pack_split")
+
+
+# -------------------------------------------- speculative decoding, positions
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _nodes(t, what):
+    """(node, batch) strides in elements of a [b, N, heads, d] bf16 tensor whose heads lie densely."""
+    _need(t.dtype == torch.bfloat16 and t.dim() == 4 and t.stride(3) == 1 and
+          (t.shape[2] == 1 or t.stride(2) == t.shape[3]), f"{what}: bf16 [b, N, heads, d] with dense heads")
+    # (a stride over an extent of one is never used: the dense value stands for it)
+    return (t.stride(1) if t.shape[1] > 1 else 0), (t.stride(0) if t.shape[0] > 1 else 0)
+
+
+def _int32(t, shape, what):
+    _need(t.dtype == torch.int32 and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{what}: contiguous int32 {list(shape)}")
+
+
+def mkv_tree_build(parents, mask, pos, ws, count=None, base=None, stream=None):
+    """Visibility words and positions of drafted trees: parents int32 [b, N] -> mask int32 [b, N, ceil(N / 32)],
+    pos int32 [b, N] (or None).  base: int32 [b], any stride (e.g. cache.seen[:, 0])."""
+    b, n = parents.shape
+    _int32(parents, (b, n), "parents")
+    _int32(mask, (b, n, (n + 31) // 32), "mask")
+    if pos is not None:
+        _int32(pos, (b, n), "pos")
+    if count is not None:
+        _int32(count, (b,), "count")
+    if base is not None:
+        _need(base.dtype == torch.int32 and tuple(base.shape) == (b,), "base: int32 [b]")
+    code = lib().mkv_tree_build(b, n, _ptr(parents), _ptr(count), _ptr(base), 0 if base is None else base.stride(0),
+                                _ptr(mask), _ptr(pos), _ptr(ws), ws.numel(), _stream(stream))
+    _check(code, "mkv_tree_build")
+
+
+def mkv_tree_workspace_size(g, n_nodes, capacity):
+    return lib().mkv_tree_workspace_size(g, n_nodes, capacity)
+
+
+def mkv_tree_step(g, tree: Tree, q, k, v, cache: Cache, mom: Moments | None, p: mkv_decode_params, out, lse, ws,
+                  stream=None):
+    """Attention of drafted nodes over the cache, the nodes they see and the moments: q bf16 [b, N, g*h_kv, d],
+    k and v bf16 [b, N, h_kv, d] (nodes and batch items may be strided), out bf16 [b, N, g*h_kv, d], lse fp32
+    [b, N, g*h_kv] or None."""
+    b, n = tree.mask.shape[:2]
+    heads, d = g.group * g.n_kv_heads, g.head_dim
+    _int32(tree.mask, (g.batch, n, (n + 31) // 32), "mask")
+    if tree.count is not None:
+        _int32(tree.count, (b,), "count")
+    _need(tuple(q.shape) == (b, n, heads, d), "q: [b, N, g*h_kv, d]")
+    _need(tuple(k.shape) == (b, n, g.n_kv_heads, d) and k.shape == v.shape, "k, v: [b, N, h_kv, d]")
+    _need(out.dtype == torch.bfloat16 and tuple(out.shape) == (b, n, heads, d) and out.is_contiguous(),
+          "out: contiguous bf16 [b, N, g*h_kv, d]")
+    _need(lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (b, n, heads) and lse.is_contiguous()),
+          "lse: contiguous float32 [b, N, g*h_kv]")
+    kv = _nodes(k, "k")
+    _need(kv == _nodes(v, "v"), "k and v: the same strides")
+    t = mkv_tree(n, _ptr(tree.count), _ptr(tree.mask), *_nodes(q, "q"), *kv)
+    code = lib().mkv_tree_step(g, t, _ptr(q), _ptr(k), _ptr(v), cache.c(), mom.c() if mom is not None else None, p,
+                               _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream))
+    _check(code, "mkv_tree_step")
+
+
+def tree_layers(layers):
+    """(cache, k, v) of every layer, k and v as given to mkv_tree_step: made once and kept beside the caches."""
+    layers = list(layers)
+    _need(len(layers) > 0, "at least one layer")
+    k0 = layers[0][1]
+    kv = _nodes(k0, "k")
+    for _, k, v in layers:
+        _need(k.shape == k0.shape and v.shape == k0.shape and _nodes(k, "k") == kv and _nodes(v, "v") == kv,
+              "k and v: the same shape and strides in every layer")
+    array = (mkv_tree_layer * len(layers))(*(mkv_tree_layer(c.c(), k.data_ptr(), v.data_ptr()) for c, k, v in layers))
+    return TreeLayers(array, mkv_tree(k0.shape[1], None, None, 0, 0, *kv), k0.shape[0], layers)
+
+
+def mkv_tree_commit(g, layers: TreeLayers, path, n_path, ws, stream=None):
+    """Appends the nodes path[b, :n_path[b]] (int32, root first) to the caches of all layers."""
+    _int32(path, (g.batch, path.shape[1]), "path")
+    _int32(n_path, (g.batch,), "n_path")
+    _need(layers.batch == g.batch and layers.held[0][1].shape[2:] == (g.n_kv_heads, g.head_dim),
+          "layers: k and v of this geometry")
+    code = lib().mkv_tree_commit(g, layers.tree, len(layers.array), layers.array, _ptr(path), path.shape[1],
+                                 _ptr(n_path), _ptr(ws), ws.numel(), _stream(stream))
+    _check(code, "mkv_tree_commit")
+
+
+def rope_params(inv_freq, axis=None, neighbours=False):
+    """Rotation parameters from rot_dim / 2 inverse frequencies and the position axis of each (None: axis 0)."""
+    inv_freq = [float(x) for x in inv_freq]
+    axis = [0] * len(inv_freq) if axis is None else [int(x) for x in axis]
+    _need(len(inv_freq) == len(axis) <= 64, "as many axes as frequencies, at most 64")
+    return mkv_rope_params(2 * len(inv_freq), int(neighbours), 0, max(axis, default=0) + 1,
+                           (ctypes.c_float * 64)(*inv_freq), (c_i32 * 64)(*axis))
+
+
+def mkv_rope(pos, p: mkv_rope_params, tensors, inverse=False, stream=None):
+    """Rotates (in, out) pairs of bf16 [b, tokens, heads, d] tensors (any strides with adjacent dims; out may be in)
+    by int32 positions pos [axes, b, tokens] (adjacent tokens; expanded axes and batches are fine).  inverse: by
+    the negative angle."""
+    _need(pos.dtype == torch.int32 and pos.dim() == 3 and pos.shape[0] >= p.n_axes and
+          (pos.stride(2) == 1 or pos.shape[2] <= 1), "pos: int32 [axes, b, tokens] with adjacent tokens")
+    _, b, t = pos.shape
+    d = tensors[0][0].shape[3]
+    arr = (mkv_rope_tensor * len(tensors))()
+    for i, (x, y) in enumerate(tensors):
+        _need(x.dtype == y.dtype == torch.bfloat16 and x.shape == y.shape and x.dim() == 4 and
+              (x.shape[0], x.shape[1], x.shape[3]) == (b, t, d) and x.stride(3) == y.stride(3) == 1,
+              "tensors: pairs of bf16 [b, tokens, heads, d] with adjacent dims")
+        # (a stride over an extent of one is never used)
+        strides = [s if n > 1 else 0 for u in (x, y) for s, n in zip(u.stride()[:3], x.shape)]
+        arr[i] = mkv_rope_tensor(x.data_ptr(), y.data_ptr(), x.shape[2], *strides)
+    q = mkv_rope_params.from_buffer_copy(p)
+    q.inverse = int(inverse)
+    code = lib().mkv_rope(b, t, d, _ptr(pos), pos.stride(0), pos.stride(1) if b > 1 else 0, q, len(tensors), arr, _stream(stream))
+    _check(code, "mkv_rope")
 
 
 def mkv_debug_set_poll_limit(polls):
