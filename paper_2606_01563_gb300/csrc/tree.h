@@ -55,6 +55,7 @@ struct TreeArgs {
   int32_t early;
   __nv_bfloat16* out;  // [b, N, Hkv*G, D]
   float* lse;
+  uint32_t polls;  // poll limit of the pipeline waits
   void* ws;
   int32_t batch;
   int32_t n_kv;

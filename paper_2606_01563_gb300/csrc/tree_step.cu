@@ -1,13 +1,38 @@
 // Attention of drafted nodes over the retained cache, the nodes they see and
-// the moment term, in one normaliser (mkv_tree_step).
+// the moment term, in one normaliser (mkv_tree_step), on the fifth-generation
+// tensor cores.
 //
-// One CTA per (node, KV head, batch item): its warps take the keys in turn, a
-// lane holds D / 32 dims of the group's queries and of each key and value,
-// and every warp keeps a running maximum, sum and output per head; the warps'
-// states and the moment term merge at the end.  Simple and slow: K and V are
-// read once per node.
+// Mathematics.  A unit's query rows are (node, head of the group).  A block
+// of 128 rows keeps a reference m, a sum l and an output O per row and takes
+// the keys 128 at a time: S = Q K^T, P = 2^(S scale log2 e - m), l += sum P,
+// O += P V.  The retained rows are tiles without a mask, the nodes are tiles
+// whose bits the mask words give.  The moment term is one more key of every
+// row, with logit e = log n + scale q.mu_k and value mu_v + scale C' q: it
+// starts the block (m = e, l = 1, O = its value), the product Q C'^T running on
+// the tensor cores with C' as bf16 hi + lo parts.  m only has to be common to a
+// row's keys, so it moves (with a rescaling of O and l) only when a score
+// exceeds it by more than 8 in log2 units.  P enters the second product
+// rounded to bf16 (2^-8 relative, the output's own rounding); l is summed from
+// the unrounded weights.
+//
+// Work.  The tiles of all (unit, row block) items form one list that is cut
+// into equal runs, one per CTA, wherever the run ends; an item cut by a
+// boundary leaves (m, l, O) of its parts in the workspace, and
+// tree_merge_kernel joins them.  Lengths of any raggedness so cost what their
+// tiles cost.  A CTA holds one or two row blocks: with two (more than 128
+// rows) every K and V tile is read once for 256 rows, with one the two
+// softmax groups take the tiles alternately and merge at the end.
+//
+// One CTA, three warpgroups: warps 0-3 and 4-7 are the softmax groups, a thread
+// a row; warp 8 issues TMA copies (Q, and K and V tiles into a ring), warp 9
+// the MMAs.  Tensor memory: S (then P over it) of the two groups, 128 columns
+// each, and O of the two, D columns each.
+#include <algorithm>
+#include <mutex>
+
 #include "common.cuh"
 #include "kernels.h"
+#include "tc.cuh"
 #include "tree.h"
 #include "warp_mma.cuh"
 
@@ -15,151 +40,973 @@ namespace mkv {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kTile = 128;                   // keys per tile, rows per block
+constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
+constexpr int kThreads = 384;                // 2 softmax groups; the TMA warp, the MMA warp and two idle ones
+// registers per thread: 168 at the launch (3 x 168 = 504 for a warp of each group), then 224 for the softmax
+// groups, whose threads hold a row of 128 scores, and 56 for the others
+constexpr int kSoftmaxRegs = 224, kIssueRegs = 56;
+static_assert(2 * kSoftmaxRegs + kIssueRegs <= 3 * 168, "the block's registers at its launch");
+constexpr int kScanUnits = 4096;             // above: one CTA per item, without a list
+constexpr float kSlack = 8.f;                // log2 headroom of the reference (weights <= 2^8)
+constexpr float kNegInf = -INFINITY;
+constexpr uint32_t kAll = 0xffffffffu;
 
-template <int D, int G>
-__global__ void __launch_bounds__(kWarps * 32) tree_step_kernel(const TreeArgs a) {
-  constexpr int E = D / 32;  // dims per lane
-  const int i = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, u = b * a.n_kv + kv;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  __shared__ float sm[kWarps + 1][G], sl[kWarps + 1][G], so[kWarps + 1][G][D], sq[G][D];
-  grid_dependency_wait();
-  const int HQ = a.n_kv * G;
-  __nv_bfloat16* out = a.out + (((size_t)b * a.N + i) * HQ + kv * G) * D;
-  float* lse = a.lse != nullptr ? a.lse + ((size_t)b * a.N + i) * HQ + kv * G : nullptr;
-  int nodes = a.count != nullptr ? a.count[b] : a.N;
-  if (nodes < 0 || nodes > a.N) {
-    if (tid == 0) record_error(a.ws, MKV_ERR_INVALID_ARG, u);
-    nodes = nodes < 0 ? 0 : a.N;
+__host__ __device__ constexpr int slot_bytes(int D) { return kTile * D * 2; }
+__host__ __device__ constexpr int ring_slots(int D, int blocks) { return D == 128 ? (blocks == 2 ? 5 : 6) : 10; }
+constexpr int kMaxSlots = 10;
+
+struct Plan {
+  int32_t blocks;   // row blocks per CTA: 1 or 2
+  int32_t mb;       // items per unit
+  int32_t g_shift;  // log2 of the group
+  int32_t list;     // 1: runs of the tile list, 0: one item per CTA
+  int32_t grid;
+  int32_t min_run;  // tiles per CTA at least
+  int32_t words;    // mask words per node
+};
+
+// A part of a split item (m, l, O of `blocks` x 128 rows).
+struct Parts {
+  int4* desc;   // [grid] of the item a CTA's run starts in the middle of: (first part or -1, last CTA, unit, mb)
+  float2* ml;   // [2 grid][blocks 128]
+  float4* o;    // [2 grid][D / 4][blocks 128]
+};
+
+struct Shared {
+  uint64_t full[kMaxSlots], empty[kMaxSlots];
+  uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], o_full, mma_done;
+  uint32_t tmem;
+  int32_t abort, issued, q_issued;
+  int32_t unit, mb, t0;
+  long long left, start, run;
+  uint32_t odd[2][8];  // nodes with a value that is not finite, of this segment and the next
+  float2 ml[kTile];  // (one row block) group 1's (m, l), then the two groups' factors
+  long long scan[kThreads / 32];
+};
+constexpr int kSharedBytes = 2048;
+static_assert(sizeof(Shared) <= kSharedBytes, "shared variables");
+__host__ __device__ constexpr int smem_bytes(int D, int blocks) {
+  return (blocks + ring_slots(D, blocks)) * slot_bytes(D) + kSharedBytes + 1024;
+}
+static_assert(smem_bytes(128, 2) <= 232448 && smem_bytes(128, 1) <= 232448 && smem_bytes(64, 2) <= 232448, "227 KB");
+
+// D[tmem] (+)= A[tmem] B over one k-step (16 elements, 8 columns of A).
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t db, uint32_t idesc,
+                                             uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(db), "r"(idesc), "r"(accumulate));
+}
+
+// 32 columns of this warp's lanes, without waiting (tmem_wait_ld, then keep()).
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The loaded registers may only be read from here on (orders their uses after the wait).
+__device__ __forceinline__ void keep16(uint32_t* r) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+               "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Shared memory written by threads, next read by the tensor cores.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::
+          "r"(smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
+      : "memory");
+}
+
+// Whether any of a word's two bf16 values is infinite or NaN.
+__device__ __forceinline__ bool odd2(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// What a unit's item consists of.
+struct Item {
+  int len, count, n_e;
+  int head, cache, nodes;  // tiles: the moment term (0 or 1), the cache, the nodes
+};
+
+__device__ __forceinline__ Item load_item(const TreeArgs& a, int u) {
+  Item it;
+  const int b = u / a.n_kv;
+  const int len = a.len[u], count = a.count != nullptr ? a.count[b] : a.N;
+  it.n_e = a.n != nullptr ? a.n[u] : 0;
+  it.len = min(max(len, 0), a.cap);
+  it.count = min(max(count, 0), a.N);
+  it.head = a.n != nullptr ? 1 : 0;
+  it.cache = (it.len + kTile - 1) / kTile;
+  it.nodes = (it.count + kTile - 1) / kTile;
+  return it;
+}
+// Tiles of an item whose rows start at node `first` (at least one: its outputs have to be written).
+__device__ __forceinline__ int item_tiles(const Item& it, int first) {
+  return first < it.count ? max(1, it.head + it.cache + it.nodes) : 1;
+}
+
+// A CTA's next segment: tiles [begin, end) of item (unit, mb).
+struct Segment {
+  int unit, mb, first;  // first node of the item's rows
+  int begin, end, tiles;
+  Item it;
+  bool live;
+  __device__ __forceinline__ bool moments() const { return live && begin == 0 && it.head > 0 && it.n_e > 0; }
+  // key tiles [k0, k1): the head is tile 0 when there is one
+  __device__ __forceinline__ int k0() const { return live ? max(begin - it.head, 0) : 0; }
+  __device__ __forceinline__ int k1() const { return live ? max(end - it.head, 0) : 0; }
+  __device__ __forceinline__ bool whole() const { return begin == 0 && end == tiles; }
+  // keys in use of key tile j
+  __device__ __forceinline__ int valid(int j) const {
+    return j < it.cache ? min(kTile, it.len - j * kTile) : min(kTile, it.count - (j - it.cache) * kTile);
   }
-  int len = a.len[u];
-  if (len < 0 || len > a.cap) {
-    if (tid == 0) record_error(a.ws, MKV_ERR_CAPACITY, u);
-    len = len < 0 ? 0 : a.cap;
+};
+
+struct Walk {
+  int unit, mb, t;
+  long long left;
+  __device__ __forceinline__ bool next(const TreeArgs& a, const Plan& p, Segment& s) {
+    if (left <= 0) return false;
+    s.unit = unit;
+    s.mb = mb;
+    s.first = mb * ((p.blocks * kTile) >> p.g_shift);
+    s.it = load_item(a, unit);
+    s.live = s.first < s.it.count;
+    s.tiles = item_tiles(s.it, s.first);
+    s.begin = t;
+    s.end = static_cast<int>(min((long long)s.tiles, t + left));
+    left -= s.end - s.begin;
+    t = 0;
+    if (++mb == p.mb) {
+      mb = 0;
+      ++unit;
+    }
+    return true;
   }
-  if (i >= nodes) {
-    for (int j = tid; j < G * D; j += kWarps * 32) out[j] = __float2bfloat16_rn(0.f);
-    if (lse != nullptr && tid < G) lse[tid] = -INFINITY;
+};
+
+// Pipeline wait that gives up after `polls` polls: records the timeout once and
+// raises the CTA's abort flag; every later wait then passes at once.
+__device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, Shared& sh, const TreeArgs& a) {
+  volatile int32_t* abort = &sh.abort;
+  if (*abort) return false;
+  if (mbar_wait(bar, parity, a.polls)) return true;
+  *abort = 1;
+  record_error(a.ws, MKV_ERR_TIMEOUT, static_cast<int32_t>(blockIdx.x));
+  return false;
+}
+
+// Where this CTA's run starts in the list of all items' tiles, and what it is
+// of an item that an earlier CTA began.
+template <int D>
+__device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Shared& sh, const Parts& parts) {
+  const int tid = threadIdx.x, units = a.batch * a.n_kv;
+  const int per_cta = (p.blocks * kTile) >> p.g_shift;  // nodes per item
+  auto record = [&](int u) {
+    const int len = a.len[u], count = a.count != nullptr ? a.count[u / a.n_kv] : a.N;
+    if (len < 0 || len > a.cap) record_error(a.ws, MKV_ERR_CAPACITY, u);
+    if (count < 0 || count > a.N) record_error(a.ws, MKV_ERR_INVALID_ARG, u);
+  };
+  if (!p.list) {
+    if (tid == 0) {
+      sh.unit = blockIdx.x / p.mb;
+      sh.mb = blockIdx.x % p.mb;
+      sh.t0 = 0;
+      const Item it = load_item(a, sh.unit);
+      sh.left = item_tiles(it, sh.mb * per_cta);
+      if (sh.mb == 0) record(sh.unit);
+    }
+    __syncthreads();
     return;
   }
-  const float qs = rsqrtf(static_cast<float>(D)) * kLog2e;
-  float q[G][E], o[G][E] = {}, m[G], l[G];
-  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + i * a.q_node + kv * G * D;
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-    load_bf16<E>(qp + h * D + lane * E, q[h]);
-    m[h] = -INFINITY;
-    l[h] = 0.f;
-    if (warp == 0)
-#pragma unroll
-      for (int e = 0; e < E; ++e) sq[h][lane * E + e] = q[h][e];
-  }
-  auto take = [&](const __nv_bfloat16* kp, const __nv_bfloat16* vp) {
-    float k[E], v[E];
-    load_bf16<E>(kp + lane * E, k);
-    load_bf16<E>(vp + lane * E, v);
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(q[h][e], k[e], x);
-      x = warp_sum(x) * qs;
-      const float mn = fmaxf(m[h], x);
-      const float f = mn == -INFINITY ? 1.f : fast_exp2(m[h] - mn), p = mn == -INFINITY ? 0.f : fast_exp2(x - mn);
-      m[h] = mn;
-      l[h] = fmaf(l[h], f, p);
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[h][e] = fmaf(o[h][e], f, p * v[e]);
-    }
+  auto weight = [&](int u) {
+    const Item it = load_item(a, u);
+    const int alive = (it.count + per_cta - 1) / per_cta;
+    return (long long)alive * item_tiles(it, 0) + (p.mb - alive);
   };
-  const __nv_bfloat16* K = static_cast<const __nv_bfloat16*>(a.K) + (size_t)u * a.cap * D;
-  const __nv_bfloat16* V = static_cast<const __nv_bfloat16*>(a.V) + (size_t)u * a.cap * D;
-  for (int j = warp; j < len; j += kWarps) take(K + (size_t)j * D, V + (size_t)j * D);
-  const uint32_t* row = a.mask + ((size_t)b * a.N + i) * tree_words(a.N);
-  for (int j = warp; j < nodes; j += kWarps)
-    if ((row[j >> 5] >> (j & 31)) & 1u) {
-      const int64_t off = b * a.kv_batch + j * a.kv_node + kv * D;
-      take(static_cast<const __nv_bfloat16*>(a.k) + off, static_cast<const __nv_bfloat16*>(a.v) + off);
-    }
+  const int chunk = (units + kThreads - 1) / kThreads, u0 = min(units, tid * chunk), u1 = min(units, u0 + chunk);
+  long long sum = 0;
+  for (int u = u0; u < u1; ++u) {
+    sum += weight(u);
+    if (blockIdx.x == 0) record(u);
+  }
+  long long incl = sum;
 #pragma unroll
-  for (int h = 0; h < G; ++h) {
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(kAll, incl, o);
+    if ((tid & 31) >= o) incl += x;
+  }
+  if ((tid & 31) == 31) sh.scan[tid >> 5] = incl;
+  if (tid == 0) sh.left = 0;
+  __syncthreads();
+  long long before = 0, total = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) so[warp][h][lane * E + e] = o[h][e];
-    if (lane == 0) {
-      sm[warp][h] = m[h];
-      sl[warp][h] = l[h];
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < (tid >> 5)) before += sh.scan[w];
+    total += sh.scan[w];
+  }
+  const long long run = max((long long)p.min_run, (total + p.grid - 1) / p.grid);
+  const long long start = run * blockIdx.x;
+  long long at = before + incl - sum;  // of this thread's first unit
+  if (start >= at && start < at + sum) {
+    int u = u0;
+    long long w = weight(u);
+    while (start >= at + w) {
+      at += w;
+      w = weight(++u);
     }
+    const Item it = load_item(a, u);
+    const int tiles = item_tiles(it, 0), alive = (it.count + per_cta - 1) / per_cta;
+    long long in = start - at;  // the unit's tiles before the run
+    int mb, t0;
+    if (in < (long long)alive * tiles) {
+      mb = static_cast<int>(in / tiles);
+      t0 = static_cast<int>(in % tiles);
+    } else {
+      mb = alive + static_cast<int>(in - (long long)alive * tiles);
+      t0 = 0;
+    }
+    sh.unit = u;
+    sh.mb = mb;
+    sh.t0 = t0;
+    sh.left = min(run, total - start);
+    // the first boundary inside an item sees to its merge: its first part is
+    // the previous CTA's last segment (its only one if the item starts with
+    // the run)
+    int4 d = make_int4(-1, 0, u, mb);
+    if (t0 > 0 && t0 <= run) {
+      d.x = 2 * (static_cast<int>(blockIdx.x) - 1) + (t0 == run ? 0 : 1);
+      d.y = static_cast<int>((start - t0 + tiles - 1) / run);
+    }
+    sh.start = d.x;
+    sh.run = d.y;
   }
   __syncthreads();
-  // the moment term as one more state: m = its logit, l = 1, o = its value
-  const int n_e = a.n != nullptr ? a.n[u] : 0;
-  for (int t = tid; t < G * D; t += kWarps * 32) {
-    const int h = t / D, c = t % D;
-    float f = 0.f;
-    if (n_e > 0) {
-      if (a.order == 1)
-        for (int j = 0; j < D; ++j) {
-          const size_t at = ((size_t)u * D + c) * D + j;
-          float x;
-          if (a.Cs != nullptr) {
-            const uint2 w = a.Cs[at / 2];
-            const __nv_bfloat162 hi = *reinterpret_cast<const __nv_bfloat162*>(&w.x);
-            const __nv_bfloat162 lo = *reinterpret_cast<const __nv_bfloat162*>(&w.y);
-            x = (j & 1) ? __high2float(hi) + __high2float(lo) : __low2float(hi) + __low2float(lo);
-          } else {
-            x = a.C16 != nullptr ? __bfloat162float(a.C16[at]) : a.C[at];
-            if (fabsf(x * static_cast<float>(n_e)) < a.tau) x = 0.f;
-          }
-          f = fmaf(x, sq[h][j], f);
+}
+
+template <int D, int BLOCKS>
+__global__ void __launch_bounds__(kThreads, 1)
+    tree_step_kernel(const __grid_constant__ TreeArgs a, const __grid_constant__ Plan p,
+                     const __grid_constant__ Parts parts, const __grid_constant__ CUtensorMap tmQ,
+                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ CUtensorMap tmKt, const __grid_constant__ CUtensorMap tmVt) {
+  constexpr int kSlot = slot_bytes(D), NS = ring_slots(D, BLOCKS), BX = D / 64;
+  constexpr uint32_t cS = 0, cO = 256;  // TMEM columns: S / P of group s at 128 s, O at 256 + D s
+  extern __shared__ __align__(1024) uint8_t smraw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = sm;
+  uint8_t* ring = sm + BLOCKS * kSlot;
+  Shared& sh = *reinterpret_cast<Shared*>(ring + NS * kSlot);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], 1);
+    }
+    mbar_init(&sh.q_full, 1);
+    mbar_init(&sh.q_empty, 1 + 8);
+    mbar_init(&sh.c_grant, 1);
+    mbar_init(&sh.c_full, 8);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sh.s_full[s], 1);
+      mbar_init(&sh.p_ready[s], 4);
+    }
+    mbar_init(&sh.o_full, 1);
+    mbar_init(&sh.mma_done, 1);
+    sh.abort = 0;
+    sh.issued = 0;
+    sh.q_issued = 0;
+    mbar_fence_init();
+  }
+  if (tid < 16) (&sh.odd[0][0])[tid] = 0;
+  if (warp == 9) tmem_alloc(&sh.tmem, 512);
+  tc_fence_before();
+  if (!a.early) grid_dependency_wait();
+  find_run<D>(a, p, sh, parts);  // (ends with a barrier)
+  tc_fence_after();
+  const uint32_t tm = sh.tmem;
+  Walk walk{sh.unit, sh.mb, sh.t0, sh.left};
+  Segment s;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+    if (warp == 8 && lane == 0) {  // ---- TMA
+      int seq = 0, nq = 0;
+      bool ok = true, waited = !a.early;
+      const uint64_t pol = l2_evict_first();
+      auto wait_prior = [&] {
+        if (!waited) {
+          grid_dependency_wait();
+          waited = true;
         }
-      f = fmaf(f, rsqrtf(static_cast<float>(D)), a.mu_v[(size_t)u * D + c]);
-    }
-    so[kWarps][h][c] = f;
-  }
-  if (tid < G) {
-    float x = 0.f;
-    for (int j = 0; n_e > 0 && j < D; ++j) x = fmaf(a.mu_k[(size_t)u * D + j], sq[tid][j], x);
-    sm[kWarps][tid] = n_e > 0 ? fmaf(x, qs, log2f(static_cast<float>(n_e))) : -INFINITY;
-    sl[kWarps][tid] = n_e > 0 ? 1.f : 0.f;
-  }
-  __syncthreads();
-  for (int t = tid; t < G * D; t += kWarps * 32) {
-    const int h = t / D, c = t % D;
-    float M = -INFINITY, L = 0.f, acc = 0.f;
-    for (int w = 0; w <= kWarps; ++w)
-      if (sl[w][h] > 0.f) M = fmaxf(M, sm[w][h]);
-    for (int w = 0; w <= kWarps; ++w)
-      if (sl[w][h] != 0.f) {  // (a NaN sum passes on)
-        const float f = fast_exp2(sm[w][h] - M);
-        L = fmaf(sl[w][h], f, L);
-        acc = fmaf(so[w][h][c], f, acc);
+        grid_launch_dependents();
+      };
+      auto slot = [&]() -> int {  // the next slot of the ring, free
+        const int i = seq % NS;
+        if (seq >= NS && !pwait(&sh.empty[i], ((seq / NS) - 1) & 1, sh, a)) ok = false;
+        return i;
+      };
+      while (ok && walk.next(a, p, s)) {
+        const bool mom = s.moments();
+        if (!mom && s.k1() == s.k0()) continue;
+        const int b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
+        auto load_q = [&] {
+          wait_prior();
+          if (nq > 0 && !pwait(&sh.q_empty, (nq - 1) & 1, sh, a)) {
+            ok = false;
+            return;
+          }
+          mbar_arrive_expect_tx(&sh.q_full, BLOCKS * kSlot);
+          for (int r = 0; r < BLOCKS; ++r)
+            for (int x = 0; x < BX; ++x)
+              tma_load_4d(sQ + r * kSlot + x * kBox, &tmQ, x * 64, kv << p.g_shift, s.first + r * (kTile >> p.g_shift), b,
+                          &sh.q_full);
+          sh.q_issued = ++nq;
+        };
+        bool q_due = true;
+        if (waited) {
+          load_q();
+          q_due = false;
+        }
+        if (ok && mom && a.order == 1) {  // the softmax threads write C' into the next slots
+          const int n = a.C16 != nullptr ? 1 : 2;
+          for (int j = 0; ok && j < n; ++j) {
+            const int i = slot();
+            if (!ok) break;
+            mbar_arrive(&sh.full[i]);
+            sh.issued = ++seq;
+          }
+          if (ok) mbar_arrive(&sh.c_grant);
+        }
+        for (int j = s.k0(); ok && j < s.k1(); ++j) {
+          const bool cache = j < s.it.cache;
+          if (q_due && (!cache || seq + 2 > NS)) {  // what follows waits for others, or reads their output
+            load_q();
+            q_due = false;
+          }
+          for (int kvx = 0; ok && kvx < 2; ++kvx) {
+            const int i = slot();
+            if (!ok) break;
+            mbar_arrive_expect_tx(&sh.full[i], kSlot);
+            for (int x = 0; x < BX; ++x) {
+              uint8_t* dst = ring + i * kSlot + x * kBox;
+              if (cache)
+                tma_load_3d_hint(dst, kvx ? &tmV : &tmK, x * 64, j * kTile, s.unit, &sh.full[i], pol);
+              else
+                tma_load_4d(dst, kvx ? &tmVt : &tmKt, x * 64, kv, (j - s.it.cache) * kTile, b, &sh.full[i]);
+            }
+            sh.issued = ++seq;
+          }
+        }
+        if (ok && q_due) load_q();
       }
-    out[t] = __float2bfloat16_rn(L != 0.f ? acc / L : 0.f);
-    if (c == 0 && lse != nullptr) lse[h] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+      wait_prior();
+    }
+    if (warp == 9 && lane == 0) {  // ---- MMA
+      const uint64_t dQ = sdesc_sw128(smem_addr(sQ), 16, 1024), dR = sdesc_sw128(smem_addr(ring), 16, 1024);
+      const uint64_t dV = sdesc_sw128(smem_addr(ring), kBox, 1024);
+      int seq = 0, nq = 0, nc = 0, np[2] = {0, 0};
+      bool ok = true;
+      while (ok && walk.next(a, p, s)) {
+        const bool mom = s.moments();
+        const int k0 = s.k0(), k1 = s.k1();
+        if (!mom && k0 == k1) continue;
+        const int W = (k1 - k0) * BLOCKS;  // (tile, group) steps: group w & 1
+        ok = pwait(&sh.q_full, nq & 1, sh, a);
+        ++nq;
+        int kv_seq = seq;  // of the first K tile
+        if (ok && mom && a.order == 1) {
+          const int n = a.C16 != nullptr ? 1 : 2;
+          ok = pwait(&sh.c_full, nc & 1, sh, a);
+          ++nc;
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t id = idesc_bf16(128, D, 0, 0);
+          for (int g = 0; g < BLOCKS; ++g) {
+            for (int j = 0; j < n; ++j) {
+              const uint64_t db = dR + ((seq + j) % NS) * (kSlot >> 4);
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk)
+                umma_bf16(tm + cS + g * 128, dQ + g * (kSlot >> 4) + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2,
+                          db + (kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2, id, (j > 0 || kk > 0) ? 1u : 0u);
+            }
+            umma_commit(&sh.s_full[g]);
+          }
+          for (int j = 0; j < n; ++j) umma_commit(&sh.empty[(seq + j) % NS]);
+          seq += n;
+          kv_seq = seq;
+        }
+        auto issue_s = [&](int w) {
+          const int t = BLOCKS == 2 ? w >> 1 : w, g = w & 1, qs = kv_seq + 2 * t, i = qs % NS;
+          if (!pwait(&sh.full[i], (qs / NS) & 1, sh, a)) {
+            ok = false;
+            return;
+          }
+          tc_fence_after();
+          const int n16 = (s.valid(k0 + t) + 15) & ~15;
+          const uint32_t id = idesc_bf16(128, 16, 0, 0) + ((uint32_t)(n16 - 16) >> 3 << 17);
+          const uint64_t da = dQ + (BLOCKS == 2 ? g * (kSlot >> 4) : 0), db = dR + i * (kSlot >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            umma_bf16(tm + cS + g * 128, da + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2,
+                      db + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, id, kk > 0 ? 1u : 0u);
+          umma_commit(&sh.s_full[g]);
+          if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
+        };
+        for (int w = 0; ok && w < 2; ++w) {
+          // the moment product's tensor memory has been read before S is written there
+          if (mom && a.order == 1 && w < BLOCKS) {
+            if (!pwait(&sh.p_ready[w], np[w] & 1, sh, a)) ok = false;
+            ++np[w];
+          }
+          if (ok && w < W) issue_s(w);
+        }
+        for (int w = 0; ok && w < W; ++w) {
+          const int t = BLOCKS == 2 ? w >> 1 : w, g = w & 1, vs = kv_seq + 2 * t + 1, i = vs % NS;
+          ok = pwait(&sh.full[i], (vs / NS) & 1, sh, a) && pwait(&sh.p_ready[g], np[g] & 1, sh, a);
+          ++np[g];
+          if (!ok) break;
+          tc_fence_after();
+          const int steps = (s.valid(k0 + t) + 15) >> 4;
+          const bool fresh = w < 2 && !(mom && (BLOCKS == 2 || g == 0));
+          const uint32_t id = idesc_bf16(128, D, 0, 1);
+          for (int kk = 0; kk < steps; ++kk)
+            umma_bf16_ts(tm + cO + g * D, tm + cS + g * 128 + kk * 8, dV + i * (kSlot >> 4) + kk * 128, id,
+                         (kk > 0 || !fresh) ? 1u : 0u);
+          if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
+          if (w + 2 < W) issue_s(w + 2);
+        }
+        umma_commit(&sh.q_empty);
+        umma_commit(&sh.o_full);
+        seq = kv_seq + 2 * (k1 - k0);
+      }
+      umma_commit(&sh.mma_done);
+    }
+  } else {
+    // ---- softmax groups: thread r of group g has row r of a block
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int g = warp >> 2, r = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
+    const uint32_t tS = tm + lanes + cS + g * 128, tO = tm + lanes + cO + g * D;
+    const float scale = rsqrtf(static_cast<float>(D)), qs = scale * kLog2e;
+    const int G = 1 << p.g_shift, HQ = a.n_kv << p.g_shift;
+    uint32_t nq = 0, nc = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots consumed
+    int seg = 0;
+    while (walk.next(a, p, s)) {
+      const bool mom = s.moments();
+      const int k0 = s.k0(), k1 = s.k1(), b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
+      const bool active = mom || k1 > k0;
+      const int node = s.first + ((BLOCKS == 2 ? g * kTile + r : r) >> p.g_shift), h = r & (G - 1);
+      const bool live = node < s.it.count;
+      const bool warp_live = __any_sync(kAll, live);
+      const bool mine = BLOCKS == 2 || g == 0;  // this group's block starts from the moment term
+      float m = kNegInf, l = 0.f;
+      bool started = false;
+      if (mom) {
+        const float nf = static_cast<float>(s.it.n_e);
+        if (a.order == 1) {
+          // C' as the operand of Q C'^T: 16-byte chunks of 8 columns, hi and lo parts
+          constexpr int kChunks = D * D / 8 / 256;
+          (void)pwait(&sh.c_grant, nc & 1, sh, a);
+          ++nc;
+          uint8_t* hi = ring + (vseq % NS) * kSlot;
+          uint8_t* lo = ring + ((vseq + 1) % NS) * kSlot;
+          vseq += a.C16 != nullptr ? 1 : 2;
+#pragma unroll
+          for (int j = 0; j < kChunks; ++j) {
+            const int c = j * 256 + tid, row = c / (D / 8), col = (c % (D / 8)) * 8;
+            const size_t at = ((size_t)s.unit * D + row) * D + col;
+            const uint32_t off = swz_off(row, col, D);
+            if (a.Cs != nullptr) {
+              const uint4 x = *reinterpret_cast<const uint4*>(a.Cs + at / 2);
+              const uint4 y = *reinterpret_cast<const uint4*>(a.Cs + at / 2 + 2);
+              *reinterpret_cast<uint4*>(hi + off) = make_uint4(x.x, x.z, y.x, y.z);
+              *reinterpret_cast<uint4*>(lo + off) = make_uint4(x.y, x.w, y.y, y.w);
+            } else {
+              float x[8];
+              if (a.C16 != nullptr) {
+                load_bf16<8>(a.C16 + at, x);
+              } else {
+                const float4 x0 = *reinterpret_cast<const float4*>(a.C + at);
+                const float4 x1 = *reinterpret_cast<const float4*>(a.C + at + 4);
+                x[0] = x0.x, x[1] = x0.y, x[2] = x0.z, x[3] = x0.w;
+                x[4] = x1.x, x[5] = x1.y, x[6] = x1.z, x[7] = x1.w;
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                if (fabsf(x[i] * nf) < a.tau) x[i] = 0.f;
+              *reinterpret_cast<uint4*>(hi + off) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                               pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+              if (a.C16 == nullptr) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = bf16_residual(x[i]);
+                *reinterpret_cast<uint4*>(lo + off) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                                 pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+              }
+            }
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.c_full);
+        }
+        (void)pwait(&sh.q_full, nq & 1, sh, a);
+        if (mine) {
+          float e = 0.f;
+          const float2* mk = reinterpret_cast<const float2*>(a.mu_k + (size_t)s.unit * D);
+          const float4* mv = reinterpret_cast<const float4*>(a.mu_v + (size_t)s.unit * D);
+          const uint8_t* row = sQ + (BLOCKS == 2 ? g * kSlot : 0) + r * 128;
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4*>(row + (c >> 3) * kBox + (((c & 7) ^ (r & 7)) << 4));
+            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
+              const float2 k2 = __ldg(mk + c * 4 + i);
+              e = fmaf(f.x, k2.x, e);
+              e = fmaf(f.y, k2.y, e);
+            }
+          }
+          m = fmaf(e, qs, log2f(nf));
+          l = 1.f;
+          started = true;
+          if (a.order == 1) {
+            (void)pwait(&sh.s_full[g], ns & 1, sh, a);
+            ++ns;
+            tc_fence_after();
+          }
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t f[32];
+            if (a.order == 1) {
+              tmem_ld32_async(tS + c, f);
+              tmem_wait_ld();
+              keep16(f);
+              keep16(f + 16);
+            }
+            const float by = a.order == 1 ? scale : 0.f;
+            if (a.order != 1)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) f[i] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float4 v4 = __ldg(mv + c / 4 + i);
+              f[4 * i] = __float_as_uint(fmaf(__uint_as_float(f[4 * i]), by, v4.x));
+              f[4 * i + 1] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 1]), by, v4.y));
+              f[4 * i + 2] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 2]), by, v4.z));
+              f[4 * i + 3] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 3]), by, v4.w));
+            }
+            tmem_st16(tO + c, f);
+            tmem_st16(tO + c + 16, f + 16);
+          }
+          tmem_wait_st();
+          if (a.order == 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.p_ready[g]);
+          }
+        }
+      }
+      if (active) {
+        ++nq;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_empty);  // (with the MMA thread's commit: Q may be replaced)
+      }
+      const uint32_t seg_seq = vseq;  // of the first K tile
+      vseq += 2 * (k1 - k0);
+      for (int j = k0 + (BLOCKS == 2 ? 0 : g); j < k1; j += BLOCKS == 2 ? 1 : 2) {
+        const int valid = s.valid(j);
+        const bool tree = j >= s.it.cache;
+        uint32_t words[4];
+        if (tree) {  // the bits of this row and tile
+          const int w0 = (j - s.it.cache) * 4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            words[i] = 0;
+            if (live && w0 + i < p.words) words[i] = a.mask[((size_t)b * a.N + node) * p.words + w0 + i];
+            const int n = valid - i * 32;
+            words[i] &= n >= 32 ? kAll : n <= 0 ? 0u : (1u << n) - 1u;
+          }
+        }
+        if (tree || valid % 16 != 0) {
+          // V rows past the keys in use must be finite (their weights are 0),
+          // and so must a node's value where its weight is 0: elements that
+          // are not are taken out here and reach the nodes that see them at
+          // the end
+          const uint32_t sv = seg_seq + 2 * (j - k0) + 1;
+          uint8_t* tv = ring + (sv % NS) * kSlot;
+          (void)pwait(&sh.full[sv % NS], (sv / NS) & 1, sh, a);
+          const int end = (valid + 15) & ~15;
+          for (int c = r; c < (end - valid) * (D / 8); c += kTile) {
+            const int row = valid + c / (D / 8), x = c % (D / 8);
+            *reinterpret_cast<uint4*>(tv + (x >> 3) * kBox + row * 128 + ((x & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          if (tree) {
+            for (int c = r; c < valid * (D / 8); c += kTile) {
+              const int row = c / (D / 8), x = c % (D / 8);
+              uint4* at = reinterpret_cast<uint4*>(tv + (x >> 3) * kBox + row * 128 + ((x & 7) << 4));
+              uint4 w = *at;
+              if (odd2(w.x) || odd2(w.y) || odd2(w.z) || odd2(w.w)) {
+                const int n = (j - s.it.cache) * kTile + row;
+                atomicOr(&sh.odd[seg & 1][n >> 5], 1u << (n & 31));
+                __threadfence_block();  // (the other group may find the zeros instead)
+                uint32_t* y = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  if ((y[i] & 0x7f80u) == 0x7f80u) y[i] &= 0xffff0000u;
+                  if ((y[i] & 0x7f800000u) == 0x7f800000u) y[i] &= 0xffffu;
+                }
+                *at = w;
+              }
+            }
+          }
+          fence_async_smem();
+        }
+        (void)pwait(&sh.s_full[g], ns & 1, sh, a);
+        ++ns;
+        tc_fence_after();
+        if (warp_live) {
+          uint32_t x[kTile];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + c * 32, x + c * 32);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < 8; ++c) keep16(x + c * 16);
+          if (tree || valid < kTile) {
+#pragma unroll
+            for (int i = 0; i < kTile; ++i) {
+              const bool on = tree ? (words[i >> 5] >> (i & 31)) & 1u : i < valid;
+              if (!on) x[i] = 0xff800000u;  // -inf
+            }
+          }
+          float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll
+          for (int i = 0; i < kTile; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qs;
+          if (__any_sync(kAll, top > m + kSlack)) {
+            const float mn = fmaxf(m, top);
+            const float f = mn == kNegInf ? 1.f : fast_exp2(m - mn);
+            m = mn;
+            if (started) {  // (S of this tile is complete, so every earlier product into O is)
+              l *= f;
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld32_async(tO + c, o);
+                tmem_wait_ld();
+                keep16(o);
+                keep16(o + 16);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st16(tO + c, o);
+                tmem_st16(tO + c + 16, o + 16);
+              }
+            }
+          }
+          const float ref = m == kNegInf ? 0.f : m;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < kTile; i += 2) {
+            const float p0 = fast_exp2(fmaf(__uint_as_float(x[i]), qs, -ref));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(x[i + 1]), qs, -ref));
+            sum[i & 3] += p0;
+            sum[(i & 3) + 1] += p1;
+            x[i >> 1] = pack_bf16x2(p0, p1);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_st16(tS + c * 16, x + c * 16);
+          tmem_wait_st();
+        }
+        started = true;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_ready[g]);
+      }
+
+      // ---- the segment's state: into the output (a whole item) or the workspace
+      if (active) {
+        (void)pwait(&sh.o_full, no & 1, sh, a);
+        ++no;
+        tc_fence_after();
+      }
+      grid_dependency_wait();  // (a no-op unless the loads went early)
+      const bool whole = s.whole();
+      const int part = 2 * blockIdx.x + (seg == 0 ? 0 : 1);
+      constexpr int R = BLOCKS * kTile;
+      uint32_t seen_odd[8];
+      bool any_odd = false;
+      if (BLOCKS == 1 && g == 1) sh.ml[r] = make_float2(m, started ? l : 0.f);
+      named_sync(1, 256);  // the other group's state; the nodes' odd values are known
+      if (live && k1 > s.it.cache) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          seen_odd[i] = sh.odd[seg & 1][i];
+          any_odd |= seen_odd[i] != 0;
+        }
+        if (any_odd)
+          for (int i = 0; i < 8; ++i)
+            seen_odd[i] = i < p.words ? seen_odd[i] & a.mask[((size_t)b * a.N + node) * p.words + i] : 0u;
+      }
+      // O = f0 O_0 + f1 O_1 over the columns this thread writes
+      float M = m, L = started ? l : 0.f, f0 = L != 0.f ? 1.f : 0.f, f1 = 0.f;
+      if (BLOCKS == 1 && g == 0) {
+        const float2 y = sh.ml[r];
+        M = fmaxf(L != 0.f ? m : kNegInf, y.y != 0.f ? y.x : kNegInf);
+        const float ref = M == kNegInf ? 0.f : M;
+        f0 = L != 0.f ? fast_exp2(m - ref) : 0.f;
+        f1 = y.y != 0.f ? fast_exp2(y.x - ref) : 0.f;
+        L = (L != 0.f ? L * f0 : 0.f) + (y.y != 0.f ? y.y * f1 : 0.f);
+      }
+      if (whole) {
+        const float inv = L != 0.f ? 1.f / L : 0.f;
+        f0 *= inv, f1 *= inv;
+      }
+      if (BLOCKS == 1) {
+        if (g == 0) sh.ml[r] = make_float2(f0, f1);
+        named_sync(1, 256);
+        f0 = sh.ml[r].x, f1 = sh.ml[r].y;
+      }
+      // a factor of 0 stands for a state without content: its columns may hold anything
+      const bool use0 = f0 != 0.f, use1 = f1 != 0.f;
+      const bool put = node < a.N;
+      const size_t orow = ((size_t)b * a.N + node) * HQ + (kv << p.g_shift) + h;
+      constexpr int kCols = BLOCKS == 2 ? D : D / 2;
+      const int c_lo = BLOCKS == 2 ? 0 : g * (D / 2);
+      const uint32_t tA = tm + lanes + cO + (BLOCKS == 2 ? g * D : 0) + c_lo, tB = tA + D;
+#pragma unroll 1
+      for (int c = 0; c < kCols; c += 32) {
+        uint32_t x[32], y[32];
+        tmem_ld32_async(tA + c, x);
+        if (BLOCKS == 1) tmem_ld32_async(tB + c, y);
+        tmem_wait_ld();
+        keep16(x), keep16(x + 16);
+        if (BLOCKS == 1) keep16(y), keep16(y + 16);
+        float o[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          o[i] = use0 ? __uint_as_float(x[i]) * f0 : 0.f;
+          if (BLOCKS == 1 && use1) o[i] = fmaf(__uint_as_float(y[i]), f1, o[i]);
+        }
+        if (any_odd) {
+#pragma unroll 1
+          for (int w = 0; w < 8; ++w)
+            for (uint32_t bits = seen_odd[w]; bits != 0; bits &= bits - 1) {
+              const int n = w * 32 + __ffs(bits) - 1;
+              const int j = s.it.cache + (n >> 7);
+              if (j < k0 || j >= k1 || n >= s.it.count) continue;
+              const __nv_bfloat16* v =
+                  static_cast<const __nv_bfloat16*>(a.v) + b * a.kv_batch + n * a.kv_node + kv * D + c_lo + c;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float z = __bfloat162float(v[i]);
+                if (!isfinite(z)) o[i] += z;
+              }
+            }
+        }
+        if (whole) {
+          if (put) {
+            uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c_lo + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              dst[i] = live ? make_uint4(pack_bf16x2(o[8 * i], o[8 * i + 1]), pack_bf16x2(o[8 * i + 2], o[8 * i + 3]),
+                                         pack_bf16x2(o[8 * i + 4], o[8 * i + 5]), pack_bf16x2(o[8 * i + 6], o[8 * i + 7]))
+                            : make_uint4(0, 0, 0, 0);
+          }
+        } else {
+          const int row = BLOCKS == 2 ? g * kTile + r : r;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            parts.o[((size_t)part * (D / 4) + (c_lo + c) / 4 + i) * R + row] =
+                make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        }
+      }
+      if (BLOCKS == 2 || g == 0) {
+        if (whole) {
+          if (put && a.lse != nullptr) a.lse[orow] = live && L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
+        } else {
+          parts.ml[(size_t)part * R + (BLOCKS == 2 ? g * kTile + r : r)] = make_float2(M, L);
+        }
+      }
+      if (tid < 8) sh.odd[(seg + 1) & 1][tid] = 0;  // (read last in the segment before)
+      ++seg;
+      tc_fence_before();
+      named_sync(1, 256);  // both groups are done with O and the exchange
+    }
+    if (p.list && tid == 0)  // a boundary inside an item: what tree_merge_kernel joins
+      parts.desc[blockIdx.x] = sh.left > 0 ? make_int4(static_cast<int>(sh.start), static_cast<int>(sh.run), sh.unit, sh.mb)
+                                           : make_int4(-1, 0, 0, 0);
   }
+
+  __syncthreads();
+  if (warp == 9) {
+    if (lane == 0) {
+      if (sh.abort) {  // wait, with the full limit, for the copies in flight
+        for (int i = 0; i < NS; ++i) {
+          const int last = sh.issued - 1 - ((sh.issued - 1 - i) % NS + NS) % NS;  // the last use of slot i
+          if (last >= 0) (void)mbar_wait(&sh.full[i], (last / NS) & 1);
+        }
+        if (sh.q_issued > 0) (void)mbar_wait(&sh.q_full, (sh.q_issued - 1) & 1);
+      }
+      (void)mbar_wait(&sh.mma_done, 0);  // no product or arrival is left
+    }
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tm, 512);
+  }
+}
+
+// Joins the parts of the items that a boundary of the list cuts: block (c, y)
+// the item whose first inner boundary is CTA c's, y the columns 8 y .. 8 y + 7,
+// a thread a row and 4 columns.
+template <int D>
+__global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
+                                                         const __grid_constant__ Plan p,
+                                                         const __grid_constant__ Parts parts) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int4 d = parts.desc[blockIdx.x];
+  if (d.x < 0) return;
+  const int R = p.blocks * kTile, row = blockIdx.z * kTile + (threadIdx.x & 127), c4 = blockIdx.y * 2 + (threadIdx.x >> 7);
+  const int G = 1 << p.g_shift, u = d.z, b = u / a.n_kv, kv = u % a.n_kv;
+  const int node = d.w * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
+  if (node >= a.N) return;
+  const int count = a.count != nullptr ? a.count[b] : a.N;
+  const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
+  const int n = d.y - blockIdx.x + 2;  // parts: the first one, then one per CTA up to the last
+  auto part = [&](int i) { return i == 0 ? d.x : 2 * (static_cast<int>(blockIdx.x) + i - 1); };
+  float M = kNegInf, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < n; ++i) {
+    const float2 x = parts.ml[(size_t)part(i) * R + row];
+    if (x.y != 0.f) M = fmaxf(M, x.x);
+  }
+  const float ref = M == kNegInf ? 0.f : M;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const float2 x = parts.ml[(size_t)part(i) * R + row];
+    const float4 o = parts.o[((size_t)part(i) * (D / 4) + c4) * R + row];
+    if (x.y != 0.f) {
+      const float f = fast_exp2(x.x - ref);
+      L = fmaf(x.y, f, L);
+      acc.x = fmaf(o.x, f, acc.x);
+      acc.y = fmaf(o.y, f, acc.y);
+      acc.z = fmaf(o.z, f, acc.z);
+      acc.w = fmaf(o.w, f, acc.w);
+    }
+  }
+  const bool live = node < min(max(count, 0), a.N) && L != 0.f;
+  const float inv = live ? 1.f / L : 0.f;
+  *reinterpret_cast<uint2*>(a.out + orow * D + c4 * 4) =
+      live ? make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0, 0);
+  if (c4 == 0 && a.lse != nullptr) a.lse[orow] = live ? (M + log2f(L)) * kLn2 : kNegInf;
+}
+
+Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
+  Plan p{};
+  const int rows = n_nodes * g.group;
+  p.blocks = rows > kTile ? 2 : 1;
+  p.mb = (rows + p.blocks * kTile - 1) / (p.blocks * kTile);
+  p.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
+  p.words = tree_words(n_nodes);
+  const long units = (long)g.batch * g.n_kv_heads, items = units * p.mb;
+  const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
+  p.min_run = 2;
+  p.list = units <= kScanUnits && tiles > 4 ? 1 : 0;
+  p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (items * tiles + p.min_run - 1) / p.min_run))
+                  : static_cast<int>(items);
+  return p;
+}
+
+size_t parts_bytes(const mkv_geom& g, const Plan& p) {
+  if (!p.list) return 0;
+  const size_t R = (size_t)p.blocks * kTile;
+  return align_up((size_t)p.grid * sizeof(int4), 256) + 2 * (size_t)p.grid * R * (8 + (size_t)g.head_dim * 4);
+}
+
+// bf16 [n3][n2][n1][inner] with the strides of n1, n2, n3 in elements; boxes of b1 x b2 rows of 64 elements.
+bool encode_4d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t n1, uint64_t n2, uint64_t n3, uint64_t s1,
+               uint64_t s2, uint64_t s3, uint32_t b1, uint32_t b2) {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  });
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[4] = {inner, n1, n2, n3}, strides[3] = {s1 * 2, s2 * 2, s3 * 2};
+  const cuuint32_t box[4] = {64, b1, b2, 1}, step[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int BLOCKS>
+cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, const CUtensorMap (&tm)[5],
+                        cudaStream_t stream) {
+  constexpr int smem = smem_bytes(D, BLOCKS);
+  cudaError_t e = cudaFuncSetAttribute(tree_step_kernel<D, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
+                 tm[3], tm[4]);
+  if (e != cudaSuccess || !p.list) return e;
+  return launch_pdl(tree_merge_kernel<D>, dim3(p.grid, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts);
 }
 
 }  // namespace
 
-size_t tree_workspace_bytes(const mkv_geom&, int32_t, int32_t, int) { return kHeaderBytes; }
+size_t tree_workspace_bytes(const mkv_geom& g, int32_t n_nodes, int32_t capacity, int num_sms) {
+  return kHeaderBytes + parts_bytes(g, make_plan(g, n_nodes, capacity, num_sms));
+}
 
-cudaError_t launch_tree_step(const TreeArgs& a, const mkv_geom& g, int, cudaStream_t stream) {
-  const dim3 grid(a.N, g.n_kv_heads, g.batch);
-#define MKV_TREE_CASE(D_, G_)                                                 \
-  if (g.head_dim == D_ && g.group == G_) {                                    \
-    tree_step_kernel<D_, G_><<<grid, kWarps * 32, 0, stream>>>(a);            \
-    return cudaGetLastError();                                                \
-  }
-  MKV_TREE_CASE(128, 1)
-  MKV_TREE_CASE(128, 2)
-  MKV_TREE_CASE(128, 4)
-  MKV_TREE_CASE(128, 8)
-  MKV_TREE_CASE(64, 1)
-  MKV_TREE_CASE(64, 2)
-  MKV_TREE_CASE(64, 4)
-  MKV_TREE_CASE(64, 8)
-#undef MKV_TREE_CASE
-  return cudaErrorInvalidValue;
+cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
+  TreeArgs a = args;
+  a.polls = pipeline_poll_limit();
+  const Plan p = make_plan(g, a.N, a.cap, num_sms);
+  Parts parts{};
+  const int D = g.head_dim, R = p.blocks * kTile;
+  uint8_t* w = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
+  parts.desc = reinterpret_cast<int4*>(w);
+  w += align_up((size_t)p.grid * sizeof(int4), 256);
+  parts.o = reinterpret_cast<float4*>(w);
+  w += 2 * (size_t)p.grid * R * D * 4;
+  parts.ml = reinterpret_cast<float2*>(w);
+  const uint64_t hq = (uint64_t)a.n_kv * g.group, units = (uint64_t)a.batch * a.n_kv, d = D;
+  CUtensorMap tm[5];
+  if (!encode_4d(&tm[0], a.q, d, hq, a.N, a.batch, d, a.q_node, a.q_batch, g.group, kTile / g.group) ||
+      !encode_tmap_bf16_3d(&tm[1], a.K, d, a.cap, units, d * 2, (uint64_t)a.cap * d * 2, kTile) ||
+      !encode_tmap_bf16_3d(&tm[2], a.V, d, a.cap, units, d * 2, (uint64_t)a.cap * d * 2, kTile) ||
+      !encode_4d(&tm[3], a.k, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile) ||
+      !encode_4d(&tm[4], a.v, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile))
+    return cudaErrorInvalidValue;
+  if (D == 128)
+    return p.blocks == 2 ? launch_step<128, 2>(a, p, parts, tm, stream) : launch_step<128, 1>(a, p, parts, tm, stream);
+  return p.blocks == 2 ? launch_step<64, 2>(a, p, parts, tm, stream) : launch_step<64, 1>(a, p, parts, tm, stream);
 }
 
 }  // namespace mkv
