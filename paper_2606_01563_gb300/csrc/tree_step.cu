@@ -23,10 +23,14 @@
 // rows) every K and V tile is read once for 256 rows, with one the two
 // softmax groups take the tiles alternately and merge at the end.
 //
-// One CTA, three warpgroups: warps 0-3 and 4-7 are the softmax groups, a thread
-// a row; warp 8 issues TMA copies (Q, and K and V tiles into a ring), warp 9
-// the MMAs.  Tensor memory: S (then P over it) of the two groups, 128 columns
-// each, and O of the two, D columns each.
+// One CTA, ten warps: warps 0-3 and 4-7 are the softmax groups, a thread a row;
+// warp 8 issues TMA copies (Q, and K and V tiles into a ring), warp 9 the MMAs:
+// S of both groups first, then in turn a group's product with V and its next
+// S, so that one group's softmax runs beside the other's products.  Code that
+// runs once per item is kept in loops: unrolled, it waited for its own
+// instructions (a masked tile took 9000 cycles instead of 2000).
+// Tensor memory: S (then P over it) of the two groups, 128 columns each, and O
+// of the two, D columns each.
 #include <algorithm>
 #include <mutex>
 
@@ -42,12 +46,9 @@ namespace {
 
 constexpr int kTile = 128;                   // keys per tile, rows per block
 constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
-constexpr int kThreads = 384;                // 2 softmax groups; the TMA warp, the MMA warp and two idle ones
-// registers per thread: 168 at the launch (3 x 168 = 504 for a warp of each group), then 224 for the softmax
-// groups, whose threads hold a row of 128 scores, and 56 for the others
-constexpr int kSoftmaxRegs = 224, kIssueRegs = 56;
-static_assert(2 * kSoftmaxRegs + kIssueRegs <= 3 * 168, "the block's registers at its launch");
-constexpr int kScanUnits = 4096;             // above: one CTA per item, without a list
+constexpr int kThreads = 320;                // 2 softmax groups, the TMA warp, the MMA warp
+constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
 constexpr float kSlack = 8.f;                // log2 headroom of the reference (weights <= 2^8)
 constexpr float kNegInf = -INFINITY;
 constexpr uint32_t kAll = 0xffffffffu;
@@ -78,11 +79,14 @@ struct Shared {
   uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], o_full, mma_done;
   uint32_t tmem;
   int32_t abort, issued, q_issued;
-  int32_t unit, mb, t0;
-  long long left, start, run;
-  uint32_t odd[2][8];  // nodes with a value that is not finite, of this segment and the next
-  float2 ml[kTile];  // (one row block) group 1's (m, l), then the two groups' factors
-  long long scan[kThreads / 32];
+  int32_t unit, mb, t0, left;  // the CTA's run of the list: first item, tile in it, tiles
+  int4 cut;                    // parts.desc of this CTA
+  uint32_t odd[2][8];          // nodes with a value that is not finite, of this segment and the next
+  union {
+    float mu[2][kTile];  // mu_k and mu_v, while a segment takes its moment term in
+    float2 ml[kTile];    // (one row block) at its end: group 1's (m, l), then the two groups' factors
+  };
+  int32_t scan[kThreads / 32];
 };
 constexpr int kSharedBytes = 2048;
 static_assert(sizeof(Shared) <= kSharedBytes, "shared variables");
@@ -138,24 +142,90 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+// Two floats in one 64-bit register, and two operations per instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^d of a whole number d <= 0, exactly (0 below the smallest normal number).
+__device__ __forceinline__ float pow2(float d) {
+  return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
+}
+// O's columns of this warp's rows times the row's factor.
+template <int D>
+__device__ __forceinline__ void scale_columns(uint32_t tO, float f) {
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t o[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]),
+          "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+        : "r"(tO + c));
+    tmem_wait_ld();
+    keep16(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st16(tO + c, o);
+  }
+}
+// The weights (pairs of bf16) of the first n times 32 columns times the row's factor, a power of two.
+__device__ __forceinline__ void scale_weights(uint32_t tS, int n, float f) {
+#pragma unroll 1
+  for (int c = 0; c < n; ++c) {
+    uint32_t o[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]),
+          "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+        : "r"(tS + c * 16));
+    tmem_wait_ld();
+    keep16(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&o[i]));
+      o[i] = pack_bf16x2(x.x * f, x.y * f);
+    }
+    tmem_st16(tS + c * 16, o);
+  }
+}
+
 // Whether any of a word's two bf16 values is infinite or NaN.
 __device__ __forceinline__ bool odd2(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
-// What a unit's item consists of.
+// What a unit's items consist of.
 struct Item {
   int len, count, n_e;
   int head, cache, nodes;  // tiles: the moment term (0 or 1), the cache, the nodes
 };
 
-__device__ __forceinline__ Item load_item(const TreeArgs& a, int u) {
+struct Raw {  // as read, so that a read can be in flight until it is needed
+  int len, count, n_e;
+};
+__device__ __forceinline__ Raw load_raw(const TreeArgs& a, int u) {
+  return Raw{a.len[u], a.count != nullptr ? a.count[u / a.n_kv] : a.N, a.n != nullptr ? a.n[u] : 0};
+}
+__device__ __forceinline__ Item make_item(const TreeArgs& a, const Raw& r) {
   Item it;
-  const int b = u / a.n_kv;
-  const int len = a.len[u], count = a.count != nullptr ? a.count[b] : a.N;
-  it.n_e = a.n != nullptr ? a.n[u] : 0;
-  it.len = min(max(len, 0), a.cap);
-  it.count = min(max(count, 0), a.N);
+  it.len = min(max(r.len, 0), a.cap);
+  it.count = min(max(r.count, 0), a.N);
+  it.n_e = r.n_e;
   it.head = a.n != nullptr ? 1 : 0;
   it.cache = (it.len + kTile - 1) / kTile;
   it.nodes = (it.count + kTile - 1) / kTile;
@@ -170,38 +240,38 @@ __device__ __forceinline__ int item_tiles(const Item& it, int first) {
 struct Segment {
   int unit, mb, first;  // first node of the item's rows
   int begin, end, tiles;
+  int k0, k1;  // key tiles: the cache's, then the nodes'
   Item it;
-  bool live;
-  __device__ __forceinline__ bool moments() const { return live && begin == 0 && it.head > 0 && it.n_e > 0; }
-  // key tiles [k0, k1): the head is tile 0 when there is one
-  __device__ __forceinline__ int k0() const { return live ? max(begin - it.head, 0) : 0; }
-  __device__ __forceinline__ int k1() const { return live ? max(end - it.head, 0) : 0; }
-  __device__ __forceinline__ bool whole() const { return begin == 0 && end == tiles; }
+  bool live, mom;
   // keys in use of key tile j
   __device__ __forceinline__ int valid(int j) const {
-    return j < it.cache ? min(kTile, it.len - j * kTile) : min(kTile, it.count - (j - it.cache) * kTile);
+    return min(kTile, (j < it.cache ? it.len : it.count + it.cache * kTile) - j * kTile);
   }
 };
 
 struct Walk {
-  int unit, mb, t;
-  long long left;
+  int unit, mb, t, left;
+  Raw raw;
   __device__ __forceinline__ bool next(const TreeArgs& a, const Plan& p, Segment& s) {
     if (left <= 0) return false;
     s.unit = unit;
     s.mb = mb;
     s.first = mb * ((p.blocks * kTile) >> p.g_shift);
-    s.it = load_item(a, unit);
+    s.it = make_item(a, raw);
     s.live = s.first < s.it.count;
     s.tiles = item_tiles(s.it, s.first);
     s.begin = t;
-    s.end = static_cast<int>(min((long long)s.tiles, t + left));
+    s.end = min(s.tiles, t + left);
+    s.mom = s.live && t == 0 && s.it.head > 0 && s.it.n_e > 0;
+    s.k0 = s.live ? max(s.begin - s.it.head, 0) : 0;
+    s.k1 = s.live ? max(s.end - s.it.head, 0) : 0;
     left -= s.end - s.begin;
     t = 0;
     if (++mb == p.mb) {
       mb = 0;
       ++unit;
     }
+    if (left > 0) raw = load_raw(a, unit);
     return true;
   }
 };
@@ -209,6 +279,7 @@ struct Walk {
 // Pipeline wait that gives up after `polls` polls: records the timeout once and
 // raises the CTA's abort flag; every later wait then passes at once.
 __device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, Shared& sh, const TreeArgs& a) {
+  if (mbar_try_wait(bar, parity)) return true;
   volatile int32_t* abort = &sh.abort;
   if (*abort) return false;
   if (mbar_wait(bar, parity, a.polls)) return true;
@@ -219,88 +290,84 @@ __device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, Shared& sh
 
 // Where this CTA's run starts in the list of all items' tiles, and what it is
 // of an item that an earlier CTA began.
-template <int D>
-__device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Shared& sh, const Parts& parts) {
+__device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Shared& sh) {
   const int tid = threadIdx.x, units = a.batch * a.n_kv;
-  const int per_cta = (p.blocks * kTile) >> p.g_shift;  // nodes per item
-  auto record = [&](int u) {
-    const int len = a.len[u], count = a.count != nullptr ? a.count[u / a.n_kv] : a.N;
-    if (len < 0 || len > a.cap) record_error(a.ws, MKV_ERR_CAPACITY, u);
-    if (count < 0 || count > a.N) record_error(a.ws, MKV_ERR_INVALID_ARG, u);
+  const int nodes = (p.blocks * kTile) >> p.g_shift;  // of an item
+  auto record = [&](int u, const Raw& r) {
+    if (r.len < 0 || r.len > a.cap) record_error(a.ws, MKV_ERR_CAPACITY, u);
+    if (r.count < 0 || r.count > a.N) record_error(a.ws, MKV_ERR_INVALID_ARG, u);
   };
   if (!p.list) {
     if (tid == 0) {
       sh.unit = blockIdx.x / p.mb;
       sh.mb = blockIdx.x % p.mb;
       sh.t0 = 0;
-      const Item it = load_item(a, sh.unit);
-      sh.left = item_tiles(it, sh.mb * per_cta);
-      if (sh.mb == 0) record(sh.unit);
+      const Raw r = load_raw(a, sh.unit);
+      sh.left = item_tiles(make_item(a, r), sh.mb * nodes);
+      if (sh.mb == 0) record(sh.unit, r);
     }
     __syncthreads();
     return;
   }
-  auto weight = [&](int u) {
-    const Item it = load_item(a, u);
-    const int alive = (it.count + per_cta - 1) / per_cta;
-    return (long long)alive * item_tiles(it, 0) + (p.mb - alive);
+  // (alive items, tiles of one) of a unit; the others weigh one tile each
+  auto weigh = [&](const Raw& r, int& tiles) {
+    const Item it = make_item(a, r);
+    const int alive = (it.count + nodes - 1) / nodes;
+    tiles = item_tiles(it, 0);
+    return alive;
   };
   const int chunk = (units + kThreads - 1) / kThreads, u0 = min(units, tid * chunk), u1 = min(units, u0 + chunk);
-  long long sum = 0;
+  int sum = 0;
+#pragma unroll 1
   for (int u = u0; u < u1; ++u) {
-    sum += weight(u);
-    if (blockIdx.x == 0) record(u);
+    const Raw r = load_raw(a, u);
+    int tiles;
+    const int alive = weigh(r, tiles);
+    sum += alive * tiles + (p.mb - alive);
+    if (blockIdx.x == 0) record(u, r);
   }
-  long long incl = sum;
+  int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(kAll, incl, o);
+    const int x = __shfl_up_sync(kAll, incl, o);
     if ((tid & 31) >= o) incl += x;
   }
   if ((tid & 31) == 31) sh.scan[tid >> 5] = incl;
-  if (tid == 0) sh.left = 0;
+  if (tid == 0) {
+    sh.left = 0;
+    sh.cut = make_int4(-1, 0, 0, 0);
+  }
   __syncthreads();
-  long long before = 0, total = 0;
+  int before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < (tid >> 5)) before += sh.scan[w];
-    total += sh.scan[w];
+    const int x = sh.scan[w];
+    if (w < (tid >> 5)) before += x;
+    total += x;
   }
-  const long long run = max((long long)p.min_run, (total + p.grid - 1) / p.grid);
-  const long long start = run * blockIdx.x;
-  long long at = before + incl - sum;  // of this thread's first unit
+  const int run = max(p.min_run, (total + p.grid - 1) / p.grid);
+  const int start = run * blockIdx.x;
+  int at = before + incl - sum;  // of this thread's first unit
   if (start >= at && start < at + sum) {
-    int u = u0;
-    long long w = weight(u);
-    while (start >= at + w) {
+    int u = u0, tiles, alive, w;
+    for (;; ++u) {
+      alive = weigh(load_raw(a, u), tiles);
+      w = alive * tiles + (p.mb - alive);
+      if (start < at + w) break;
       at += w;
-      w = weight(++u);
     }
-    const Item it = load_item(a, u);
-    const int tiles = item_tiles(it, 0), alive = (it.count + per_cta - 1) / per_cta;
-    long long in = start - at;  // the unit's tiles before the run
-    int mb, t0;
-    if (in < (long long)alive * tiles) {
-      mb = static_cast<int>(in / tiles);
-      t0 = static_cast<int>(in % tiles);
-    } else {
-      mb = alive + static_cast<int>(in - (long long)alive * tiles);
-      t0 = 0;
-    }
+    int in = start - at, mb = 0;  // the unit's tiles before the run
+    while (mb < alive && in >= tiles) in -= tiles, ++mb;
+    if (mb == alive) mb += in, in = 0;
     sh.unit = u;
     sh.mb = mb;
-    sh.t0 = t0;
+    sh.t0 = in;
     sh.left = min(run, total - start);
     // the first boundary inside an item sees to its merge: its first part is
     // the previous CTA's last segment (its only one if the item starts with
     // the run)
-    int4 d = make_int4(-1, 0, u, mb);
-    if (t0 > 0 && t0 <= run) {
-      d.x = 2 * (static_cast<int>(blockIdx.x) - 1) + (t0 == run ? 0 : 1);
-      d.y = static_cast<int>((start - t0 + tiles - 1) / run);
-    }
-    sh.start = d.x;
-    sh.run = d.y;
+    if (in > 0 && in <= run)
+      sh.cut = make_int4(2 * (static_cast<int>(blockIdx.x) - 1) + (in == run ? 0 : 1), (start - in + tiles - 1) / run, u, mb);
   }
   __syncthreads();
 }
@@ -341,18 +408,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_fence_init();
   }
   if (tid < 16) (&sh.odd[0][0])[tid] = 0;
-  if (warp == 9) tmem_alloc(&sh.tmem, 512);
+  if (warp == kWarpMma) tmem_alloc(&sh.tmem, 512);
   tc_fence_before();
   if (!a.early) grid_dependency_wait();
-  find_run<D>(a, p, sh, parts);  // (ends with a barrier)
+  find_run(a, p, sh);  // (ends with a barrier)
   tc_fence_after();
   const uint32_t tm = sh.tmem;
-  Walk walk{sh.unit, sh.mb, sh.t0, sh.left};
+  Walk walk{sh.unit, sh.mb, sh.t0, sh.left, {}};
+  if (walk.left > 0) walk.raw = load_raw(a, walk.unit);
   Segment s;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
-    if (warp == 8 && lane == 0) {  // ---- TMA
+  if (warp == kWarpTma) {
+    if (lane == 0) {  // ---- TMA
       int seq = 0, nq = 0;
       bool ok = true, waited = !a.early;
       const uint64_t pol = l2_evict_first();
@@ -369,8 +436,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         return i;
       };
       while (ok && walk.next(a, p, s)) {
-        const bool mom = s.moments();
-        if (!mom && s.k1() == s.k0()) continue;
+        const bool mom = s.mom;
+        if (!mom && s.k1 == s.k0) continue;
         const int b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
         auto load_q = [&] {
           wait_prior();
@@ -400,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (ok) mbar_arrive(&sh.c_grant);
         }
-        for (int j = s.k0(); ok && j < s.k1(); ++j) {
+        for (int j = s.k0; ok && j < s.k1; ++j) {
           const bool cache = j < s.it.cache;
           if (q_due && (!cache || seq + 2 > NS)) {  // what follows waits for others, or reads their output
             load_q();
@@ -424,89 +491,119 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       wait_prior();
     }
-    if (warp == 9 && lane == 0) {  // ---- MMA
+  } else if (warp == kWarpMma) {
+    if (lane == 0) {  // ---- MMA
       const uint64_t dQ = sdesc_sw128(smem_addr(sQ), 16, 1024), dR = sdesc_sw128(smem_addr(ring), 16, 1024);
       const uint64_t dV = sdesc_sw128(smem_addr(ring), kBox, 1024);
-      int seq = 0, nq = 0, nc = 0, np[2] = {0, 0};
+      constexpr uint32_t idS = idesc_bf16(128, kTile, 0, 0), idP = idesc_bf16(128, D, 0, 1);
+      int seq = 0;  // ring slots of the segments before
+      uint32_t qph = 0, cph = 0, pph = 0;  // phases; p_ready's in bit g
       bool ok = true;
+      // S of group g = Q K^T of the tile in slot i (n16 keys)
+      auto issue_s = [&](int g, int i, int n16) {
+        const uint64_t da = dQ + (BLOCKS == 2 ? g * (kSlot >> 4) : 0), db = dR + i * (kSlot >> 4);
+        const uint32_t id = idS - ((uint32_t)(kTile - n16) >> 3 << 17), t = tm + cS + g * 128;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          umma_bf16(t, da + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, db + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, id,
+                    kk > 0 ? 1u : 0u);
+        umma_commit(&sh.s_full[g]);
+        if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
+      };
       while (ok && walk.next(a, p, s)) {
-        const bool mom = s.moments();
-        const int k0 = s.k0(), k1 = s.k1();
-        if (!mom && k0 == k1) continue;
-        const int W = (k1 - k0) * BLOCKS;  // (tile, group) steps: group w & 1
-        ok = pwait(&sh.q_full, nq & 1, sh, a);
-        ++nq;
-        int kv_seq = seq;  // of the first K tile
-        if (ok && mom && a.order == 1) {
+        const int k0 = s.k0, k1 = s.k1;
+        if (!s.mom && k0 == k1) continue;
+        ok = pwait(&sh.q_full, qph, sh, a);
+        qph ^= 1;
+        int i = seq % NS;
+        uint32_t ph = (seq / NS) & 1;
+        auto advance = [&] {
+          if (++i == NS) i = 0, ph ^= 1;
+        };
+        const bool f_tiles = s.mom && a.order == 1;
+        if (f_tiles) {  // the moment term's value, Q C'^T, in the place of S
           const int n = a.C16 != nullptr ? 1 : 2;
-          ok = pwait(&sh.c_full, nc & 1, sh, a);
-          ++nc;
+          ok = ok && pwait(&sh.c_full, cph, sh, a);
+          cph ^= 1;
           if (!ok) break;
           tc_fence_after();
-          const uint32_t id = idesc_bf16(128, D, 0, 0);
-          for (int g = 0; g < BLOCKS; ++g) {
-            for (int j = 0; j < n; ++j) {
-              const uint64_t db = dR + ((seq + j) % NS) * (kSlot >> 4);
+          constexpr uint32_t id = idesc_bf16(128, D, 0, 0);
+          for (int j = 0; j < n; ++j) {
+            const uint64_t db = dR + i * (kSlot >> 4);
+            for (int g = 0; g < BLOCKS; ++g)
 #pragma unroll
               for (int kk = 0; kk < D / 16; ++kk)
                 umma_bf16(tm + cS + g * 128, dQ + g * (kSlot >> 4) + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2,
                           db + (kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2, id, (j > 0 || kk > 0) ? 1u : 0u);
-            }
-            umma_commit(&sh.s_full[g]);
+            umma_commit(&sh.empty[i]);
+            advance();
           }
-          for (int j = 0; j < n; ++j) umma_commit(&sh.empty[(seq + j) % NS]);
+          for (int g = 0; g < BLOCKS; ++g) umma_commit(&sh.s_full[g]);
           seq += n;
-          kv_seq = seq;
         }
-        auto issue_s = [&](int w) {
-          const int t = BLOCKS == 2 ? w >> 1 : w, g = w & 1, qs = kv_seq + 2 * t, i = qs % NS;
-          if (!pwait(&sh.full[i], (qs / NS) & 1, sh, a)) {
-            ok = false;
-            return;
-          }
+        // steps w = (tile, group w & 1): S of steps 0 and 1, then for every
+        // step its product with V and S of the group's next step
+        const int W = (k1 - k0) * BLOCKS;
+        int si = i;  // slot and phase of the next S step's K tile; (i, ph) of the next product's
+        uint32_t sph = ph;
+        int sw = 0;
+        auto next_s = [&] {
+          const int g = sw & 1, t = k0 + (BLOCKS == 2 ? sw >> 1 : sw);
+          ok = pwait(&sh.full[si], sph, sh, a);
+          if (!ok) return;
           tc_fence_after();
-          const int n16 = (s.valid(k0 + t) + 15) & ~15;
-          const uint32_t id = idesc_bf16(128, 16, 0, 0) + ((uint32_t)(n16 - 16) >> 3 << 17);
-          const uint64_t da = dQ + (BLOCKS == 2 ? g * (kSlot >> 4) : 0), db = dR + i * (kSlot >> 4);
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            umma_bf16(tm + cS + g * 128, da + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2,
-                      db + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, id, kk > 0 ? 1u : 0u);
-          umma_commit(&sh.s_full[g]);
-          if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
-        };
-        for (int w = 0; ok && w < 2; ++w) {
-          // the moment product's tensor memory has been read before S is written there
-          if (mom && a.order == 1 && w < BLOCKS) {
-            if (!pwait(&sh.p_ready[w], np[w] & 1, sh, a)) ok = false;
-            ++np[w];
+          issue_s(g, si, (s.valid(t) + 15) & ~15);
+          ++sw;
+          if (BLOCKS == 1 || g == 1) {
+            si += 2;
+            if (si >= NS) si -= NS, sph ^= 1;
           }
-          if (ok && w < W) issue_s(w);
+        };
+#pragma unroll 1
+        for (int g = 0; ok && g < 2; ++g) {
+          if (f_tiles && g < BLOCKS) {  // F has been read
+            ok = pwait(&sh.p_ready[g], (pph >> g) & 1, sh, a);
+            pph ^= 1u << g;
+          }
+          if (ok && g < W) next_s();
         }
+#pragma unroll 1
         for (int w = 0; ok && w < W; ++w) {
-          const int t = BLOCKS == 2 ? w >> 1 : w, g = w & 1, vs = kv_seq + 2 * t + 1, i = vs % NS;
-          ok = pwait(&sh.full[i], (vs / NS) & 1, sh, a) && pwait(&sh.p_ready[g], np[g] & 1, sh, a);
-          ++np[g];
+          const int g = w & 1, t = k0 + (BLOCKS == 2 ? w >> 1 : w);
+          int vi = i + 1;
+          uint32_t vph = ph;
+          if (vi == NS) vi = 0, vph ^= 1;
+          ok = pwait(&sh.full[vi], vph, sh, a) && pwait(&sh.p_ready[g], (pph >> g) & 1, sh, a);
+          pph ^= 1u << g;
           if (!ok) break;
           tc_fence_after();
-          const int steps = (s.valid(k0 + t) + 15) >> 4;
-          const bool fresh = w < 2 && !(mom && (BLOCKS == 2 || g == 0));
-          const uint32_t id = idesc_bf16(128, D, 0, 1);
-          for (int kk = 0; kk < steps; ++kk)
-            umma_bf16_ts(tm + cO + g * D, tm + cS + g * 128 + kk * 8, dV + i * (kSlot >> 4) + kk * 128, id,
-                         (kk > 0 || !fresh) ? 1u : 0u);
-          if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
-          if (w + 2 < W) issue_s(w + 2);
+          const uint64_t db = dV + vi * (kSlot >> 4);
+          const uint32_t tP = tm + cS + g * 128, tO = tm + cO + g * D;
+          const bool fresh = w < 2 && !(s.mom && (BLOCKS == 2 || g == 0));
+          const int steps = (s.valid(t) + 15) >> 4;
+          umma_bf16_ts(tO, tP, db, idP, fresh ? 0u : 1u);
+          if (steps == 8) {
+#pragma unroll
+            for (int kk = 1; kk < 8; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
+          } else {
+#pragma unroll 1
+            for (int kk = 1; kk < steps; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
+          }
+          if (BLOCKS == 1 || g == 1) {
+            umma_commit(&sh.empty[vi]);
+            advance();
+            advance();
+          }
+          if (sw < W) next_s();
         }
         umma_commit(&sh.q_empty);
         umma_commit(&sh.o_full);
-        seq = kv_seq + 2 * (k1 - k0);
+        seq += 2 * (k1 - k0);
       }
       umma_commit(&sh.mma_done);
     }
   } else {
     // ---- softmax groups: thread r of group g has row r of a block
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int g = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
     const uint32_t tS = tm + lanes + cS + g * 128, tO = tm + lanes + cO + g * D;
@@ -515,8 +612,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t nq = 0, nc = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots consumed
     int seg = 0;
     while (walk.next(a, p, s)) {
-      const bool mom = s.moments();
-      const int k0 = s.k0(), k1 = s.k1(), b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
+      const bool mom = s.mom;
+      const int k0 = s.k0, k1 = s.k1, b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
       const bool active = mom || k1 > k0;
       const int node = s.first + ((BLOCKS == 2 ? g * kTile + r : r) >> p.g_shift), h = r & (G - 1);
       const bool live = node < s.it.count;
@@ -526,44 +623,65 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool started = false;
       if (mom) {
         const float nf = static_cast<float>(s.it.n_e);
+        if (tid < 2 * D) {
+          const float* src = (tid < D ? a.mu_k : a.mu_v) + (size_t)s.unit * D;
+          sh.mu[tid >= D][tid & (D - 1)] = src[tid & (D - 1)];
+        }
         if (a.order == 1) {
           // C' as the operand of Q C'^T: 16-byte chunks of 8 columns, hi and lo parts
-          constexpr int kChunks = D * D / 8 / 256;
-          (void)pwait(&sh.c_grant, nc & 1, sh, a);
-          ++nc;
+          constexpr int kBatch = D == 128 ? 4 : 2, kRounds = D * D / 8 / 256 / kBatch;
           uint8_t* hi = ring + (vseq % NS) * kSlot;
           uint8_t* lo = ring + ((vseq + 1) % NS) * kSlot;
           vseq += a.C16 != nullptr ? 1 : 2;
+          const size_t base = (size_t)s.unit * D * D;
+#pragma unroll 1
+          for (int k = 0; k < kRounds; ++k) {
+            uint4 x[kBatch], y[kBatch];
 #pragma unroll
-          for (int j = 0; j < kChunks; ++j) {
-            const int c = j * 256 + tid, row = c / (D / 8), col = (c % (D / 8)) * 8;
-            const size_t at = ((size_t)s.unit * D + row) * D + col;
-            const uint32_t off = swz_off(row, col, D);
-            if (a.Cs != nullptr) {
-              const uint4 x = *reinterpret_cast<const uint4*>(a.Cs + at / 2);
-              const uint4 y = *reinterpret_cast<const uint4*>(a.Cs + at / 2 + 2);
-              *reinterpret_cast<uint4*>(hi + off) = make_uint4(x.x, x.z, y.x, y.z);
-              *reinterpret_cast<uint4*>(lo + off) = make_uint4(x.y, x.w, y.y, y.w);
-            } else {
-              float x[8];
-              if (a.C16 != nullptr) {
-                load_bf16<8>(a.C16 + at, x);
+            for (int j = 0; j < kBatch; ++j) {
+              const size_t at = base + ((k * kBatch + j) * 256 + tid) * 8;
+              const uint4* src = a.C16 != nullptr ? reinterpret_cast<const uint4*>(a.C16 + at)
+                                 : a.Cs != nullptr ? reinterpret_cast<const uint4*>(a.Cs + at / 2)
+                                                   : reinterpret_cast<const uint4*>(a.C + at);
+              x[j] = src[0];
+              if (a.C16 == nullptr) y[j] = src[1];
+            }
+            if (k == 0) {
+              (void)pwait(&sh.c_grant, nc & 1, sh, a);
+              ++nc;
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+              const int c = (k * kBatch + j) * 256 + tid;
+              const uint32_t off = swz_off(c / (D / 8), (c % (D / 8)) * 8, D);
+              if (a.Cs != nullptr) {
+                *reinterpret_cast<uint4*>(hi + off) = make_uint4(x[j].x, x[j].z, y[j].x, y[j].z);
+                *reinterpret_cast<uint4*>(lo + off) = make_uint4(x[j].y, x[j].w, y[j].y, y[j].w);
               } else {
-                const float4 x0 = *reinterpret_cast<const float4*>(a.C + at);
-                const float4 x1 = *reinterpret_cast<const float4*>(a.C + at + 4);
-                x[0] = x0.x, x[1] = x0.y, x[2] = x0.z, x[3] = x0.w;
-                x[4] = x1.x, x[5] = x1.y, x[6] = x1.z, x[7] = x1.w;
-              }
+                float v[8];
+                if (a.C16 != nullptr) {
+                  const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (fabsf(x[i] * nf) < a.tau) x[i] = 0.f;
-              *reinterpret_cast<uint4*>(hi + off) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                               pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-              if (a.C16 == nullptr) {
+                  for (int i = 0; i < 4; ++i) {
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+                    v[2 * i] = f.x, v[2 * i + 1] = f.y;
+                  }
+                } else {
+                  const uint32_t w[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = bf16_residual(x[i]);
-                *reinterpret_cast<uint4*>(lo + off) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                                 pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+                  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  if (fabsf(v[i] * nf) < a.tau) v[i] = 0.f;
+                *reinterpret_cast<uint4*>(hi + off) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                if (a.C16 == nullptr) {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) v[i] = bf16_residual(v[i]);
+                  *reinterpret_cast<uint4*>(lo + off) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                }
               }
             }
           }
@@ -571,27 +689,30 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.c_full);
         }
+        named_sync(1, 256);  // mu_k and mu_v are in place
         (void)pwait(&sh.q_full, nq & 1, sh, a);
         if (mine) {
-          float e = 0.f;
-          const float2* mk = reinterpret_cast<const float2*>(a.mu_k + (size_t)s.unit * D);
-          const float4* mv = reinterpret_cast<const float4*>(a.mu_v + (size_t)s.unit * D);
+          float e0 = 0.f, e1 = 0.f;
           const uint8_t* row = sQ + (BLOCKS == 2 ? g * kSlot : 0) + r * 128;
-#pragma unroll
+#pragma unroll 2
           for (int c = 0; c < D / 8; ++c) {
             const uint4 w = *reinterpret_cast<const uint4*>(row + (c >> 3) * kBox + (((c & 7) ^ (r & 7)) << 4));
             const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+            const float4 k0 = *reinterpret_cast<const float4*>(&sh.mu[0][c * 8]);
+            const float4 k1 = *reinterpret_cast<const float4*>(&sh.mu[0][c * 8 + 4]);
+            const float k[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
-              const float2 k2 = __ldg(mk + c * 4 + i);
-              e = fmaf(f.x, k2.x, e);
-              e = fmaf(f.y, k2.y, e);
+              e0 = fmaf(f.x, k[2 * i], e0);
+              e1 = fmaf(f.y, k[2 * i + 1], e1);
             }
           }
-          m = fmaf(e, qs, log2f(nf));
-          l = 1.f;
+          const float e = fmaf(e0 + e1, qs, log2f(nf));
+          m = ceilf(e);
+          l = fast_exp2(e - m);  // (a NaN passes on)
           started = true;
+          const float by = a.order == 1 ? l * scale : 0.f;
           if (a.order == 1) {
             (void)pwait(&sh.s_full[g], ns & 1, sh, a);
             ++ns;
@@ -600,23 +721,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             uint32_t f[32];
-            if (a.order == 1) {
-              tmem_ld32_async(tS + c, f);
-              tmem_wait_ld();
-              keep16(f);
-              keep16(f + 16);
-            }
-            const float by = a.order == 1 ? scale : 0.f;
-            if (a.order != 1)
-#pragma unroll
-              for (int i = 0; i < 32; ++i) f[i] = 0;
+            tmem_ld32_async(tS + c, f);  // (order 0: not used)
+            tmem_wait_ld();
+            keep16(f);
+            keep16(f + 16);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float4 v4 = __ldg(mv + c / 4 + i);
-              f[4 * i] = __float_as_uint(fmaf(__uint_as_float(f[4 * i]), by, v4.x));
-              f[4 * i + 1] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 1]), by, v4.y));
-              f[4 * i + 2] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 2]), by, v4.z));
-              f[4 * i + 3] = __float_as_uint(fmaf(__uint_as_float(f[4 * i + 3]), by, v4.w));
+              const float4 v4 = *reinterpret_cast<const float4*>(&sh.mu[1][c + 4 * i]);
+              const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                f[4 * i + k] = __float_as_uint(
+                    by != 0.f ? fmaf(__uint_as_float(f[4 * i + k]), by, v[k] * l) : v[k] * l);
             }
             tmem_st16(tO + c, f);
             tmem_st16(tO + c + 16, f + 16);
@@ -639,16 +755,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = k0 + (BLOCKS == 2 ? 0 : g); j < k1; j += BLOCKS == 2 ? 1 : 2) {
         const int valid = s.valid(j);
         const bool tree = j >= s.it.cache;
-        uint32_t words[4];
-        if (tree) {  // the bits of this row and tile
-          const int w0 = (j - s.it.cache) * 4;
+        uint32_t words[4];  // the keys of this tile that the row sees
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            words[i] = 0;
-            if (live && w0 + i < p.words) words[i] = a.mask[((size_t)b * a.N + node) * p.words + w0 + i];
-            const int n = valid - i * 32;
-            words[i] &= n >= 32 ? kAll : n <= 0 ? 0u : (1u << n) - 1u;
-          }
+        for (int i = 0; i < 4; ++i) {
+          const int n = valid - i * 32;
+          words[i] = n >= 32 ? kAll : n <= 0 ? 0u : (1u << n) - 1u;
+        }
+        if (tree) {
+          const int w0 = (j - s.it.cache) * 4;
+          const uint32_t* row = a.mask + ((size_t)b * a.N + node) * p.words + w0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) words[i] &= live && w0 + i < p.words ? row[i] : 0u;
         }
         if (tree || valid % 16 != 0) {
           // V rows past the keys in use must be finite (their weights are 0),
@@ -688,56 +805,64 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++ns;
         tc_fence_after();
         if (warp_live) {
-          uint32_t x[kTile];
+          // 32 columns at a time; a reference that has to move (by a whole
+          // number: the factor is exact) takes O, l and the weights already
+          // written of this tile along.  (P's columns lie below those of S that
+          // are still to be read.)
+          const uint64_t qs2 = pair(qs, qs);
+          uint64_t sum2[2] = {0, 0};
+          auto columns = [&](uint32_t (&x)[32], int c) {
+            const uint32_t word = c == 0 ? words[0] : c == 1 ? words[1] : c == 2 ? words[2] : words[3];
+            if (word != kAll) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + c * 32, x + c * 32);
-          tmem_wait_ld();
-#pragma unroll
-          for (int c = 0; c < 8; ++c) keep16(x + c * 16);
-          if (tree || valid < kTile) {
-#pragma unroll
-            for (int i = 0; i < kTile; ++i) {
-              const bool on = tree ? (words[i >> 5] >> (i & 31)) & 1u : i < valid;
-              if (!on) x[i] = 0xff800000u;  // -inf
+              for (int i = 0; i < 32; ++i)
+                if (!((word >> i) & 1u)) x[i] = 0xff800000u;  // -inf
             }
-          }
-          float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+            float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
 #pragma unroll
-          for (int i = 0; i < kTile; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qs;
-          if (__any_sync(kAll, top > m + kSlack)) {
-            const float mn = fmaxf(m, top);
-            const float f = mn == kNegInf ? 1.f : fast_exp2(m - mn);
-            m = mn;
-            if (started) {  // (S of this tile is complete, so every earlier product into O is)
+            for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qs;
+            if (__any_sync(kAll, top > m + kSlack)) {
+              const float mn = fmaxf(m, ceilf(top));
+              const float f = m == kNegInf ? 1.f : pow2(m - mn);
+              m = mn;
+              float lo, hi;
+              unpair(sum2[0], lo, hi);
+              sum2[0] = pair(lo * f, hi * f);
+              unpair(sum2[1], lo, hi);
+              sum2[1] = pair(lo * f, hi * f);
               l *= f;
-#pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tmem_ld32_async(tO + c, o);
-                tmem_wait_ld();
-                keep16(o);
-                keep16(o + 16);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                tmem_st16(tO + c, o);
-                tmem_st16(tO + c + 16, o + 16);
-              }
+              if (started) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
+              scale_weights(tS, c, f);
             }
-          }
-          const float ref = m == kNegInf ? 0.f : m;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const float ref = m == kNegInf ? 0.f : m;
+            const uint64_t nref = pair(-ref, -ref);
 #pragma unroll
-          for (int i = 0; i < kTile; i += 2) {
-            const float p0 = fast_exp2(fmaf(__uint_as_float(x[i]), qs, -ref));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(x[i + 1]), qs, -ref));
-            sum[i & 3] += p0;
-            sum[(i & 3) + 1] += p1;
-            x[i >> 1] = pack_bf16x2(p0, p1);
+            for (int i = 0; i < 32; i += 2) {
+              float t0, t1;
+              unpair(fma2(pair(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), qs2, nref), t0, t1);
+              const float p0 = fast_exp2(t0), p1 = fast_exp2(t1);
+              sum2[(i >> 1) & 1] = add2(sum2[(i >> 1) & 1], pair(p0, p1));
+              x[i >> 1] = pack_bf16x2(p0, p1);
+            }
+            tmem_st16(tS + c * 16, x);
+          };
+#pragma unroll 1
+          for (int c = 0; c * 32 < valid; c += 2) {
+            uint32_t xa[32], xb[32];
+            tmem_ld32_async(tS + c * 32, xa);
+            tmem_ld32_async(tS + c * 32 + 32, xb);
+            tmem_wait_ld();
+            keep16(xa);
+            keep16(xa + 16);
+            keep16(xb);
+            keep16(xb + 16);
+            columns(xa, c);
+            columns(xb, c + 1);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_st16(tS + c * 16, x + c * 16);
+          float lo, hi;
+          unpair(add2(sum2[0], sum2[1]), lo, hi);
+          l += lo + hi;
           tmem_wait_st();
         }
         started = true;
@@ -753,11 +878,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
       }
       grid_dependency_wait();  // (a no-op unless the loads went early)
-      const bool whole = s.whole();
+      const bool whole = s.begin == 0 && s.end == s.tiles;
       const int part = 2 * blockIdx.x + (seg == 0 ? 0 : 1);
       constexpr int R = BLOCKS * kTile;
       uint32_t seen_odd[8];
       bool any_odd = false;
+      if (BLOCKS == 1 && mom && k0 == k1) named_sync(1, 256);  // (group 0 has read mu, in ml's place)
       if (BLOCKS == 1 && g == 1) sh.ml[r] = make_float2(m, started ? l : 0.f);
       named_sync(1, 256);  // the other group's state; the nodes' odd values are known
       if (live && k1 > s.it.cache) {
@@ -855,13 +981,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_before();
       named_sync(1, 256);  // both groups are done with O and the exchange
     }
-    if (p.list && tid == 0)  // a boundary inside an item: what tree_merge_kernel joins
-      parts.desc[blockIdx.x] = sh.left > 0 ? make_int4(static_cast<int>(sh.start), static_cast<int>(sh.run), sh.unit, sh.mb)
-                                           : make_int4(-1, 0, 0, 0);
+    if (p.list && tid == 0) parts.desc[blockIdx.x] = sh.cut;  // what tree_merge_kernel joins
   }
 
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kWarpMma) {
     if (lane == 0) {
       if (sh.abort) {  // wait, with the full limit, for the copies in flight
         for (int i = 0; i < NS; ++i) {
@@ -934,7 +1058,7 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   const long units = (long)g.batch * g.n_kv_heads, items = units * p.mb;
   const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
   p.min_run = 2;
-  p.list = units <= kScanUnits && tiles > 4 ? 1 : 0;
+  p.list = units <= kScanUnits && tiles > 4 && items * tiles < (1L << 30) ? 1 : 0;
   p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (items * tiles + p.min_run - 1) / p.min_run))
                   : static_cast<int>(items);
   return p;
