@@ -7,30 +7,33 @@
 // the keys 128 at a time: S = Q K^T, P = 2^(S scale log2 e - m), l += sum P,
 // O += P V.  The retained rows are tiles without a mask, the nodes are tiles
 // whose bits the mask words give.  The moment term is one more key of every
-// row, with logit e = log n + scale q.mu_k and value mu_v + scale C' q: it
-// starts the block (m = e, l = 1, O = its value), the product Q C'^T running on
-// the tensor cores with C' as bf16 hi + lo parts.  m only has to be common to a
-// row's keys, so it moves (with a rescaling of O and l) only when a score
-// exceeds it by more than 8 in log2 units.  P enters the second product
-// rounded to bf16 (2^-8 relative, the output's own rounding); l is summed from
-// the unrounded weights.
+// row, with logit e = log n + scale q.mu_k and value mu_v + scale C' q: its
+// weight starts m and l, and its value joins at the end, the product Q C'^T
+// running on the tensor cores with C' as bf16 hi + lo parts.  m only has to be
+// common to a row's keys, so it moves (by a whole number, with a rescaling of
+// O and l) only when a score exceeds it by more than 8 in log2 units.  P enters
+// the second product rounded to bf16 (2^-8 relative, the output's own
+// rounding); l is summed from the unrounded weights.
 //
 // Work.  The tiles of all (unit, row block) items form one list that is cut
 // into equal runs, one per CTA, wherever the run ends; an item cut by a
 // boundary leaves (m, l, O) of its parts in the workspace, and
 // tree_merge_kernel joins them.  Lengths of any raggedness so cost what their
-// tiles cost.  A CTA holds one or two row blocks: with two (more than 128
-// rows) every K and V tile is read once for 256 rows, with one the two
-// softmax groups take the tiles alternately and merge at the end.
+// tiles cost.  A CTA holds one or two row blocks: with two every K and V tile
+// is read once for 256 rows, with one the two softmax groups take the tiles
+// alternately and merge at the end.
 //
-// One CTA, ten warps: warps 0-3 and 4-7 are the softmax groups, a thread a row;
-// warp 8 issues TMA copies (Q, and K and V tiles into a ring), warp 9 the MMAs:
-// S of both groups first, then in turn a group's product with V and its next
-// S, so that one group's softmax runs beside the other's products.  Code that
-// runs once per item is kept in loops: unrolled, it waited for its own
-// instructions (a masked tile took 9000 cycles instead of 2000).
-// Tensor memory: S (then P over it) of the two groups, 128 columns each, and O
-// of the two, D columns each.
+// One CTA, four warpgroups: warps 0-3 and 4-7 are the softmax groups, a thread
+// a row; warp 8 issues TMA copies (Q, and K and V tiles into a ring), warps 9
+// and 10 the MMAs of a group each: S of its first tile, then in turn its product
+// with V and its next S, so that one group's softmax runs beside the other's
+// products (one thread for both groups: its own instructions, some 10 cycles
+// each, left the tensor cores idle between the batches); warps 12-15 turn C'
+// into operands, in the ring's next free slots, while the last tiles are
+// worked on.  Code that runs once per item is kept in loops: unrolled, it
+// waited for its own instructions (a masked tile took 9000 cycles instead of
+// 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
+// 128 columns each, and O of the two, D columns each.
 #include <algorithm>
 #include <mutex>
 
@@ -46,8 +49,8 @@ namespace {
 
 constexpr int kTile = 128;                   // keys per tile, rows per block
 constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
-constexpr int kThreads = 320;                // 2 softmax groups, the TMA warp, the MMA warp
-constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr int kWarpTma = 8, kWarpMma = 9, kWarpC = 12;
+constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps and an idle one; four for C'
 constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
 constexpr float kSlack = 8.f;                // log2 headroom of the reference (weights <= 2^8)
 constexpr float kNegInf = -INFINITY;
@@ -65,28 +68,35 @@ struct Plan {
   int32_t grid;
   int32_t min_run;  // tiles per CTA at least
   int32_t words;    // mask words per node
+  uint64_t kv_inv;  // 2^40 / KV heads, rounded up: units (below 2^22) divided by a product, u * n_kv < 2^40
 };
 
 // A part of a split item (m, l, O of `blocks` x 128 rows).
 struct Parts {
-  int4* desc;   // [grid] of the item a CTA's run starts in the middle of: (first part or -1, last CTA, unit, mb)
+  int4* desc;   // [grid] of the item whose first inner boundary is the CTA's start: (1 or -1, last CTA, unit, mb)
   float2* ml;   // [2 grid][blocks 128]
   float4* o;    // [2 grid][D / 4][blocks 128]
 };
 
+struct Raw {  // a unit's sizes as read
+  int len, count, n_e;
+};
+
 struct Shared {
   uint64_t full[kMaxSlots], empty[kMaxSlots];
-  uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], o_full, mma_done;
+  uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], turn[2], o_full, mma_done;
   uint32_t tmem;
   int32_t abort, issued, q_issued;
-  int32_t unit, mb, t0, left;  // the CTA's run of the list: first item, tile in it, tiles
+  int32_t unit, mb, t0, start, end;  // the CTA's run of the list: first item, tile in it, the list's tiles [start, end)
+  Raw raw;                     // of the first unit
+  int32_t scan[kThreads / 32];
   int4 cut;                    // parts.desc of this CTA
   uint32_t odd[2][8];          // nodes with a value that is not finite, of this segment and the next
+  float2 ml[kTile];            // (one row block) group 1's (m, l), then the two groups' factors
   union {
-    float mu[2][kTile];  // mu_k and mu_v, while a segment takes its moment term in
-    float2 ml[kTile];    // (one row block) at its end: group 1's (m, l), then the two groups' factors
+    float mu_k[kTile];  // from a segment's start
+    float w[kTile];     // (one row block) at its end: the moment term's factor
   };
-  int32_t scan[kThreads / 32];
 };
 constexpr int kSharedBytes = 2048;
 static_assert(sizeof(Shared) <= kSharedBytes, "shared variables");
@@ -161,6 +171,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // 2^d of a whole number d <= 0, exactly (0 below the smallest normal number).
 __device__ __forceinline__ float pow2(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
@@ -212,28 +227,28 @@ __device__ __forceinline__ bool odd2(uint32_t w) {
 // What a unit's items consist of.
 struct Item {
   int len, count, n_e;
-  int head, cache, nodes;  // tiles: the moment term (0 or 1), the cache, the nodes
+  int cache, nodes, tail;  // tiles: the cache, the nodes, the moment term (0 or 1)
 };
 
-struct Raw {  // as read, so that a read can be in flight until it is needed
-  int len, count, n_e;
-};
-__device__ __forceinline__ Raw load_raw(const TreeArgs& a, int u) {
-  return Raw{a.len[u], a.count != nullptr ? a.count[u / a.n_kv] : a.N, a.n != nullptr ? a.n[u] : 0};
+__device__ __forceinline__ int batch_of(const Plan& p, int u) {
+  return static_cast<int>((static_cast<uint64_t>(u) * p.kv_inv) >> 40);
+}
+__device__ __forceinline__ Raw load_raw(const TreeArgs& a, const Plan& p, int u) {
+  return Raw{a.len[u], a.count != nullptr ? a.count[batch_of(p, u)] : a.N, a.n != nullptr ? a.n[u] : 0};
 }
 __device__ __forceinline__ Item make_item(const TreeArgs& a, const Raw& r) {
   Item it;
   it.len = min(max(r.len, 0), a.cap);
   it.count = min(max(r.count, 0), a.N);
   it.n_e = r.n_e;
-  it.head = a.n != nullptr ? 1 : 0;
+  it.tail = a.n != nullptr ? 1 : 0;
   it.cache = (it.len + kTile - 1) / kTile;
   it.nodes = (it.count + kTile - 1) / kTile;
   return it;
 }
 // Tiles of an item whose rows start at node `first` (at least one: its outputs have to be written).
 __device__ __forceinline__ int item_tiles(const Item& it, int first) {
-  return first < it.count ? max(1, it.head + it.cache + it.nodes) : 1;
+  return first < it.count ? max(1, it.cache + it.nodes + it.tail) : 1;
 }
 
 // A CTA's next segment: tiles [begin, end) of item (unit, mb).
@@ -242,7 +257,7 @@ struct Segment {
   int begin, end, tiles;
   int k0, k1;  // key tiles: the cache's, then the nodes'
   Item it;
-  bool live, mom;
+  bool live, mom;  // rows in use; the moment term belongs to this segment
   // keys in use of key tile j
   __device__ __forceinline__ int valid(int j) const {
     return min(kTile, (j < it.cache ? it.len : it.count + it.cache * kTile) - j * kTile);
@@ -251,7 +266,7 @@ struct Segment {
 
 struct Walk {
   int unit, mb, t, left;
-  Raw raw;
+  Raw raw;  // (read while the segment before is worked on)
   __device__ __forceinline__ bool next(const TreeArgs& a, const Plan& p, Segment& s) {
     if (left <= 0) return false;
     s.unit = unit;
@@ -262,65 +277,70 @@ struct Walk {
     s.tiles = item_tiles(s.it, s.first);
     s.begin = t;
     s.end = min(s.tiles, t + left);
-    s.mom = s.live && t == 0 && s.it.head > 0 && s.it.n_e > 0;
-    s.k0 = s.live ? max(s.begin - s.it.head, 0) : 0;
-    s.k1 = s.live ? max(s.end - s.it.head, 0) : 0;
+    const int keys = s.live ? s.it.cache + s.it.nodes : 0;
+    s.mom = s.live && s.end == s.tiles && s.it.tail > 0 && s.it.n_e > 0;
+    s.k0 = min(s.begin, keys);
+    s.k1 = min(s.end, keys);
     left -= s.end - s.begin;
     t = 0;
     if (++mb == p.mb) {
       mb = 0;
       ++unit;
     }
-    if (left > 0) raw = load_raw(a, unit);
+    if (left > 0) raw = load_raw(a, p, unit);
     return true;
   }
 };
 
 // Pipeline wait that gives up after `polls` polls: records the timeout once and
-// raises the CTA's abort flag; every later wait then passes at once.
-__device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, Shared& sh, const TreeArgs& a) {
-  if (mbar_try_wait(bar, parity)) return true;
-  volatile int32_t* abort = &sh.abort;
-  if (*abort) return false;
-  if (mbar_wait(bar, parity, a.polls)) return true;
-  *abort = 1;
-  record_error(a.ws, MKV_ERR_TIMEOUT, static_cast<int32_t>(blockIdx.x));
+// raises the CTA's abort flag; every later wait that has to poll then passes.
+__device__ __noinline__ void record_bad(void* ws, uint32_t code, int32_t info) { record_error(ws, code, info); }
+__device__ __noinline__ bool pwait_slow(uint64_t* bar, uint32_t parity, int32_t* abort, void* ws, uint32_t polls) {
+  volatile int32_t* flag = abort;
+  if (*flag) return false;
+  if (mbar_wait(bar, parity, polls)) return true;
+  *flag = 1;
+  record_error(ws, MKV_ERR_TIMEOUT, static_cast<int32_t>(blockIdx.x));
   return false;
 }
+__device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, Shared& sh, const TreeArgs& a) {
+  return (a.polls > 0 && mbar_try_wait(bar, parity)) || pwait_slow(bar, parity, &sh.abort, a.ws, a.polls);
+}
 
-// Where this CTA's run starts in the list of all items' tiles, and what it is
-// of an item that an earlier CTA began.
-__device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Shared& sh) {
+// Where this CTA's run starts in the list of all items' tiles, and whether its
+// start cuts an item
+// (`mine`: the sizes of unit threadIdx.x, read ahead).
+__device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Shared& sh, const Raw& mine) {
   const int tid = threadIdx.x, units = a.batch * a.n_kv;
   const int nodes = (p.blocks * kTile) >> p.g_shift;  // of an item
   auto record = [&](int u, const Raw& r) {
-    if (r.len < 0 || r.len > a.cap) record_error(a.ws, MKV_ERR_CAPACITY, u);
-    if (r.count < 0 || r.count > a.N) record_error(a.ws, MKV_ERR_INVALID_ARG, u);
+    if (static_cast<uint32_t>(r.len) > static_cast<uint32_t>(a.cap)) record_bad(a.ws, MKV_ERR_CAPACITY, u);
+    if (static_cast<uint32_t>(r.count) > static_cast<uint32_t>(a.N)) record_bad(a.ws, MKV_ERR_INVALID_ARG, u);
   };
   if (!p.list) {
     if (tid == 0) {
       sh.unit = blockIdx.x / p.mb;
       sh.mb = blockIdx.x % p.mb;
       sh.t0 = 0;
-      const Raw r = load_raw(a, sh.unit);
-      sh.left = item_tiles(make_item(a, r), sh.mb * nodes);
-      if (sh.mb == 0) record(sh.unit, r);
+      sh.raw = load_raw(a, p, sh.unit);
+      sh.start = 0;
+      sh.end = item_tiles(make_item(a, sh.raw), sh.mb * nodes);
+      if (sh.mb == 0) record(sh.unit, sh.raw);
     }
     __syncthreads();
     return;
   }
-  // (alive items, tiles of one) of a unit; the others weigh one tile each
+  // a unit's items with rows in use (the others weigh one tile each), and the tiles of one
   auto weigh = [&](const Raw& r, int& tiles) {
     const Item it = make_item(a, r);
-    const int alive = (it.count + nodes - 1) / nodes;
     tiles = item_tiles(it, 0);
-    return alive;
+    return (it.count + nodes - 1) / nodes;
   };
   const int chunk = (units + kThreads - 1) / kThreads, u0 = min(units, tid * chunk), u1 = min(units, u0 + chunk);
   int sum = 0;
 #pragma unroll 1
   for (int u = u0; u < u1; ++u) {
-    const Raw r = load_raw(a, u);
+    const Raw r = chunk == 1 ? mine : load_raw(a, p, u);
     int tiles;
     const int alive = weigh(r, tiles);
     sum += alive * tiles + (p.mb - alive);
@@ -334,7 +354,7 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
   }
   if ((tid & 31) == 31) sh.scan[tid >> 5] = incl;
   if (tid == 0) {
-    sh.left = 0;
+    sh.start = sh.end = 0;
     sh.cut = make_int4(-1, 0, 0, 0);
   }
   __syncthreads();
@@ -346,28 +366,51 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
     total += x;
   }
   const int run = max(p.min_run, (total + p.grid - 1) / p.grid);
-  const int start = run * blockIdx.x;
-  int at = before + incl - sum;  // of this thread's first unit
-  if (start >= at && start < at + sum) {
-    int u = u0, tiles, alive, w;
+  const int at = before + incl - sum;  // of this thread's first unit
+  // The run is [start, end) with both ends moved off an item's first and last
+  // tile, to the item's edge: no CTA is left with the moment term alone or with
+  // one tile to begin with.
+#pragma unroll 1
+  for (int edge = 0; edge < 2; ++edge) {
+    const int pos = run * (blockIdx.x + edge);
+    if (tid == 0 && pos >= total) (edge == 0 ? sh.start : sh.end) = total;
+    if (pos < at || pos >= at + sum) continue;
+    int u = u0, tiles, alive, w, base = at;
+    Raw r;
+#pragma unroll 1
     for (;; ++u) {
-      alive = weigh(load_raw(a, u), tiles);
+      r = chunk == 1 ? mine : load_raw(a, p, u);
+      alive = weigh(r, tiles);
       w = alive * tiles + (p.mb - alive);
-      if (start < at + w) break;
-      at += w;
+      if (pos < base + w) break;
+      base += w;
     }
-    int in = start - at, mb = 0;  // the unit's tiles before the run
+    int in = pos - base, mb = 0;  // the unit's tiles before `pos`
     while (mb < alive && in >= tiles) in -= tiles, ++mb;
     if (mb == alive) mb += in, in = 0;
+    const int item = pos - in;  // where the item starts
+    int snap = pos;
+    if (in > 0) {
+      if (tiles - in <= 1) snap = item + tiles;
+      else if (in <= 1) snap = item;
+    }
+    if (edge == 1) {
+      sh.end = snap;
+      continue;
+    }
+    if (snap == item + tiles && in > 0) {  // the next item
+      if (++mb == p.mb) {
+        mb = 0;
+        if (++u < units) r = load_raw(a, p, u);
+      }
+    }
     sh.unit = u;
     sh.mb = mb;
-    sh.t0 = in;
-    sh.left = min(run, total - start);
-    // the first boundary inside an item sees to its merge: its first part is
-    // the previous CTA's last segment (its only one if the item starts with
-    // the run)
-    if (in > 0 && in <= run)
-      sh.cut = make_int4(2 * (static_cast<int>(blockIdx.x) - 1) + (in == run ? 0 : 1), (start - in + tiles - 1) / run, u, mb);
+    sh.t0 = in > 0 && snap == pos ? in : 0;
+    sh.raw = r;
+    sh.start = snap;
+    // the first boundary inside an item sees to its merge
+    if (sh.t0 > 0 && in - run <= 1) sh.cut = make_int4(1, (item + tiles - 2) / run, u, mb);
   }
   __syncthreads();
 }
@@ -387,35 +430,36 @@ __global__ void __launch_bounds__(kThreads, 1)
   Shared& sh = *reinterpret_cast<Shared*>(ring + NS * kSlot);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid == 0) {
-    for (int i = 0; i < NS; ++i) {
-      mbar_init(&sh.full[i], 1);
-      mbar_init(&sh.empty[i], 1);
-    }
+  if (!a.early) grid_dependency_wait();
+  Raw mine{};  // in flight while the barriers are set up
+  if (tid < a.batch * a.n_kv) mine = load_raw(a, p, tid);
+  if (tid < NS) {
+    mbar_init(&sh.full[tid], 1);
+    mbar_init(&sh.empty[tid], BLOCKS);  // the groups that read a slot
+  } else if (tid >= 32 && tid < 34) {
+    mbar_init(&sh.s_full[tid - 32], 1);
+    mbar_init(&sh.p_ready[tid - 32], 4);
+    mbar_init(&sh.turn[tid - 32], 4);
+  } else if (tid == 64) {
     mbar_init(&sh.q_full, 1);
-    mbar_init(&sh.q_empty, 1 + 8);
+    mbar_init(&sh.q_empty, 2 + 8);
     mbar_init(&sh.c_grant, 1);
-    mbar_init(&sh.c_full, 8);
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(&sh.s_full[s], 1);
-      mbar_init(&sh.p_ready[s], 4);
-    }
-    mbar_init(&sh.o_full, 1);
-    mbar_init(&sh.mma_done, 1);
+    mbar_init(&sh.c_full, 4);
+    mbar_init(&sh.o_full, 2);
+    mbar_init(&sh.mma_done, 2);
     sh.abort = 0;
     sh.issued = 0;
     sh.q_issued = 0;
-    mbar_fence_init();
+  } else if (tid >= 96 && tid < 112) {
+    (&sh.odd[0][0])[tid - 96] = 0;
   }
-  if (tid < 16) (&sh.odd[0][0])[tid] = 0;
+  mbar_fence_init();
   if (warp == kWarpMma) tmem_alloc(&sh.tmem, 512);
   tc_fence_before();
-  if (!a.early) grid_dependency_wait();
-  find_run(a, p, sh);  // (ends with a barrier)
+  find_run(a, p, sh, mine);  // (ends with a barrier)
   tc_fence_after();
   const uint32_t tm = sh.tmem;
-  Walk walk{sh.unit, sh.mb, sh.t0, sh.left, {}};
-  if (walk.left > 0) walk.raw = load_raw(a, walk.unit);
+  Walk walk{sh.unit, sh.mb, sh.t0, sh.end - sh.start, sh.raw};
   Segment s;
 
   if (warp == kWarpTma) {
@@ -424,10 +468,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true, waited = !a.early;
       const uint64_t pol = l2_evict_first();
       auto wait_prior = [&] {
-        if (!waited) {
-          grid_dependency_wait();
-          waited = true;
-        }
+        if (!waited) grid_dependency_wait();
+        waited = true;
         grid_launch_dependents();
       };
       auto slot = [&]() -> int {  // the next slot of the ring, free
@@ -436,28 +478,54 @@ __global__ void __launch_bounds__(kThreads, 1)
         return i;
       };
       while (ok && walk.next(a, p, s)) {
-        const bool mom = s.mom;
-        if (!mom && s.k1 == s.k0) continue;
-        const int b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
-        auto load_q = [&] {
-          wait_prior();
-          if (nq > 0 && !pwait(&sh.q_empty, (nq - 1) & 1, sh, a)) {
-            ok = false;
-            return;
-          }
-          mbar_arrive_expect_tx(&sh.q_full, BLOCKS * kSlot);
-          for (int r = 0; r < BLOCKS; ++r)
-            for (int x = 0; x < BX; ++x)
-              tma_load_4d(sQ + r * kSlot + x * kBox, &tmQ, x * 64, kv << p.g_shift, s.first + r * (kTile >> p.g_shift), b,
-                          &sh.q_full);
-          sh.q_issued = ++nq;
-        };
-        bool q_due = true;
-        if (waited) {
-          load_q();
-          q_due = false;
+        if (!s.mom && s.k1 == s.k0) continue;
+        const int b = batch_of(p, s.unit), kv = s.unit - b * a.n_kv;
+        if (s.mom && a.order == 1) {  // C' is read when slots are free: into L2 now
+          const size_t at = (size_t)s.unit * D * D;
+          const void* c = a.C16 != nullptr ? static_cast<const void*>(a.C16 + at)
+                          : a.Cs != nullptr ? static_cast<const void*>(a.Cs + at / 2)
+                                            : static_cast<const void*>(a.C + at);
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(c), "r"(D * D * (a.C16 != nullptr ? 2 : 4))
+                       : "memory");
         }
-        if (ok && mom && a.order == 1) {  // the softmax threads write C' into the next slots
+        bool q_due = true;
+        for (int j = s.k0; ok && j <= s.k1; ++j) {
+          const bool cache = j < s.it.cache;
+          // Q as soon as it may be replaced, but after the first tile at the
+          // latest; before what precedes this launch is done, only the cache's
+          // tiles, as many as the ring holds
+          if (q_due && (!waited ? (!cache || j == s.k1 || seq + 2 > NS)
+                                : (j != s.k0 || j == s.k1 || nq == 0 || mbar_try_wait(&sh.q_empty, (nq - 1) & 1)))) {
+            wait_prior();
+            if (nq > 0 && !pwait(&sh.q_empty, (nq - 1) & 1, sh, a)) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&sh.q_full, BLOCKS * kSlot);
+            for (int r = 0; r < BLOCKS; ++r)
+              for (int x = 0; x < BX; ++x)
+                tma_load_4d(sQ + r * kSlot + x * kBox, &tmQ, x * 64, kv << p.g_shift, s.first + r * (kTile >> p.g_shift), b,
+                            &sh.q_full);
+            sh.q_issued = ++nq;
+            q_due = false;
+          }
+          if (j == s.k1) break;
+#pragma unroll 1
+          for (int v = 0; ok && v < 2; ++v) {
+            const int i = slot();
+            if (!ok) break;
+            mbar_arrive_expect_tx(&sh.full[i], kSlot);
+            for (int x = 0; x < BX; ++x) {
+              uint8_t* dst = ring + i * kSlot + x * kBox;
+              if (cache)
+                tma_load_3d_hint(dst, v ? &tmV : &tmK, x * 64, j * kTile, s.unit, &sh.full[i], pol);
+              else
+                tma_load_4d(dst, v ? &tmVt : &tmKt, x * 64, kv, (j - s.it.cache) * kTile, b, &sh.full[i]);
+            }
+            sh.issued = ++seq;
+          }
+        }
+        if (s.mom && a.order == 1) {  // C' goes into the next slots
           const int n = a.C16 != nullptr ? 1 : 2;
           for (int j = 0; ok && j < n; ++j) {
             const int i = slot();
@@ -467,121 +535,69 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (ok) mbar_arrive(&sh.c_grant);
         }
-        for (int j = s.k0; ok && j < s.k1; ++j) {
-          const bool cache = j < s.it.cache;
-          if (q_due && (!cache || seq + 2 > NS)) {  // what follows waits for others, or reads their output
-            load_q();
-            q_due = false;
-          }
-          for (int kvx = 0; ok && kvx < 2; ++kvx) {
-            const int i = slot();
-            if (!ok) break;
-            mbar_arrive_expect_tx(&sh.full[i], kSlot);
-            for (int x = 0; x < BX; ++x) {
-              uint8_t* dst = ring + i * kSlot + x * kBox;
-              if (cache)
-                tma_load_3d_hint(dst, kvx ? &tmV : &tmK, x * 64, j * kTile, s.unit, &sh.full[i], pol);
-              else
-                tma_load_4d(dst, kvx ? &tmVt : &tmKt, x * 64, kv, (j - s.it.cache) * kTile, b, &sh.full[i]);
-            }
-            sh.issued = ++seq;
-          }
-        }
-        if (ok && q_due) load_q();
       }
       wait_prior();
     }
-  } else if (warp == kWarpMma) {
-    if (lane == 0) {  // ---- MMA
-      const uint64_t dQ = sdesc_sw128(smem_addr(sQ), 16, 1024), dR = sdesc_sw128(smem_addr(ring), 16, 1024);
-      const uint64_t dV = sdesc_sw128(smem_addr(ring), kBox, 1024);
+  } else if (warp == kWarpMma || warp == kWarpMma + 1) {
+    if (lane == 0) {  // ---- MMA, a thread per group
+      const int g = warp - kWarpMma;
+      const bool reads_c = BLOCKS == 2 || g == 0;  // the moment term counts in this group's state
+      const uint64_t dQ = sdesc_sw128(smem_addr(sQ) + (BLOCKS == 2 ? g * kSlot : 0), 16, 1024);
+      const uint64_t dR = sdesc_sw128(smem_addr(ring), 16, 1024), dV = sdesc_sw128(smem_addr(ring), kBox, 1024);
+      const uint32_t tP = tm + cS + g * 128, tO = tm + cO + g * D;
       constexpr uint32_t idS = idesc_bf16(128, kTile, 0, 0), idP = idesc_bf16(128, D, 0, 1);
-      int seq = 0;  // ring slots of the segments before
-      uint32_t qph = 0, cph = 0, pph = 0;  // phases; p_ready's in bit g
-      bool ok = true;
-      // S of group g = Q K^T of the tile in slot i (n16 keys)
-      auto issue_s = [&](int g, int i, int n16) {
-        const uint64_t da = dQ + (BLOCKS == 2 ? g * (kSlot >> 4) : 0), db = dR + i * (kSlot >> 4);
-        const uint32_t id = idS - ((uint32_t)(kTile - n16) >> 3 << 17), t = tm + cS + g * 128;
+      constexpr int kStep = BLOCKS == 2 ? 2 : 4;  // ring slots from one K tile of this group to the next
+      int seq = 0;                                // ring slots of the segments before
+      uint32_t qph = 0, cph = 0, pph = 0;
+      bool ok = true, f_read = false;
+      // S = Q K^T of the tile in slot i (n16 keys)
+      auto issue_s = [&](int i, int n16) {
+        const uint64_t db = dR + i * (kSlot >> 4);
+        const uint32_t id = idS - ((uint32_t)(kTile - n16) >> 3 << 17);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          umma_bf16(t, da + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, db + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, id,
+          umma_bf16(tP, dQ + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, db + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, id,
                     kk > 0 ? 1u : 0u);
         umma_commit(&sh.s_full[g]);
-        if (BLOCKS == 1 || g == 1) umma_commit(&sh.empty[i]);
+        umma_commit(&sh.empty[i]);
       };
       while (ok && walk.next(a, p, s)) {
         const int k0 = s.k0, k1 = s.k1;
         if (!s.mom && k0 == k1) continue;
         ok = pwait(&sh.q_full, qph, sh, a);
         qph ^= 1;
-        int i = seq % NS;
-        uint32_t ph = (seq / NS) & 1;
-        auto advance = [&] {
-          if (++i == NS) i = 0, ph ^= 1;
-        };
-        const bool f_tiles = s.mom && a.order == 1;
-        if (f_tiles) {  // the moment term's value, Q C'^T, in the place of S
-          const int n = a.C16 != nullptr ? 1 : 2;
-          ok = ok && pwait(&sh.c_full, cph, sh, a);
-          cph ^= 1;
-          if (!ok) break;
-          tc_fence_after();
-          constexpr uint32_t id = idesc_bf16(128, D, 0, 0);
-          for (int j = 0; j < n; ++j) {
-            const uint64_t db = dR + i * (kSlot >> 4);
-            for (int g = 0; g < BLOCKS; ++g)
-#pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk)
-                umma_bf16(tm + cS + g * 128, dQ + g * (kSlot >> 4) + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2,
-                          db + (kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2, id, (j > 0 || kk > 0) ? 1u : 0u);
-            umma_commit(&sh.empty[i]);
-            advance();
-          }
-          for (int g = 0; g < BLOCKS; ++g) umma_commit(&sh.s_full[g]);
-          seq += n;
+        if (f_read && reads_c) {  // the last segment's Q C'^T has been read
+          ok = ok && pwait(&sh.p_ready[g], pph, sh, a);
+          pph ^= 1;
         }
-        // steps w = (tile, group w & 1): S of steps 0 and 1, then for every
-        // step its product with V and S of the group's next step
-        const int W = (k1 - k0) * BLOCKS;
-        int si = i;  // slot and phase of the next S step's K tile; (i, ph) of the next product's
-        uint32_t sph = ph;
-        int sw = 0;
-        auto next_s = [&] {
-          const int g = sw & 1, t = k0 + (BLOCKS == 2 ? sw >> 1 : sw);
-          ok = pwait(&sh.full[si], sph, sh, a);
-          if (!ok) return;
+        f_read = false;
+        int t = k0 + (BLOCKS == 2 ? 0 : g);
+        int i = seq + 2 * (t - k0);  // slot and phase of the K tile; V is in the next slot
+        uint32_t ph = (i / NS) & 1;
+        i %= NS;
+        uint32_t add = 0;
+        int n16 = (s.valid(t) + 15) & ~15;
+        if (ok && t < k1) {
+          ok = pwait(&sh.full[i], ph, sh, a);
           tc_fence_after();
-          issue_s(g, si, (s.valid(t) + 15) & ~15);
-          ++sw;
-          if (BLOCKS == 1 || g == 1) {
-            si += 2;
-            if (si >= NS) si -= NS, sph ^= 1;
-          }
-        };
-#pragma unroll 1
-        for (int g = 0; ok && g < 2; ++g) {
-          if (f_tiles && g < BLOCKS) {  // F has been read
-            ok = pwait(&sh.p_ready[g], (pph >> g) & 1, sh, a);
-            pph ^= 1u << g;
-          }
-          if (ok && g < W) next_s();
+          if (ok) issue_s(i, n16);
         }
 #pragma unroll 1
-        for (int w = 0; ok && w < W; ++w) {
-          const int g = w & 1, t = k0 + (BLOCKS == 2 ? w >> 1 : w);
-          int vi = i + 1;
-          uint32_t vph = ph;
-          if (vi == NS) vi = 0, vph ^= 1;
-          ok = pwait(&sh.full[vi], vph, sh, a) && pwait(&sh.p_ready[g], (pph >> g) & 1, sh, a);
-          pph ^= 1u << g;
-          if (!ok) break;
-          tc_fence_after();
+        while (ok && t < k1) {
+          const int steps = n16 >> 4;
+          int vi = i + 1, ni = i + kStep;
+          uint32_t vph = ph, nph = ph;
+          if (vi >= NS) vi -= NS, vph ^= 1;
+          if (ni >= NS) ni -= NS, nph ^= 1;
+          t += kStep / 2;
+          n16 = t < k1 ? (s.valid(t) + 15) & ~15 : 0;
           const uint64_t db = dV + vi * (kSlot >> 4);
-          const uint32_t tP = tm + cS + g * 128, tO = tm + cO + g * D;
-          const bool fresh = w < 2 && !(s.mom && (BLOCKS == 2 || g == 0));
-          const int steps = (s.valid(t) + 15) >> 4;
-          umma_bf16_ts(tO, tP, db, idP, fresh ? 0u : 1u);
+          ok = pwait(&sh.full[vi], vph, sh, a) && pwait(&sh.p_ready[g], pph, sh, a);
+          pph ^= 1;
+          if (!ok) break;
+          tc_fence_after();
+          umma_bf16_ts(tO, tP, db, idP, add);
+          add = 1;
           if (steps == 8) {
 #pragma unroll
             for (int kk = 1; kk < 8; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
@@ -589,107 +605,133 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
             for (int kk = 1; kk < steps; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
           }
-          if (BLOCKS == 1 || g == 1) {
-            umma_commit(&sh.empty[vi]);
-            advance();
-            advance();
+          umma_commit(&sh.empty[vi]);
+          if (n16 > 0) {
+            ok = pwait(&sh.full[ni], nph, sh, a);
+            if (!ok) break;
+            tc_fence_after();
+            issue_s(ni, n16);
           }
-          if (sw < W) next_s();
+          i = ni, ph = nph;
+        }
+        seq += 2 * (k1 - k0);
+        if (ok && s.mom && a.order == 1) {  // the moment term's value, Q C'^T, in the place of S
+          const int n = a.C16 != nullptr ? 1 : 2;
+          if (reads_c) {
+            ok = pwait(&sh.c_full, cph, sh, a);
+            cph ^= 1;
+            if (!ok) break;
+            tc_fence_after();
+            constexpr uint32_t id = idesc_bf16(128, D, 0, 0);
+#pragma unroll 1
+            for (int j = 0; j < n; ++j) {
+              const int ci = (seq + j) % NS;
+              const uint64_t db = dR + ci * (kSlot >> 4);
+#pragma unroll 1
+              for (int kk = 0; kk < D / 16; ++kk)
+                umma_bf16(tP, dQ + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, db + (kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2,
+                          id, (j > 0 || kk > 0) ? 1u : 0u);
+              umma_commit(&sh.empty[ci]);
+            }
+          }
+          seq += n;
+          f_read = true;
         }
         umma_commit(&sh.q_empty);
         umma_commit(&sh.o_full);
-        seq += 2 * (k1 - k0);
       }
       umma_commit(&sh.mma_done);
     }
-  } else {
+  } else if (warp >= kWarpC) {
+    // ---- C' as the operand of Q C'^T: 16-byte chunks of 8 columns, hi and lo parts
+    constexpr int kBatch = 4, kRounds = D * D / 8 / 128 / kBatch;
+    const int t = tid - kWarpC * 32;
+    uint32_t seq = 0, cph = 0;
+    while (walk.next(a, p, s)) {
+      if (!s.mom && s.k0 == s.k1) continue;
+      seq += 2 * (s.k1 - s.k0);
+      if (!s.mom || a.order != 1) continue;
+      const float nf = static_cast<float>(s.it.n_e);
+      uint8_t* hi = ring + (seq % NS) * kSlot;
+      uint8_t* lo = ring + ((seq + 1) % NS) * kSlot;
+      seq += a.C16 != nullptr ? 1 : 2;
+      const size_t base = (size_t)s.unit * D * D;
+#pragma unroll 1
+      for (int k = 0; k < kRounds; ++k) {
+        uint4 x[kBatch], y[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const size_t at = base + ((k * kBatch + j) * 128 + t) * 8;
+          const uint4* src = a.C16 != nullptr ? reinterpret_cast<const uint4*>(a.C16 + at)
+                             : a.Cs != nullptr ? reinterpret_cast<const uint4*>(a.Cs + at / 2)
+                                               : reinterpret_cast<const uint4*>(a.C + at);
+          x[j] = src[0];
+          y[j] = a.C16 == nullptr ? src[1] : make_uint4(0, 0, 0, 0);
+        }
+        if (k == 0) {
+          (void)pwait(&sh.c_grant, cph, sh, a);
+          cph ^= 1;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const int c = (k * kBatch + j) * 128 + t;
+          const uint32_t off = swz_off(c / (D / 8), (c % (D / 8)) * 8, D);
+          if (a.Cs != nullptr) {
+            *reinterpret_cast<uint4*>(hi + off) = make_uint4(x[j].x, x[j].z, y[j].x, y[j].z);
+            *reinterpret_cast<uint4*>(lo + off) = make_uint4(x[j].y, x[j].w, y[j].y, y[j].w);
+            continue;
+          }
+          uint32_t w[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w}, h[4];
+          if (a.C16 != nullptr) {
+#pragma unroll
+            for (int i = 3; i >= 0; --i) {
+              w[2 * i + 1] = w[i] & 0xffff0000u;
+              w[2 * i] = w[i] << 16;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (fabsf(__uint_as_float(w[i]) * nf) < a.tau) w[i] = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h[i] = pack_bf16x2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+          *reinterpret_cast<uint4*>(hi + off) = make_uint4(h[0], h[1], h[2], h[3]);
+          if (a.C16 == nullptr) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              h[i] = pack_bf16x2(__uint_as_float(w[2 * i]) - __uint_as_float(h[i] << 16),
+                                 __uint_as_float(w[2 * i + 1]) - __uint_as_float(h[i] & 0xffff0000u));
+            *reinterpret_cast<uint4*>(lo + off) = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.c_full);
+    }
+  } else if (warp < kWarpTma) {
     // ---- softmax groups: thread r of group g has row r of a block
     const int g = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's 32 TMEM lanes
     const uint32_t tS = tm + lanes + cS + g * 128, tO = tm + lanes + cO + g * D;
     const float scale = rsqrtf(static_cast<float>(D)), qs = scale * kLog2e;
     const int G = 1 << p.g_shift, HQ = a.n_kv << p.g_shift;
-    uint32_t nq = 0, nc = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots consumed
+    uint32_t nq = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots of the segments before
+    uint32_t tph = 0;
+    if (g == 1 && lane == 0) mbar_arrive(&sh.turn[0]);  // group 0 begins
     int seg = 0;
     while (walk.next(a, p, s)) {
       const bool mom = s.mom;
-      const int k0 = s.k0, k1 = s.k1, b = s.unit / a.n_kv, kv = s.unit % a.n_kv;
+      const int k0 = s.k0, k1 = s.k1, b = batch_of(p, s.unit), kv = s.unit - b * a.n_kv;
       const bool active = mom || k1 > k0;
       const int node = s.first + ((BLOCKS == 2 ? g * kTile + r : r) >> p.g_shift), h = r & (G - 1);
       const bool live = node < s.it.count;
       const bool warp_live = __any_sync(kAll, live);
-      const bool mine = BLOCKS == 2 || g == 0;  // this group's block starts from the moment term
-      float m = kNegInf, l = 0.f;
-      bool started = false;
+      const bool mine = BLOCKS == 2 || g == 0;  // the moment term counts in this group's state
+      float m = kNegInf, l = 0.f, e = kNegInf;
+      bool filled = false;  // O holds something
       if (mom) {
-        const float nf = static_cast<float>(s.it.n_e);
-        if (tid < 2 * D) {
-          const float* src = (tid < D ? a.mu_k : a.mu_v) + (size_t)s.unit * D;
-          sh.mu[tid >= D][tid & (D - 1)] = src[tid & (D - 1)];
-        }
-        if (a.order == 1) {
-          // C' as the operand of Q C'^T: 16-byte chunks of 8 columns, hi and lo parts
-          constexpr int kBatch = D == 128 ? 4 : 2, kRounds = D * D / 8 / 256 / kBatch;
-          uint8_t* hi = ring + (vseq % NS) * kSlot;
-          uint8_t* lo = ring + ((vseq + 1) % NS) * kSlot;
-          vseq += a.C16 != nullptr ? 1 : 2;
-          const size_t base = (size_t)s.unit * D * D;
-#pragma unroll 1
-          for (int k = 0; k < kRounds; ++k) {
-            uint4 x[kBatch], y[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-              const size_t at = base + ((k * kBatch + j) * 256 + tid) * 8;
-              const uint4* src = a.C16 != nullptr ? reinterpret_cast<const uint4*>(a.C16 + at)
-                                 : a.Cs != nullptr ? reinterpret_cast<const uint4*>(a.Cs + at / 2)
-                                                   : reinterpret_cast<const uint4*>(a.C + at);
-              x[j] = src[0];
-              if (a.C16 == nullptr) y[j] = src[1];
-            }
-            if (k == 0) {
-              (void)pwait(&sh.c_grant, nc & 1, sh, a);
-              ++nc;
-            }
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-              const int c = (k * kBatch + j) * 256 + tid;
-              const uint32_t off = swz_off(c / (D / 8), (c % (D / 8)) * 8, D);
-              if (a.Cs != nullptr) {
-                *reinterpret_cast<uint4*>(hi + off) = make_uint4(x[j].x, x[j].z, y[j].x, y[j].z);
-                *reinterpret_cast<uint4*>(lo + off) = make_uint4(x[j].y, x[j].w, y[j].y, y[j].w);
-              } else {
-                float v[8];
-                if (a.C16 != nullptr) {
-                  const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-                    v[2 * i] = f.x, v[2 * i + 1] = f.y;
-                  }
-                } else {
-                  const uint32_t w[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  if (fabsf(v[i] * nf) < a.tau) v[i] = 0.f;
-                *reinterpret_cast<uint4*>(hi + off) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-                if (a.C16 == nullptr) {
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) v[i] = bf16_residual(v[i]);
-                  *reinterpret_cast<uint4*>(lo + off) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-                }
-              }
-            }
-          }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.c_full);
-        }
-        named_sync(1, 256);  // mu_k and mu_v are in place
+        if (tid < D) sh.mu_k[tid] = a.mu_k[(size_t)s.unit * D + tid];
+        named_sync(1, 256);
         (void)pwait(&sh.q_full, nq & 1, sh, a);
         if (mine) {
           float e0 = 0.f, e1 = 0.f;
@@ -698,9 +740,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < D / 8; ++c) {
             const uint4 w = *reinterpret_cast<const uint4*>(row + (c >> 3) * kBox + (((c & 7) ^ (r & 7)) << 4));
             const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-            const float4 k0 = *reinterpret_cast<const float4*>(&sh.mu[0][c * 8]);
-            const float4 k1 = *reinterpret_cast<const float4*>(&sh.mu[0][c * 8 + 4]);
-            const float k[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
+            const float4 ka = *reinterpret_cast<const float4*>(&sh.mu_k[c * 8]);
+            const float4 kb = *reinterpret_cast<const float4*>(&sh.mu_k[c * 8 + 4]);
+            const float k[8] = {ka.x, ka.y, ka.z, ka.w, kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
@@ -708,51 +750,30 @@ __global__ void __launch_bounds__(kThreads, 1)
               e1 = fmaf(f.y, k[2 * i + 1], e1);
             }
           }
-          const float e = fmaf(e0 + e1, qs, log2f(nf));
+          e = fmaf(e0 + e1, qs, log2f(static_cast<float>(s.it.n_e)));
           m = ceilf(e);
           l = fast_exp2(e - m);  // (a NaN passes on)
-          started = true;
-          const float by = a.order == 1 ? l * scale : 0.f;
-          if (a.order == 1) {
-            (void)pwait(&sh.s_full[g], ns & 1, sh, a);
-            ++ns;
-            tc_fence_after();
-          }
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t f[32];
-            tmem_ld32_async(tS + c, f);  // (order 0: not used)
-            tmem_wait_ld();
-            keep16(f);
-            keep16(f + 16);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float4 v4 = *reinterpret_cast<const float4*>(&sh.mu[1][c + 4 * i]);
-              const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                f[4 * i + k] = __float_as_uint(
-                    by != 0.f ? fmaf(__uint_as_float(f[4 * i + k]), by, v[k] * l) : v[k] * l);
-            }
-            tmem_st16(tO + c, f);
-            tmem_st16(tO + c + 16, f + 16);
-          }
-          tmem_wait_st();
-          if (a.order == 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.p_ready[g]);
-          }
         }
       }
       if (active) {
         ++nq;
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.q_empty);  // (with the MMA thread's commit: Q may be replaced)
+        if (lane == 0) mbar_arrive(&sh.q_empty);  // (with the MMA threads' commits: Q may be replaced)
       }
       const uint32_t seg_seq = vseq;  // of the first K tile
-      vseq += 2 * (k1 - k0);
-      for (int j = k0 + (BLOCKS == 2 ? 0 : g); j < k1; j += BLOCKS == 2 ? 1 : 2) {
+      vseq += 2 * (k1 - k0) + (mom && a.order == 1 ? (a.C16 != nullptr ? 1 : 2) : 0);
+      // The groups take turns at the exponentials: left to themselves they fell
+      // into step, and both waited for the special-function units and then for
+      // the tensor cores (4200 cycles a tile of 256 rows instead of 3000).
+      const int turns = BLOCKS == 2 ? k1 - k0 : (k1 - k0 + 1) >> 1;
+      for (int turn = 0; turn < turns; ++turn) {
+        const int j = BLOCKS == 2 ? k0 + turn : k0 + 2 * turn + g;
+        if (BLOCKS == 1 && j >= k1) {  // (an odd number of tiles: group 1 passes)
+          (void)pwait(&sh.turn[g], tph, sh, a);
+          tph ^= 1;
+          if (lane == 0) mbar_arrive(&sh.turn[g ^ 1]);
+          break;
+        }
         const int valid = s.valid(j);
         const bool tree = j >= s.it.cache;
         uint32_t words[4];  // the keys of this tile that the row sees
@@ -803,16 +824,71 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         (void)pwait(&sh.s_full[g], ns & 1, sh, a);
         ++ns;
+        (void)pwait(&sh.turn[g], tph, sh, a);
+        tph ^= 1;
         tc_fence_after();
-        if (warp_live) {
+        if (warp_live && !tree && valid == kTile) {
+          // a tile without a mask: its maximum, then its weights, the next 32
+          // columns on their way while 32 are worked on
+          uint32_t x[4][32];
+          float mx[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+          tmem_ld32_async(tS, x[0]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_wait_ld();
+            keep16(x[c]), keep16(x[c] + 16);
+            if (c < 3) tmem_ld32_async(tS + (c + 1) * 32, x[c + 1]);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2)
+              mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+          }
+          const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * qs;
+          if (__any_sync(kAll, top > m + kSlack)) {
+            const float mn = fmaxf(m, ceilf(top));
+            const float f = m == kNegInf ? 1.f : pow2(m - mn);
+            m = mn;
+            l *= f;
+            if (filled) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
+          }
+          const float ref = m == kNegInf ? 0.f : m;
+          const uint64_t qs2 = pair(qs, qs), nref = pair(-ref, -ref);
+          uint64_t sum2[2] = {0, 0};
+          uint32_t y[4][32];
+          tmem_ld32_async(tS, y[0]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_wait_ld();
+            keep16(y[c]), keep16(y[c] + 16);
+            if (c < 3) tmem_ld32_async(tS + (c + 1) * 32, y[c + 1]);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float t0, t1;
+              unpair(fma2(pair(__uint_as_float(y[c][i]), __uint_as_float(y[c][i + 1])), qs2, nref), t0, t1);
+              const float p0 = fast_exp2(t0), p1 = fast_exp2(t1);
+              sum2[(i >> 1) & 1] = add2(sum2[(i >> 1) & 1], pair(p0, p1));
+              y[c][i >> 1] = pack_bf16x2(p0, p1);
+            }
+            tmem_st16(tS + c * 16, y[c]);
+          }
+          float lo, hi;
+          unpair(add2(sum2[0], sum2[1]), lo, hi);
+          l += lo + hi;
+          tmem_wait_st();
+        } else if (warp_live) {
           // 32 columns at a time; a reference that has to move (by a whole
           // number: the factor is exact) takes O, l and the weights already
           // written of this tile along.  (P's columns lie below those of S that
           // are still to be read.)
           const uint64_t qs2 = pair(qs, qs);
           uint64_t sum2[2] = {0, 0};
-          auto columns = [&](uint32_t (&x)[32], int c) {
+#pragma unroll 1
+          for (int c = 0; c * 32 < valid; ++c) {
+            uint32_t x[32];
+            tmem_ld32_async(tS + c * 32, x);
             const uint32_t word = c == 0 ? words[0] : c == 1 ? words[1] : c == 2 ? words[2] : words[3];
+            tmem_wait_ld();
+            keep16(x);
+            keep16(x + 16);
             if (word != kAll) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
@@ -827,12 +903,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float f = m == kNegInf ? 1.f : pow2(m - mn);
               m = mn;
               float lo, hi;
-              unpair(sum2[0], lo, hi);
-              sum2[0] = pair(lo * f, hi * f);
-              unpair(sum2[1], lo, hi);
-              sum2[1] = pair(lo * f, hi * f);
-              l *= f;
-              if (started) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
+              unpair(add2(sum2[0], sum2[1]), lo, hi);
+              l = (l + lo + hi) * f;
+              sum2[0] = sum2[1] = 0;
+              if (filled) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
               scale_weights(tS, c, f);
             }
             const float ref = m == kNegInf ? 0.f : m;
@@ -846,29 +920,19 @@ __global__ void __launch_bounds__(kThreads, 1)
               x[i >> 1] = pack_bf16x2(p0, p1);
             }
             tmem_st16(tS + c * 16, x);
-          };
-#pragma unroll 1
-          for (int c = 0; c * 32 < valid; c += 2) {
-            uint32_t xa[32], xb[32];
-            tmem_ld32_async(tS + c * 32, xa);
-            tmem_ld32_async(tS + c * 32 + 32, xb);
-            tmem_wait_ld();
-            keep16(xa);
-            keep16(xa + 16);
-            keep16(xb);
-            keep16(xb + 16);
-            columns(xa, c);
-            columns(xb, c + 1);
           }
           float lo, hi;
           unpair(add2(sum2[0], sum2[1]), lo, hi);
           l += lo + hi;
           tmem_wait_st();
         }
-        started = true;
+        filled = true;
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_ready[g]);
+        if (lane == 0) {
+          mbar_arrive(&sh.p_ready[g]);
+          mbar_arrive(&sh.turn[g ^ 1]);
+        }
       }
 
       // ---- the segment's state: into the output (a whole item) or the workspace
@@ -879,25 +943,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       grid_dependency_wait();  // (a no-op unless the loads went early)
       const bool whole = s.begin == 0 && s.end == s.tiles;
-      const int part = 2 * blockIdx.x + (seg == 0 ? 0 : 1);
+      const int part = 2 * blockIdx.x + (s.begin == 0 ? 1 : 0);  // an item's start: this CTA's last segment; else its first
       constexpr int R = BLOCKS * kTile;
-      uint32_t seen_odd[8];
       bool any_odd = false;
-      if (BLOCKS == 1 && mom && k0 == k1) named_sync(1, 256);  // (group 0 has read mu, in ml's place)
-      if (BLOCKS == 1 && g == 1) sh.ml[r] = make_float2(m, started ? l : 0.f);
+      if (BLOCKS == 1 && g == 1) sh.ml[r] = make_float2(m, l);
       named_sync(1, 256);  // the other group's state; the nodes' odd values are known
+      auto seen_odd = [&](int w) {
+        return w < p.words ? sh.odd[seg & 1][w] & a.mask[((size_t)b * a.N + node) * p.words + w] : 0u;
+      };
       if (live && k1 > s.it.cache) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          seen_odd[i] = sh.odd[seg & 1][i];
-          any_odd |= seen_odd[i] != 0;
-        }
-        if (any_odd)
-          for (int i = 0; i < 8; ++i)
-            seen_odd[i] = i < p.words ? seen_odd[i] & a.mask[((size_t)b * a.N + node) * p.words + i] : 0u;
+        for (int i = 0; i < 8; ++i) any_odd |= sh.odd[seg & 1][i] != 0;
       }
-      // O = f0 O_0 + f1 O_1 over the columns this thread writes
-      float M = m, L = started ? l : 0.f, f0 = L != 0.f ? 1.f : 0.f, f1 = 0.f;
+      // output = f0 O_0 + f1 O_1 + w (mu_v + scale F) over the columns this thread writes
+      float M = m, L = l, f0 = L != 0.f ? 1.f : 0.f, f1 = 0.f;
       if (BLOCKS == 1 && g == 0) {
         const float2 y = sh.ml[r];
         M = fmaxf(L != 0.f ? m : kNegInf, y.y != 0.f ? y.x : kNegInf);
@@ -906,22 +965,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         f1 = y.y != 0.f ? fast_exp2(y.x - ref) : 0.f;
         L = (L != 0.f ? L * f0 : 0.f) + (y.y != 0.f ? y.y * f1 : 0.f);
       }
+      float w = mom && mine ? fast_exp2(e - M) : 0.f;
       if (whole) {
         const float inv = L != 0.f ? 1.f / L : 0.f;
-        f0 *= inv, f1 *= inv;
+        f0 *= inv, f1 *= inv, w *= inv;
       }
       if (BLOCKS == 1) {
-        if (g == 0) sh.ml[r] = make_float2(f0, f1);
+        if (g == 0) {
+          sh.ml[r] = make_float2(f0, f1);
+          sh.w[r] = w;
+        }
         named_sync(1, 256);
-        f0 = sh.ml[r].x, f1 = sh.ml[r].y;
+        f0 = sh.ml[r].x, f1 = sh.ml[r].y, w = sh.w[r];
       }
       // a factor of 0 stands for a state without content: its columns may hold anything
-      const bool use0 = f0 != 0.f, use1 = f1 != 0.f;
+      const bool use0 = f0 != 0.f && k1 > k0, use1 = f1 != 0.f && k1 > k0 + 1, use_f = mom && a.order == 1;
+      const float wf = w * scale;
       const bool put = node < a.N;
       const size_t orow = ((size_t)b * a.N + node) * HQ + (kv << p.g_shift) + h;
       constexpr int kCols = BLOCKS == 2 ? D : D / 2;
       const int c_lo = BLOCKS == 2 ? 0 : g * (D / 2);
       const uint32_t tA = tm + lanes + cO + (BLOCKS == 2 ? g * D : 0) + c_lo, tB = tA + D;
+      const uint32_t tF = tm + lanes + cS + (BLOCKS == 2 ? g * 128 : 0) + c_lo;
 #pragma unroll 1
       for (int c = 0; c < kCols; c += 32) {
         uint32_t x[32], y[32];
@@ -936,21 +1001,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           o[i] = use0 ? __uint_as_float(x[i]) * f0 : 0.f;
           if (BLOCKS == 1 && use1) o[i] = fmaf(__uint_as_float(y[i]), f1, o[i]);
         }
-        if (any_odd) {
-#pragma unroll 1
-          for (int w = 0; w < 8; ++w)
-            for (uint32_t bits = seen_odd[w]; bits != 0; bits &= bits - 1) {
-              const int n = w * 32 + __ffs(bits) - 1;
-              const int j = s.it.cache + (n >> 7);
-              if (j < k0 || j >= k1 || n >= s.it.count) continue;
-              const __nv_bfloat16* v =
-                  static_cast<const __nv_bfloat16*>(a.v) + b * a.kv_batch + n * a.kv_node + kv * D + c_lo + c;
+        if (mom) {
+          if (use_f) {
+            tmem_ld32_async(tF + c, x);
+            tmem_wait_ld();
+            keep16(x), keep16(x + 16);
+          }
+          const float4* mv = reinterpret_cast<const float4*>(a.mu_v + (size_t)s.unit * D + c_lo + c);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float z = __bfloat162float(v[i]);
-                if (!isfinite(z)) o[i] += z;
-              }
+          for (int i = 0; i < 8; ++i) {
+            const float4 v4 = mv[i];
+            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              o[4 * i + k] = fmaf(v[k], w, o[4 * i + k]);
+              if (use_f) o[4 * i + k] = fmaf(__uint_as_float(x[4 * i + k]), wf, o[4 * i + k]);
             }
+          }
         }
         if (whole) {
           if (put) {
@@ -969,6 +1036,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                 make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         }
       }
+      if (any_odd && (put || !whole)) {
+        // the values that are not finite join the row's columns one by one
+        const int row = BLOCKS == 2 ? g * kTile + r : r;
+#pragma unroll 1
+        for (int n = 0; n < s.it.count; ++n) {
+          const int j = s.it.cache + (n >> 7);
+          if (j < k0 || j >= k1 || !((seen_odd(n >> 5) >> (n & 31)) & 1u)) continue;
+          const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v) + b * a.kv_batch + n * a.kv_node + kv * D;
+#pragma unroll 1
+          for (int c = c_lo; c < c_lo + kCols; ++c) {
+            const float z = __bfloat162float(v[c]);
+            if (isfinite(z)) continue;
+            if (whole) {
+              a.out[orow * D + c] = __float2bfloat16_rn(__bfloat162float(a.out[orow * D + c]) + z);
+            } else {
+              float* o = reinterpret_cast<float*>(&parts.o[((size_t)part * (D / 4) + c / 4) * R + row]) + (c & 3);
+              *o += z;
+            }
+          }
+        }
+      }
       if (BLOCKS == 2 || g == 0) {
         if (whole) {
           if (put && a.lse != nullptr) a.lse[orow] = live && L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
@@ -979,7 +1067,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (tid < 8) sh.odd[(seg + 1) & 1][tid] = 0;  // (read last in the segment before)
       ++seg;
       tc_fence_before();
-      named_sync(1, 256);  // both groups are done with O and the exchange
+      named_sync(1, 256);  // both groups are done with O, Q C'^T and the exchange
+      if (use_f && mine && lane == 0) mbar_arrive(&sh.p_ready[g]);
     }
     if (p.list && tid == 0) parts.desc[blockIdx.x] = sh.cut;  // what tree_merge_kernel joins
   }
@@ -1002,9 +1091,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins the parts of the items that a boundary of the list cuts: block (c, y)
-// the item whose first inner boundary is CTA c's, y the columns 8 y .. 8 y + 7,
-// a thread a row and 4 columns.
+// Joins the parts of the items that a boundary of the list cuts: block (c, y, z)
+// the item whose first inner boundary is CTA c's, y 32 columns, z a row block;
+// a thread a row and 16 columns (with 4 columns the blocks took four waves of
+// the same latency).
 template <int D>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
                                                          const __grid_constant__ Plan p,
@@ -1013,38 +1103,48 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   grid_launch_dependents();
   const int4 d = parts.desc[blockIdx.x];
   if (d.x < 0) return;
-  const int R = p.blocks * kTile, row = blockIdx.z * kTile + (threadIdx.x & 127), c4 = blockIdx.y * 2 + (threadIdx.x >> 7);
-  const int G = 1 << p.g_shift, u = d.z, b = u / a.n_kv, kv = u % a.n_kv;
+  const int R = p.blocks * kTile, row = blockIdx.z * kTile + (threadIdx.x & 127);
+  const int c4 = (blockIdx.y * 2 + (threadIdx.x >> 7)) * 4;
+  const int G = 1 << p.g_shift, u = d.z, b = batch_of(p, u), kv = u - b * a.n_kv;
   const int node = d.w * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
   if (node >= a.N) return;
   const int count = a.count != nullptr ? a.count[b] : a.N;
   const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
-  const int n = d.y - blockIdx.x + 2;  // parts: the first one, then one per CTA up to the last
-  auto part = [&](int i) { return i == 0 ? d.x : 2 * (static_cast<int>(blockIdx.x) + i - 1); };
+  const int n = d.y - blockIdx.x + 2;  // parts: the end of the CTA before, then the starts of those up to the last
+  auto part = [&](int i) { return (size_t)(2 * (static_cast<int>(blockIdx.x) + i - 1) + (i == 0 ? 1 : 0)); };
   float M = kNegInf, L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int i = 0; i < n; ++i) {
-    const float2 x = parts.ml[(size_t)part(i) * R + row];
+    const float2 x = parts.ml[part(i) * R + row];
     if (x.y != 0.f) M = fmaxf(M, x.x);
   }
   const float ref = M == kNegInf ? 0.f : M;
-#pragma unroll 4
+  float acc[16] = {};
+#pragma unroll 2
   for (int i = 0; i < n; ++i) {
-    const float2 x = parts.ml[(size_t)part(i) * R + row];
-    const float4 o = parts.o[((size_t)part(i) * (D / 4) + c4) * R + row];
-    if (x.y != 0.f) {
+    const float2 x = parts.ml[part(i) * R + row];
+    const float4* src = parts.o + (part(i) * (D / 4) + c4) * R + row;
+    const float4 o[4] = {src[0], src[R], src[2 * R], src[3 * R]};
+    if (x.y != 0.f) {  // (a part without content may hold anything)
       const float f = fast_exp2(x.x - ref);
       L = fmaf(x.y, f, L);
-      acc.x = fmaf(o.x, f, acc.x);
-      acc.y = fmaf(o.y, f, acc.y);
-      acc.z = fmaf(o.z, f, acc.z);
-      acc.w = fmaf(o.w, f, acc.w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        acc[4 * k] = fmaf(o[k].x, f, acc[4 * k]);
+        acc[4 * k + 1] = fmaf(o[k].y, f, acc[4 * k + 1]);
+        acc[4 * k + 2] = fmaf(o[k].z, f, acc[4 * k + 2]);
+        acc[4 * k + 3] = fmaf(o[k].w, f, acc[4 * k + 3]);
+      }
     }
   }
   const bool live = node < min(max(count, 0), a.N) && L != 0.f;
   const float inv = live ? 1.f / L : 0.f;
-  *reinterpret_cast<uint2*>(a.out + orow * D + c4 * 4) =
-      live ? make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0, 0);
+  uint32_t y[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y[k] = live ? pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv) : 0u;
+  uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c4 * 4);
+  dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+  dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
   if (c4 == 0 && a.lse != nullptr) a.lse[orow] = live ? (M + log2f(L)) * kLn2 : kNegInf;
 }
 
@@ -1055,6 +1155,7 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   p.mb = (rows + p.blocks * kTile - 1) / (p.blocks * kTile);
   p.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
   p.words = tree_words(n_nodes);
+  p.kv_inv = ((1ull << 40) + g.n_kv_heads - 1) / g.n_kv_heads;
   const long units = (long)g.batch * g.n_kv_heads, items = units * p.mb;
   const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
   p.min_run = 2;
@@ -1099,7 +1200,7 @@ cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, co
   e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
                  tm[3], tm[4]);
   if (e != cudaSuccess || !p.list) return e;
-  return launch_pdl(tree_merge_kernel<D>, dim3(p.grid, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts);
+  return launch_pdl(tree_merge_kernel<D>, dim3(p.grid, D / 32, BLOCKS), dim3(256), 0, stream, a, p, parts);
 }
 
 }  // namespace
