@@ -430,6 +430,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   Shared& sh = *reinterpret_cast<Shared*>(ring + NS * kSlot);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == kWarpTma && lane < 5) {
+    const CUtensorMap* map = lane == 0 ? &tmQ : lane == 1 ? &tmK : lane == 2 ? &tmV : lane == 3 ? &tmKt : &tmVt;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+  }
   if (!a.early) grid_dependency_wait();
   Raw mine{};  // in flight while the barriers are set up
   if (tid < a.batch * a.n_kv) mine = load_raw(a, p, tid);
@@ -592,7 +596,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           t += kStep / 2;
           n16 = t < k1 ? (s.valid(t) + 15) & ~15 : 0;
           const uint64_t db = dV + vi * (kSlot >> 4);
-          ok = pwait(&sh.full[vi], vph, sh, a) && pwait(&sh.p_ready[g], pph, sh, a);
+          // (P first: it is ready only after the slot's use before has been
+          // consumed -- with one row block that is the other thread's, and a
+          // phase's parity alone would not tell the two apart)
+          ok = pwait(&sh.p_ready[g], pph, sh, a) && pwait(&sh.full[vi], vph, sh, a);
           pph ^= 1;
           if (!ok) break;
           tc_fence_after();
@@ -788,8 +795,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) words[i] &= live && w0 + i < p.words ? row[i] : 0u;
         }
+        (void)pwait(&sh.s_full[g], ns & 1, sh, a);
+        ++ns;
+        (void)pwait(&sh.turn[g], tph, sh, a);
+        tph ^= 1;
         if (tree || valid % 16 != 0) {
-          // V rows past the keys in use must be finite (their weights are 0),
+          // (in turn: the other group's products with what the slot held before
+          // are complete.)  V rows past the keys in use must be finite (their weights are 0),
           // and so must a node's value where its weight is 0: elements that
           // are not are taken out here and reach the nodes that see them at
           // the end
@@ -822,10 +834,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           fence_async_smem();
         }
-        (void)pwait(&sh.s_full[g], ns & 1, sh, a);
-        ++ns;
-        (void)pwait(&sh.turn[g], tph, sh, a);
-        tph ^= 1;
         tc_fence_after();
         if (warp_live && !tree && valid == kTile) {
           // a tile without a mask: its maximum, then its weights, the next 32
@@ -1028,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                          pack_bf16x2(o[8 * i + 4], o[8 * i + 5]), pack_bf16x2(o[8 * i + 6], o[8 * i + 7]))
                             : make_uint4(0, 0, 0, 0);
           }
-        } else {
+        } else if (warp_live) {  // (rows that are not in use are not joined)
           const int row = BLOCKS == 2 ? g * kTile + r : r;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -1060,7 +1068,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (BLOCKS == 2 || g == 0) {
         if (whole) {
           if (put && a.lse != nullptr) a.lse[orow] = live && L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
-        } else {
+        } else if (warp_live) {
           parts.ml[(size_t)part * R + (BLOCKS == 2 ? g * kTile + r : r)] = make_float2(M, L);
         }
       }
@@ -1092,60 +1100,62 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of the items that a boundary of the list cuts: block (c, y, z)
-// the item whose first inner boundary is CTA c's, y 32 columns, z a row block;
-// a thread a row and 16 columns (with 4 columns the blocks took four waves of
-// the same latency).
-template <int D>
+// the item whose first inner boundary is CTA c's, y 8 Q columns, z a row block; a
+// thread a row and 4 Q columns.  Bounded by latency: with many items Q = 4 keeps
+// the blocks in one wave, with few (of many parts each) Q = 1 spreads them.
+template <int D, int Q>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
                                                          const __grid_constant__ Plan p,
                                                          const __grid_constant__ Parts parts) {
   grid_dependency_wait();
   grid_launch_dependents();
-  const int4 d = parts.desc[blockIdx.x];
+  const int c = blockIdx.x;
+  const int4 d = parts.desc[c];
   if (d.x < 0) return;
   const int R = p.blocks * kTile, row = blockIdx.z * kTile + (threadIdx.x & 127);
-  const int c4 = (blockIdx.y * 2 + (threadIdx.x >> 7)) * 4;
+  const int c4 = (blockIdx.y * 2 + (threadIdx.x >> 7)) * Q;
   const int G = 1 << p.g_shift, u = d.z, b = batch_of(p, u), kv = u - b * a.n_kv;
   const int node = d.w * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
   if (node >= a.N) return;
-  const int count = a.count != nullptr ? a.count[b] : a.N;
   const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
-  const int n = d.y - blockIdx.x + 2;  // parts: the end of the CTA before, then the starts of those up to the last
-  auto part = [&](int i) { return (size_t)(2 * (static_cast<int>(blockIdx.x) + i - 1) + (i == 0 ? 1 : 0)); };
-  float M = kNegInf, L = 0.f;
+  float M = kNegInf, L = 0.f, acc[4 * Q] = {};
+  if (node < (a.count != nullptr ? a.count[b] : a.N)) {
+    const int n = d.y - c + 2;  // parts: the end of the CTA before, then the starts of those up to the last
+    auto part = [&](int i) { return (size_t)(2 * (c + i - 1) + (i == 0 ? 1 : 0)); };
 #pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float2 x = parts.ml[part(i) * R + row];
-    if (x.y != 0.f) M = fmaxf(M, x.x);
-  }
-  const float ref = M == kNegInf ? 0.f : M;
-  float acc[16] = {};
-#pragma unroll 2
-  for (int i = 0; i < n; ++i) {
-    const float2 x = parts.ml[part(i) * R + row];
-    const float4* src = parts.o + (part(i) * (D / 4) + c4) * R + row;
-    const float4 o[4] = {src[0], src[R], src[2 * R], src[3 * R]};
-    if (x.y != 0.f) {  // (a part without content may hold anything)
-      const float f = fast_exp2(x.x - ref);
-      L = fmaf(x.y, f, L);
+    for (int i = 0; i < n; ++i) {
+      const float2 x = parts.ml[part(i) * R + row];
+      if (x.y != 0.f) M = fmaxf(M, x.x);
+    }
+    const float ref = M == kNegInf ? 0.f : M;
+#pragma unroll(Q == 1 ? 4 : 2)
+    for (int i = 0; i < n; ++i) {
+      const float2 x = parts.ml[part(i) * R + row];
+      const float4* src = parts.o + (part(i) * (D / 4) + c4) * R + row;
+      float4 o[Q];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        acc[4 * k] = fmaf(o[k].x, f, acc[4 * k]);
-        acc[4 * k + 1] = fmaf(o[k].y, f, acc[4 * k + 1]);
-        acc[4 * k + 2] = fmaf(o[k].z, f, acc[4 * k + 2]);
-        acc[4 * k + 3] = fmaf(o[k].w, f, acc[4 * k + 3]);
+      for (int k = 0; k < Q; ++k) o[k] = src[k * R];
+      if (x.y != 0.f) {  // (a part without content may hold anything)
+        const float f = fast_exp2(x.x - ref);
+        L = fmaf(x.y, f, L);
+#pragma unroll
+        for (int k = 0; k < Q; ++k) {
+          acc[4 * k] = fmaf(o[k].x, f, acc[4 * k]);
+          acc[4 * k + 1] = fmaf(o[k].y, f, acc[4 * k + 1]);
+          acc[4 * k + 2] = fmaf(o[k].z, f, acc[4 * k + 2]);
+          acc[4 * k + 3] = fmaf(o[k].w, f, acc[4 * k + 3]);
+        }
       }
     }
   }
-  const bool live = node < min(max(count, 0), a.N) && L != 0.f;
-  const float inv = live ? 1.f / L : 0.f;
-  uint32_t y[8];
+  const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y[k] = live ? pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv) : 0u;
-  uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c4 * 4);
-  dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
-  dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
-  if (c4 == 0 && a.lse != nullptr) a.lse[orow] = live ? (M + log2f(L)) * kLn2 : kNegInf;
+  for (int k = 0; k < Q; ++k)
+    reinterpret_cast<uint2*>(a.out + orow * D)[c4 + k] =
+        L != 0.f ? make_uint2(pack_bf16x2(acc[4 * k] * inv, acc[4 * k + 1] * inv),
+                              pack_bf16x2(acc[4 * k + 2] * inv, acc[4 * k + 3] * inv))
+                 : make_uint2(0, 0);
+  if (c4 == 0 && a.lse != nullptr) a.lse[orow] = L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
 }
 
 Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
@@ -1200,7 +1210,9 @@ cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, co
   e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
                  tm[3], tm[4]);
   if (e != cudaSuccess || !p.list) return e;
-  return launch_pdl(tree_merge_kernel<D>, dim3(p.grid, D / 32, BLOCKS), dim3(256), 0, stream, a, p, parts);
+  return (long)a.batch * a.n_kv * p.mb >= 48
+             ? launch_pdl(tree_merge_kernel<D, 4>, dim3(p.grid, D / 32, BLOCKS), dim3(256), 0, stream, a, p, parts)
+             : launch_pdl(tree_merge_kernel<D, 1>, dim3(p.grid, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts);
 }
 
 }  // namespace
