@@ -11,7 +11,10 @@
 // weight starts m and l, and its value joins at the end, the product Q C'^T
 // running on the tensor cores with C' as bf16 hi + lo parts.  m only has to be
 // common to a row's keys, so it moves (by a whole number, with a rescaling of
-// O and l) only when a score exceeds it by more than 8 in log2 units.  P enters
+// O and l) only when a score exceeds it by more than 32 in log2 units: a
+// floating-point sum of weights up to 2^32 is as exact as one of weights up to 1,
+// and with 8 some row of a warp moved in most tiles of a long cache (700
+// cycles each).  P enters
 // the second product rounded to bf16 (2^-8 relative, the output's own
 // rounding); l is summed from the unrounded weights.
 //
@@ -34,6 +37,8 @@
 // waited for its own instructions (a masked tile took 9000 cycles instead of
 // 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
 // 128 columns each, and O of the two, D columns each.
+#include <stddef.h>
+
 #include <algorithm>
 #include <mutex>
 
@@ -52,7 +57,7 @@ constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpC = 12;
 constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps and an idle one; four for C'
 constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
-constexpr float kSlack = 8.f;                // log2 headroom of the reference (weights <= 2^8)
+constexpr float kSlack = 32.f;               // log2 headroom of the reference: weights are at most 2^32
 constexpr float kNegInf = -INFINITY;
 constexpr uint32_t kAll = 0xffffffffu;
 
@@ -73,7 +78,7 @@ struct Plan {
 
 // A part of a split item (m, l, O of `blocks` x 128 rows).
 struct Parts {
-  int4* desc;   // [grid] of the item whose first inner boundary is the CTA's start: (1 or -1, last CTA, unit, mb)
+  int2* desc;   // [items]: the CTAs of its first and of its last part (the same: it is whole)
   float2* ml;   // [2 grid][blocks 128]
   float4* o;    // [2 grid][D / 4][blocks 128]
 };
@@ -90,16 +95,17 @@ struct Shared {
   int32_t unit, mb, t0, start, end;  // the CTA's run of the list: first item, tile in it, the list's tiles [start, end)
   Raw raw;                     // of the first unit
   int32_t scan[kThreads / 32];
-  int4 cut;                    // parts.desc of this CTA
+  int32_t run;                 // tiles per CTA before the ends are moved
   uint32_t odd[2][8];          // nodes with a value that is not finite, of this segment and the next
   float2 ml[kTile];            // (one row block) group 1's (m, l), then the two groups' factors
-  union {
+  union alignas(16) {   // (read as float4)
     float mu_k[kTile];  // from a segment's start
     float w[kTile];     // (one row block) at its end: the moment term's factor
   };
 };
 constexpr int kSharedBytes = 2048;
 static_assert(sizeof(Shared) <= kSharedBytes, "shared variables");
+static_assert(offsetof(Shared, mu_k) % 16 == 0 && kSharedBytes % 16 == 0, "mu_k is read 16 bytes at a time");
 __host__ __device__ constexpr int smem_bytes(int D, int blocks) {
   return (blocks + ring_slots(D, blocks)) * slot_bytes(D) + kSharedBytes + 1024;
 }
@@ -216,6 +222,19 @@ __device__ __forceinline__ void scale_weights(uint32_t tS, int n, float f) {
       o[i] = pack_bf16x2(x.x * f, x.y * f);
     }
     tmem_st16(tS + c * 16, o);
+  }
+}
+
+// Eight words of a row, at once where the address is a multiple of 32 bytes (the
+// rows of a warp lie 256 bytes apart: the fewer stores the better).
+__device__ __forceinline__ void store8(void* dst, const uint32_t* x, bool aligned32) {
+  if (aligned32) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(x[0]), "r"(x[1]), "r"(x[2]),
+                 "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(x[4], x[5], x[6], x[7]);
   }
 }
 
@@ -355,7 +374,6 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
   if ((tid & 31) == 31) sh.scan[tid >> 5] = incl;
   if (tid == 0) {
     sh.start = sh.end = 0;
-    sh.cut = make_int4(-1, 0, 0, 0);
   }
   __syncthreads();
   int before = 0, total = 0;
@@ -367,6 +385,7 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
   }
   const int run = max(p.min_run, (total + p.grid - 1) / p.grid);
   const int at = before + incl - sum;  // of this thread's first unit
+  if (tid == 0) sh.run = run;
   // The run is [start, end) with both ends moved off an item's first and last
   // tile, to the item's edge: no CTA is left with the moment term alone or with
   // one tile to begin with.
@@ -409,8 +428,6 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
     sh.t0 = in > 0 && snap == pos ? in : 0;
     sh.raw = r;
     sh.start = snap;
-    // the first boundary inside an item sees to its merge
-    if (sh.t0 > 0 && in - run <= 1) sh.cut = make_int4(1, (item + tiles - 2) / run, u, mb);
   }
   __syncthreads();
 }
@@ -724,8 +741,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = 1 << p.g_shift, HQ = a.n_kv << p.g_shift;
     uint32_t nq = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots of the segments before
     uint32_t tph = 0;
+    const bool aligned_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
     if (g == 1 && lane == 0) mbar_arrive(&sh.turn[0]);  // group 0 begins
-    int seg = 0;
+    int seg = 0, at = sh.start;  // the list's tile that the segment begins with
     while (walk.next(a, p, s)) {
       const bool mom = s.mom;
       const int k0 = s.k0, k1 = s.k1, b = batch_of(p, s.unit), kv = s.unit - b * a.n_kv;
@@ -738,6 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool filled = false;  // O holds something
       if (mom) {
         if (tid < D) sh.mu_k[tid] = a.mu_k[(size_t)s.unit * D + tid];
+        if (tid < D / 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.mu_v + (size_t)s.unit * D + tid * 32));
         named_sync(1, 256);
         (void)pwait(&sh.q_full, nq & 1, sh, a);
         if (mine) {
@@ -951,6 +970,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       grid_dependency_wait();  // (a no-op unless the loads went early)
       const bool whole = s.begin == 0 && s.end == s.tiles;
+      // An item's first part says where the others are: the last boundary that
+      // stays inside it is the last at or below its tile tiles - 2.
+      if (p.list && s.begin == 0 && tid == 0)
+        parts.desc[s.unit * p.mb + s.mb] = make_int2(blockIdx.x, whole ? blockIdx.x : (at + s.tiles - 2) / sh.run);
+      at += s.end - s.begin;
       const int part = 2 * blockIdx.x + (s.begin == 0 ? 1 : 0);  // an item's start: this CTA's last segment; else its first
       constexpr int R = BLOCKS * kTile;
       bool any_odd = false;
@@ -1029,12 +1053,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (whole) {
           if (put) {
-            uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c_lo + c);
+            __nv_bfloat16* dst = a.out + orow * D + c_lo + c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              dst[i] = live ? make_uint4(pack_bf16x2(o[8 * i], o[8 * i + 1]), pack_bf16x2(o[8 * i + 2], o[8 * i + 3]),
-                                         pack_bf16x2(o[8 * i + 4], o[8 * i + 5]), pack_bf16x2(o[8 * i + 6], o[8 * i + 7]))
-                            : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) x[i] = live ? pack_bf16x2(o[2 * i], o[2 * i + 1]) : 0u;
+            store8(dst, x, aligned_out);
+            store8(dst + 16, x + 8, aligned_out);
           }
         } else if (warp_live) {  // (rows that are not in use are not joined)
           const int row = BLOCKS == 2 ? g * kTile + r : r;
@@ -1078,7 +1101,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       named_sync(1, 256);  // both groups are done with O, Q C'^T and the exchange
       if (use_f && mine && lane == 0) mbar_arrive(&sh.p_ready[g]);
     }
-    if (p.list && tid == 0) parts.desc[blockIdx.x] = sh.cut;  // what tree_merge_kernel joins
   }
 
   __syncthreads();
@@ -1099,55 +1121,81 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins the parts of the items that a boundary of the list cuts: block (c, y, z)
-// the item whose first inner boundary is CTA c's, y 8 Q columns, z a row block; a
-// thread a row and 4 Q columns.  Bounded by latency: with many items Q = 4 keeps
-// the blocks in one wave, with few (of many parts each) Q = 1 spreads them.
-template <int D, int Q>
+// Joins the parts of the items that a boundary of the list cuts.  Bounded by
+// latency, so the parts are read side by side: block (item, y, z) has W rows of
+// 32 x 4 Q columns of the item's row block z, 8 / W warps a group of rows, each
+// taking every (8 / W)-th part.  Few items of many parts: W = 1, Q = 1; many
+// items of two or three parts: W = 4, Q = 2.
+template <int D, int W, int Q>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
                                                          const __grid_constant__ Plan p,
                                                          const __grid_constant__ Parts parts) {
+  constexpr int kParts = 8 / W;  // parts side by side
+  constexpr int kCols = D / (4 * Q);
+  __shared__ float2 s_ml[kParts > 1 ? 8 : 1][32];
+  __shared__ float4 s_o[kParts > 1 ? 8 : 1][Q][32];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int c = blockIdx.x;
-  const int4 d = parts.desc[c];
-  if (d.x < 0) return;
-  const int R = p.blocks * kTile, row = blockIdx.z * kTile + (threadIdx.x & 127);
-  const int c4 = (blockIdx.y * 2 + (threadIdx.x >> 7)) * Q;
-  const int G = 1 << p.g_shift, u = d.z, b = batch_of(p, u), kv = u - b * a.n_kv;
-  const int node = d.w * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
-  if (node >= a.N) return;
-  const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
+  const int item = blockIdx.x, u = item / p.mb, mb = item - u * p.mb;
+  const int2 d = parts.desc[item];
+  if (d.x == d.y) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp / kParts, wp = warp % kParts;
+  const int R = p.blocks * kTile, rg = blockIdx.y / kCols * W + wr, row = blockIdx.z * kTile + rg * 32 + lane;
+  const int c4 = blockIdx.y % kCols * Q;
+  const int G = 1 << p.g_shift, b = batch_of(p, u), kv = u - b * a.n_kv;
+  const int node = mb * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
+  const int n = d.y - d.x + 1;
   float M = kNegInf, L = 0.f, acc[4 * Q] = {};
-  if (node < (a.count != nullptr ? a.count[b] : a.N)) {
-    const int n = d.y - c + 2;  // parts: the end of the CTA before, then the starts of those up to the last
-    auto part = [&](int i) { return (size_t)(2 * (c + i - 1) + (i == 0 ? 1 : 0)); };
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float2 x = parts.ml[part(i) * R + row];
-      if (x.y != 0.f) M = fmaxf(M, x.x);
-    }
-    const float ref = M == kNegInf ? 0.f : M;
-#pragma unroll(Q == 1 ? 4 : 2)
-    for (int i = 0; i < n; ++i) {
+  if (node < a.N && node < (a.count != nullptr ? a.count[b] : a.N)) {
+    // parts: the end of CTA d.x, then the starts of those up to d.y
+    auto part = [&](int i) { return (size_t)(2 * (d.x + i) + (i == 0 ? 1 : 0)); };
+#pragma unroll 2
+    for (int i = wp; i < n; i += kParts) {
       const float2 x = parts.ml[part(i) * R + row];
       const float4* src = parts.o + (part(i) * (D / 4) + c4) * R + row;
       float4 o[Q];
 #pragma unroll
       for (int k = 0; k < Q; ++k) o[k] = src[k * R];
       if (x.y != 0.f) {  // (a part without content may hold anything)
-        const float f = fast_exp2(x.x - ref);
-        L = fmaf(x.y, f, L);
+        const float mn = fmaxf(M, x.x), ref = mn == kNegInf ? 0.f : mn;
+        const float f0 = L != 0.f ? fast_exp2(M - ref) : 0.f, f = fast_exp2(x.x - ref);
+        M = mn;
+        L = L * f0 + x.y * f;
 #pragma unroll
         for (int k = 0; k < Q; ++k) {
-          acc[4 * k] = fmaf(o[k].x, f, acc[4 * k]);
-          acc[4 * k + 1] = fmaf(o[k].y, f, acc[4 * k + 1]);
-          acc[4 * k + 2] = fmaf(o[k].z, f, acc[4 * k + 2]);
-          acc[4 * k + 3] = fmaf(o[k].w, f, acc[4 * k + 3]);
+          acc[4 * k] = fmaf(o[k].x, f, acc[4 * k] * f0);
+          acc[4 * k + 1] = fmaf(o[k].y, f, acc[4 * k + 1] * f0);
+          acc[4 * k + 2] = fmaf(o[k].z, f, acc[4 * k + 2] * f0);
+          acc[4 * k + 3] = fmaf(o[k].w, f, acc[4 * k + 3] * f0);
         }
       }
     }
   }
+  if constexpr (kParts > 1) {
+    s_ml[warp][lane] = make_float2(M, L);
+#pragma unroll
+    for (int k = 0; k < Q; ++k) s_o[warp][k][lane] = make_float4(acc[4 * k], acc[4 * k + 1], acc[4 * k + 2], acc[4 * k + 3]);
+    __syncthreads();
+    if (wp != 0) return;
+    for (int w = 1; w < min(kParts, n); ++w) {
+      const float2 x = s_ml[warp + w][lane];
+      if (x.y == 0.f) continue;
+      const float mn = fmaxf(M, x.x), ref = mn == kNegInf ? 0.f : mn;
+      const float f0 = L != 0.f ? fast_exp2(M - ref) : 0.f, f = fast_exp2(x.x - ref);
+      M = mn;
+      L = L * f0 + x.y * f;
+#pragma unroll
+      for (int k = 0; k < Q; ++k) {
+        const float4 o = s_o[warp + w][k][lane];
+        acc[4 * k] = fmaf(o.x, f, acc[4 * k] * f0);
+        acc[4 * k + 1] = fmaf(o.y, f, acc[4 * k + 1] * f0);
+        acc[4 * k + 2] = fmaf(o.z, f, acc[4 * k + 2] * f0);
+        acc[4 * k + 3] = fmaf(o.w, f, acc[4 * k + 3] * f0);
+      }
+    }
+  }
+  if (node >= a.N) return;
+  const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
   const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
   for (int k = 0; k < Q; ++k)
@@ -1178,7 +1226,7 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
 size_t parts_bytes(const mkv_geom& g, const Plan& p) {
   if (!p.list) return 0;
   const size_t R = (size_t)p.blocks * kTile;
-  return align_up((size_t)p.grid * sizeof(int4), 256) + 2 * (size_t)p.grid * R * (8 + (size_t)g.head_dim * 4);
+  return align_up((size_t)g.batch * g.n_kv_heads * p.mb * sizeof(int2), 256) + 2 * (size_t)p.grid * R * (8 + (size_t)g.head_dim * 4);
 }
 
 // bf16 [n3][n2][n1][inner] with the strides of n1, n2, n3 in elements; boxes of b1 x b2 rows of 64 elements.
@@ -1210,9 +1258,10 @@ cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, co
   e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
                  tm[3], tm[4]);
   if (e != cudaSuccess || !p.list) return e;
-  return (long)a.batch * a.n_kv * p.mb >= 48
-             ? launch_pdl(tree_merge_kernel<D, 4>, dim3(p.grid, D / 32, BLOCKS), dim3(256), 0, stream, a, p, parts)
-             : launch_pdl(tree_merge_kernel<D, 1>, dim3(p.grid, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts);
+  const int items = a.batch * a.n_kv * p.mb;
+  return items >= 48
+             ? launch_pdl(tree_merge_kernel<D, 4, 2>, dim3(items, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts)
+             : launch_pdl(tree_merge_kernel<D, 1, 1>, dim3(items, D / 4 * 4, BLOCKS), dim3(256), 0, stream, a, p, parts);
 }
 
 }  // namespace
@@ -1228,8 +1277,8 @@ cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sm
   Parts parts{};
   const int D = g.head_dim, R = p.blocks * kTile;
   uint8_t* w = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
-  parts.desc = reinterpret_cast<int4*>(w);
-  w += align_up((size_t)p.grid * sizeof(int4), 256);
+  parts.desc = reinterpret_cast<int2*>(w);
+  w += align_up((size_t)a.batch * a.n_kv * p.mb * sizeof(int2), 256);
   parts.o = reinterpret_cast<float4*>(w);
   w += 2 * (size_t)p.grid * R * D * 4;
   parts.ml = reinterpret_cast<float2*>(w);
