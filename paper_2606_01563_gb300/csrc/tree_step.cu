@@ -1122,26 +1122,25 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of the items that a boundary of the list cuts.  Bounded by
-// latency, so the parts are read side by side: block (item, y, z) has W rows of
-// 32 x 4 Q columns of the item's row block z, 8 / W warps a group of rows, each
-// taking every (8 / W)-th part.  Few items of many parts: W = 1, Q = 1; many
-// items of two or three parts: W = 4, Q = 2.
-template <int D, int W, int Q>
+// latency: as many threads as the GPU holds at once are best, each with all of
+// its loads in flight.  A warp has 32 rows x 4 Q columns of an item; P warps
+// share them where there are few, every P-th part each.
+template <int D, int P, int Q>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
                                                          const __grid_constant__ Plan p,
                                                          const __grid_constant__ Parts parts) {
-  constexpr int kParts = 8 / W;  // parts side by side
-  constexpr int kCols = D / (4 * Q);
-  __shared__ float2 s_ml[kParts > 1 ? 8 : 1][32];
-  __shared__ float4 s_o[kParts > 1 ? 8 : 1][Q][32];
+  constexpr int kCols = D / (4 * Q);  // column groups of an item
+  __shared__ float2 s_ml[P > 1 ? 8 : 1][32];
+  __shared__ float4 s_o[P > 1 ? 8 : 1][Q][32];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int item = blockIdx.x, u = item / p.mb, mb = item - u * p.mb;
-  const int2 d = parts.desc[item];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wp = warp % P;
+  const int id = blockIdx.x * (8 / P) + warp / P;  // (item, row block, column group, 32 rows)
+  const int c4 = (id >> 2) % kCols * Q, z = (id >> 2) / kCols % p.blocks, item = (id >> 2) / kCols / p.blocks;
+  const int u = item / p.mb, mb = item - u * p.mb;
+  const int2 d = parts.desc[item];  // (the same item in all warps of a block: it has at least 16 groups)
   if (d.x == d.y) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp / kParts, wp = warp % kParts;
-  const int R = p.blocks * kTile, rg = blockIdx.y / kCols * W + wr, row = blockIdx.z * kTile + rg * 32 + lane;
-  const int c4 = blockIdx.y % kCols * Q;
+  const int R = p.blocks * kTile, row = z * kTile + (id & 3) * 32 + lane;
   const int G = 1 << p.g_shift, b = batch_of(p, u), kv = u - b * a.n_kv;
   const int node = mb * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);
   const int n = d.y - d.x + 1;
@@ -1149,8 +1148,8 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   if (node < a.N && node < (a.count != nullptr ? a.count[b] : a.N)) {
     // parts: the end of CTA d.x, then the starts of those up to d.y
     auto part = [&](int i) { return (size_t)(2 * (d.x + i) + (i == 0 ? 1 : 0)); };
-#pragma unroll 2
-    for (int i = wp; i < n; i += kParts) {
+#pragma unroll 4
+    for (int i = wp; i < n; i += P) {
       const float2 x = parts.ml[part(i) * R + row];
       const float4* src = parts.o + (part(i) * (D / 4) + c4) * R + row;
       float4 o[Q];
@@ -1171,13 +1170,13 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
       }
     }
   }
-  if constexpr (kParts > 1) {
+  if constexpr (P > 1) {
     s_ml[warp][lane] = make_float2(M, L);
 #pragma unroll
     for (int k = 0; k < Q; ++k) s_o[warp][k][lane] = make_float4(acc[4 * k], acc[4 * k + 1], acc[4 * k + 2], acc[4 * k + 3]);
     __syncthreads();
     if (wp != 0) return;
-    for (int w = 1; w < min(kParts, n); ++w) {
+    for (int w = 1; w < min(P, n); ++w) {
       const float2 x = s_ml[warp + w][lane];
       if (x.y == 0.f) continue;
       const float mn = fmaxf(M, x.x), ref = mn == kNegInf ? 0.f : mn;
@@ -1251,17 +1250,25 @@ bool encode_4d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t n1, 
 
 template <int D, int BLOCKS>
 cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, const CUtensorMap (&tm)[5],
-                        cudaStream_t stream) {
+                        int num_sms, cudaStream_t stream) {
   constexpr int smem = smem_bytes(D, BLOCKS);
   cudaError_t e = cudaFuncSetAttribute(tree_step_kernel<D, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
                  tm[3], tm[4]);
   if (e != cudaSuccess || !p.list) return e;
-  const int items = a.batch * a.n_kv * p.mb;
-  return items >= 48
-             ? launch_pdl(tree_merge_kernel<D, 4, 2>, dim3(items, D / 8, BLOCKS), dim3(256), 0, stream, a, p, parts)
-             : launch_pdl(tree_merge_kernel<D, 1, 1>, dim3(items, D / 4 * 4, BLOCKS), dim3(256), 0, stream, a, p, parts);
+  // threads if each had 4 columns of a row: at most grid - 1 items are cut, and
+  // the GPU holds 2048 threads per SM
+  const long items = (long)a.batch * a.n_kv * p.mb, units = items * BLOCKS * (D / 4) * 4;
+  const long cut = std::min<long>(items, p.grid) * BLOCKS * kTile * (D / 4), most = 2048l * num_sms;
+  const auto merge = [&](auto kernel, int P, int Q) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(units * P / Q / 8)), dim3(256), 0, stream, a, p, parts);
+  };
+  if (cut * 8 <= most) return merge(tree_merge_kernel<D, 8, 1>, 8, 1);
+  if (cut * 4 <= most) return merge(tree_merge_kernel<D, 4, 1>, 4, 1);
+  if (cut * 2 <= most) return merge(tree_merge_kernel<D, 2, 1>, 2, 1);
+  if (cut <= most) return merge(tree_merge_kernel<D, 1, 1>, 1, 1);
+  return merge(tree_merge_kernel<D, 1, 4>, 1, 4);
 }
 
 }  // namespace
@@ -1291,8 +1298,8 @@ cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sm
       !encode_4d(&tm[4], a.v, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile))
     return cudaErrorInvalidValue;
   if (D == 128)
-    return p.blocks == 2 ? launch_step<128, 2>(a, p, parts, tm, stream) : launch_step<128, 1>(a, p, parts, tm, stream);
-  return p.blocks == 2 ? launch_step<64, 2>(a, p, parts, tm, stream) : launch_step<64, 1>(a, p, parts, tm, stream);
+    return p.blocks == 2 ? launch_step<128, 2>(a, p, parts, tm, num_sms, stream) : launch_step<128, 1>(a, p, parts, tm, num_sms, stream);
+  return p.blocks == 2 ? launch_step<64, 2>(a, p, parts, tm, num_sms, stream) : launch_step<64, 1>(a, p, parts, tm, num_sms, stream);
 }
 
 }  // namespace mkv
