@@ -136,7 +136,7 @@ typedef struct {
  * has n_path or a node index out of range (MKV_ERR_INVALID_ARG), is left as it
  * is and recorded (info: batch item * h_kv + head).
  * The workspace is 256 bytes, zero-filled before its first use.  One launch
- * for every 32 layers.
+ * for every 64 layers.
  */
 MKV_API mkv_status mkv_tree_commit(mkv_geom geom, const mkv_tree* tree, int32_t n_layers,
                                    const mkv_tree_layer* layers, const int32_t* path, int32_t path_len,

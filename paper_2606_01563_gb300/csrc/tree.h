@@ -77,7 +77,7 @@ struct TreeBuildArgs {
 };
 cudaError_t launch_tree_build(const TreeBuildArgs& a, int batch, cudaStream_t stream);
 
-constexpr int kCommitLayers = 32;  // layers per launch: their pointers travel in the launch's arguments
+constexpr int kCommitLayers = 64;  // layers per launch: their pointers travel in the launch's arguments (4 KB)
 struct CommitLayer {
   void* K;
   void* V;

@@ -137,15 +137,14 @@ def lib():
         L.mkv_tree_workspace_size.restype = ctypes.c_size_t
         L.mkv_tree_workspace_size.argtypes = [mkv_geom, c_i32, c_i32]
         L.mkv_tree_step.restype = c_i32
-        L.mkv_tree_step.argtypes = [mkv_geom, ctypes.POINTER(mkv_tree), c_vp, c_vp, c_vp, ctypes.POINTER(mkv_cache),
+        L.mkv_tree_step.argtypes = [mkv_geom, c_vp, c_vp, c_vp, c_vp, ctypes.POINTER(mkv_cache),
                                     ctypes.POINTER(mkv_moments), ctypes.POINTER(mkv_decode_params), c_vp, c_vp, c_vp,
                                     ctypes.c_size_t, c_vp]
         L.mkv_tree_commit.restype = c_i32
-        L.mkv_tree_commit.argtypes = [mkv_geom, ctypes.POINTER(mkv_tree), c_i32, ctypes.POINTER(mkv_tree_layer), c_vp,
+        L.mkv_tree_commit.argtypes = [mkv_geom, c_vp, c_i32, ctypes.POINTER(mkv_tree_layer), c_vp,
                                       c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.mkv_rope.restype = c_i32
-        L.mkv_rope.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params), c_i32,
-                               ctypes.POINTER(mkv_rope_tensor), c_vp]
+        L.mkv_rope.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params), c_i32, c_vp, c_vp]
         L.mkv_debug_set_poll_limit.restype = ctypes.c_int64
         L.mkv_debug_set_poll_limit.argtypes = [ctypes.c_int64]
         L.mkv_debug_force_ticket_merge.restype = c_i32
@@ -178,6 +177,27 @@ def _stream(stream):
 def _check(code, where):
     if code != 0:
         raise MKVError(code, where)
+
+
+_BF16 = torch.bfloat16
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _int32(t, shape, what):
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 {list(shape)}")
+
+
+def _nodes(t, what):
+    """(node, batch) strides in elements of a [b, N, heads, d] bf16 tensor whose heads lie densely."""
+    _need(t.dtype is _BF16 and t.dim() == 4 and t.stride(3) == 1 and
+          (t.shape[2] == 1 or t.stride(2) == t.shape[3]), f"{what}: bf16 [b, N, heads, d] with dense heads")
+    # (a stride over an extent of one is never used: the dense value stands for it)
+    return (t.stride(1) if t.shape[1] > 1 else 0), (t.stride(0) if t.shape[0] > 1 else 0)
 
 
 # ----------------------------------------------------------------- state
@@ -215,12 +235,17 @@ class Moments:
         return mkv_moments(self.n.data_ptr(), self.mu_k.data_ptr(), self.mu_v.data_ptr(), self.C.data_ptr())
 
 
-@dataclass
 class Tree:
     """Drafted nodes (mkv_tree): mask int32 [b, N, ceil(N / 32)], the words of mkv_tree_build; count int32 [b],
-    the nodes in use (None: all N)."""
-    mask: torch.Tensor
-    count: torch.Tensor | None = None
+    the nodes in use (None: all N).  Made once per tree and given to every layer's mkv_tree_step."""
+    __slots__ = ("mask", "count", "batch", "n_nodes", "usable")
+
+    def __init__(self, mask, count=None):
+        self.mask, self.count = mask, count
+        self.batch, self.n_nodes, words = mask.shape
+        self.usable = (mask.dtype is torch.int32 and mask.is_contiguous() and words == (self.n_nodes + 31) // 32 and
+                       (count is None or (count.dtype is torch.int32 and count.shape == (self.batch,) and
+                                          count.is_contiguous())))
 
 
 @dataclass
@@ -345,39 +370,32 @@ def mkv_moments_pack_split(g, mom: Moments, tau, C_split, stream=None):
 
 
 # -------------------------------------------- speculative decoding, positions
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _nodes(t, what):
-    """(node, batch) strides in elements of a [b, N, heads, d] bf16 tensor whose heads lie densely."""
-    _need(t.dtype == torch.bfloat16 and t.dim() == 4 and t.stride(3) == 1 and
-          (t.shape[2] == 1 or t.stride(2) == t.shape[3]), f"{what}: bf16 [b, N, heads, d] with dense heads")
-    # (a stride over an extent of one is never used: the dense value stands for it)
-    return (t.stride(1) if t.shape[1] > 1 else 0), (t.stride(0) if t.shape[0] > 1 else 0)
-
-
-def _int32(t, shape, what):
-    _need(t.dtype == torch.int32 and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{what}: contiguous int32 {list(shape)}")
+# These calls are made for every layer of every step, and a tensor's attribute
+# takes 0.1 us on the host: shapes and strides are read once each, and the small
+# structures of whole 64-bit fields go out as integer arrays.
+_I64x7, _I64x9 = ctypes.c_int64 * 7, [ctypes.c_int64 * (9 * n) for n in range(5)]
 
 
 def mkv_tree_build(parents, mask, pos, ws, count=None, base=None, stream=None):
     """Visibility words and positions of drafted trees: parents int32 [b, N] -> mask int32 [b, N, ceil(N / 32)],
     pos int32 [b, N] (or None).  base: int32 [b], any stride (e.g. cache.seen[:, 0])."""
-    b, n = parents.shape
-    _int32(parents, (b, n), "parents")
+    shape = parents.shape
+    b, n = shape
+    _int32(parents, shape, "parents")
     _int32(mask, (b, n, (n + 31) // 32), "mask")
     if pos is not None:
-        _int32(pos, (b, n), "pos")
+        _int32(pos, shape, "pos")
     if count is not None:
         _int32(count, (b,), "count")
+    at, step = None, 0
     if base is not None:
-        _need(base.dtype == torch.int32 and tuple(base.shape) == (b,), "base: int32 [b]")
-    code = lib().mkv_tree_build(b, n, _ptr(parents), _ptr(count), _ptr(base), 0 if base is None else base.stride(0),
-                                _ptr(mask), _ptr(pos), _ptr(ws), ws.numel(), _stream(stream))
-    _check(code, "mkv_tree_build")
+        if base.dtype is not torch.int32 or base.shape != (b,):
+            raise ValueError("base: int32 [b]")
+        at, step = base.data_ptr(), base.stride(0)
+    code = lib().mkv_tree_build(b, n, parents.data_ptr(), _ptr(count), at, step, mask.data_ptr(), _ptr(pos),
+                                ws.data_ptr(), ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_tree_build")
 
 
 def mkv_tree_workspace_size(g, n_nodes, capacity):
@@ -389,23 +407,28 @@ def mkv_tree_step(g, tree: Tree, q, k, v, cache: Cache, mom: Moments | None, p: 
     """Attention of drafted nodes over the cache, the nodes they see and the moments: q bf16 [b, N, g*h_kv, d],
     k and v bf16 [b, N, h_kv, d] (nodes and batch items may be strided), out bf16 [b, N, g*h_kv, d], lse fp32
     [b, N, g*h_kv] or None."""
-    b, n = tree.mask.shape[:2]
-    heads, d = g.group * g.n_kv_heads, g.head_dim
-    _int32(tree.mask, (g.batch, n, (n + 31) // 32), "mask")
-    if tree.count is not None:
-        _int32(tree.count, (b,), "count")
-    _need(tuple(q.shape) == (b, n, heads, d), "q: [b, N, g*h_kv, d]")
-    _need(tuple(k.shape) == (b, n, g.n_kv_heads, d) and k.shape == v.shape, "k, v: [b, N, h_kv, d]")
-    _need(out.dtype == torch.bfloat16 and tuple(out.shape) == (b, n, heads, d) and out.is_contiguous(),
-          "out: contiguous bf16 [b, N, g*h_kv, d]")
-    _need(lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (b, n, heads) and lse.is_contiguous()),
-          "lse: contiguous float32 [b, N, g*h_kv]")
-    kv = _nodes(k, "k")
-    _need(kv == _nodes(v, "v"), "k and v: the same strides")
-    t = mkv_tree(n, _ptr(tree.count), _ptr(tree.mask), *_nodes(q, "q"), *kv)
-    code = lib().mkv_tree_step(g, t, _ptr(q), _ptr(k), _ptr(v), cache.c(), mom.c() if mom is not None else None, p,
-                               _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream))
-    _check(code, "mkv_tree_step")
+    b, n, h, d = tree.batch, tree.n_nodes, g.n_kv_heads, g.head_dim
+    heads = g.group * h
+    if not tree.usable:
+        raise ValueError("tree: mask contiguous int32 [b, N, ceil(N / 32)], count contiguous int32 [b]")
+    want, want_kv = (b, n, heads, d), (b, n, h, d)
+    if g.batch != b or q.shape != want or out.shape != want or k.shape != want_kv or v.shape != want_kv:
+        raise ValueError("q, out: [b, N, g*h_kv, d]; k, v: [b, N, h_kv, d], of the tree's b and N")
+    qs, ks = q.stride(), k.stride()
+    if (q.dtype is not _BF16 or k.dtype is not _BF16 or v.dtype is not _BF16 or out.dtype is not _BF16
+            or v.stride() != ks or not out.is_contiguous() or qs[3] != 1 or ks[3] != 1
+            or (heads > 1 and qs[2] != d) or (h > 1 and ks[2] != d)):
+        raise ValueError("q, k, v, out: bf16 with dense heads, k and v of the same strides, out contiguous")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (b, n, heads) or not lse.is_contiguous()):
+        raise ValueError("lse: contiguous float32 [b, N, g*h_kv]")
+    # (a stride over an extent of one is never used: 0, the dense value, stands for it)
+    t = _I64x7(n, 0 if tree.count is None else tree.count.data_ptr(), tree.mask.data_ptr(), qs[1] if n > 1 else 0,
+               qs[0] if b > 1 else 0, ks[1] if n > 1 else 0, ks[0] if b > 1 else 0)
+    code = lib().mkv_tree_step(g, t, q.data_ptr(), k.data_ptr(), v.data_ptr(), cache.c(),
+                               None if mom is None else mom.c(), p, out.data_ptr(), _ptr(lse), ws.data_ptr(),
+                               ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_tree_step")
 
 
 def tree_layers(layers):
@@ -427,9 +450,10 @@ def mkv_tree_commit(g, layers: TreeLayers, path, n_path, ws, stream=None):
     _int32(n_path, (g.batch,), "n_path")
     _need(layers.batch == g.batch and layers.held[0][1].shape[2:] == (g.n_kv_heads, g.head_dim),
           "layers: k and v of this geometry")
-    code = lib().mkv_tree_commit(g, layers.tree, len(layers.array), layers.array, _ptr(path), path.shape[1],
-                                 _ptr(n_path), _ptr(ws), ws.numel(), _stream(stream))
-    _check(code, "mkv_tree_commit")
+    code = lib().mkv_tree_commit(g, ctypes.byref(layers.tree), len(layers.array), layers.array, path.data_ptr(),
+                                 path.shape[1], n_path.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_tree_commit")
 
 
 def rope_params(inv_freq, axis=None, neighbours=False):
@@ -445,22 +469,30 @@ def mkv_rope(pos, p: mkv_rope_params, tensors, inverse=False, stream=None):
     """Rotates (in, out) pairs of bf16 [b, tokens, heads, d] tensors (any strides with adjacent dims; out may be in)
     by int32 positions pos [axes, b, tokens] (adjacent tokens; expanded axes and batches are fine).  inverse: by
     the negative angle."""
-    _need(pos.dtype == torch.int32 and pos.dim() == 3 and pos.shape[0] >= p.n_axes and
-          (pos.stride(2) == 1 or pos.shape[2] <= 1), "pos: int32 [axes, b, tokens] with adjacent tokens")
-    _, b, t = pos.shape
+    axes, b, t = pos.shape
+    ps = pos.stride()
+    if pos.dtype is not torch.int32 or axes < p.n_axes or (ps[2] != 1 and t > 1):
+        raise ValueError("pos: int32 [axes, b, tokens] with adjacent tokens")
+    if not 0 < len(tensors) < 5:
+        raise ValueError("tensors: one to four (in, out) pairs")
     d = tensors[0][0].shape[3]
-    arr = (mkv_rope_tensor * len(tensors))()
-    for i, (x, y) in enumerate(tensors):
-        _need(x.dtype == y.dtype == torch.bfloat16 and x.shape == y.shape and x.dim() == 4 and
-              (x.shape[0], x.shape[1], x.shape[3]) == (b, t, d) and x.stride(3) == y.stride(3) == 1,
-              "tensors: pairs of bf16 [b, tokens, heads, d] with adjacent dims")
-        # (a stride over an extent of one is never used)
-        strides = [s if n > 1 else 0 for u in (x, y) for s, n in zip(u.stride()[:3], x.shape)]
-        arr[i] = mkv_rope_tensor(x.data_ptr(), y.data_ptr(), x.shape[2], *strides)
-    q = mkv_rope_params.from_buffer_copy(p)
-    q.inverse = int(inverse)
-    code = lib().mkv_rope(b, t, d, _ptr(pos), pos.stride(0), pos.stride(1) if b > 1 else 0, q, len(tensors), arr, _stream(stream))
-    _check(code, "mkv_rope")
+    flat = []
+    for x, y in tensors:
+        shape, xs, ys = x.shape, x.stride(), y.stride()
+        h = shape[2]
+        if (x.dtype is not _BF16 or y.dtype is not _BF16 or shape != (b, t, h, d) or y.shape != shape or xs[3] != 1
+                or ys[3] != 1):
+            raise ValueError("tensors: pairs of bf16 [b, tokens, heads, d] with adjacent dims")
+        if b == 1 or t == 1 or h == 1:  # (a stride over an extent of one is never used)
+            xs, ys = ([s if e > 1 else 0 for s, e in zip(u, shape)] for u in (xs, ys))
+        flat += (x.data_ptr(), y.data_ptr(), h, xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
+    if inverse != p.inverse:
+        p = mkv_rope_params.from_buffer_copy(p)
+        p.inverse = int(inverse)
+    code = lib().mkv_rope(b, t, d, pos.data_ptr(), ps[0], ps[1] if b > 1 else 0, p, len(tensors),
+                          _I64x9[len(tensors)](*flat), _stream(stream))
+    if code:
+        _check(code, "mkv_rope")
 
 
 def mkv_debug_set_poll_limit(polls):
