@@ -32,8 +32,7 @@
 // with V and its next S, so that one group's softmax runs beside the other's
 // products (one thread for both groups: its own instructions, some 10 cycles
 // each, left the tensor cores idle between the batches); warps 12-15 turn C'
-// into operands, in the ring's next free slots, while the last tiles are
-// worked on.  Code that runs once per item is kept in loops: unrolled, it
+// into operands, in slots of the ring, while the last tiles are worked on.  Code that runs once per item is kept in loops: unrolled, it
 // waited for its own instructions (a masked tile took 9000 cycles instead of
 // 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
 // 128 columns each, and O of the two, D columns each.
@@ -275,8 +274,14 @@ struct Segment {
   int unit, mb, first;  // first node of the item's rows
   int begin, end, tiles;
   int k0, k1;  // key tiles: the cache's, then the nodes'
+  // Ring: K and V of every key tile, and before the last one or two tiles the
+  // operands of C' (0 to 2 slots), so that they are made while those tiles run.
+  int c_slots, c_tile;
   Item it;
   bool live, mom;  // rows in use; the moment term belongs to this segment
+  __device__ __forceinline__ int slot(int j) const { return 2 * (j - k0) + (j >= c_tile ? c_slots : 0); }  // of K
+  __device__ __forceinline__ int c_slot() const { return 2 * (c_tile - k0); }
+  __device__ __forceinline__ int slots() const { return 2 * (k1 - k0) + c_slots; }
   // keys in use of key tile j
   __device__ __forceinline__ int valid(int j) const {
     return min(kTile, (j < it.cache ? it.len : it.count + it.cache * kTile) - j * kTile);
@@ -300,6 +305,8 @@ struct Walk {
     s.mom = s.live && s.end == s.tiles && s.it.tail > 0 && s.it.n_e > 0;
     s.k0 = min(s.begin, keys);
     s.k1 = min(s.end, keys);
+    s.c_slots = s.mom && a.order == 1 ? (a.C16 != nullptr ? 1 : 2) : 0;
+    s.c_tile = max(s.k0, s.k1 - (p.blocks == 1 ? 2 : 1));
     left -= s.end - s.begin;
     t = 0;
     if (++mb == p.mb) {
@@ -501,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (ok && walk.next(a, p, s)) {
         if (!s.mom && s.k1 == s.k0) continue;
         const int b = batch_of(p, s.unit), kv = s.unit - b * a.n_kv;
-        if (s.mom && a.order == 1) {  // C' is read when slots are free: into L2 now
+        if (s.c_slots > 0) {  // C' is read when slots are free: into L2 now
           const size_t at = (size_t)s.unit * D * D;
           const void* c = a.C16 != nullptr ? static_cast<const void*>(a.C16 + at)
                           : a.Cs != nullptr ? static_cast<const void*>(a.Cs + at / 2)
@@ -515,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // Q as soon as it may be replaced, but after the first tile at the
           // latest; before what precedes this launch is done, only the cache's
           // tiles, as many as the ring holds
-          if (q_due && (!waited ? (!cache || j == s.k1 || seq + 2 > NS)
+          if (q_due && (!waited ? (!cache || j == s.k1 || j == s.c_tile || seq + 2 > NS)
                                 : (j != s.k0 || j == s.k1 || nq == 0 || mbar_try_wait(&sh.q_empty, (nq - 1) & 1)))) {
             wait_prior();
             if (nq > 0 && !pwait(&sh.q_empty, (nq - 1) & 1, sh, a)) {
@@ -529,6 +536,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                             &sh.q_full);
             sh.q_issued = ++nq;
             q_due = false;
+          }
+          if (j == s.c_tile && s.c_slots > 0) {
+            for (int k = 0; ok && k < s.c_slots; ++k) {
+              const int i = slot();
+              if (!ok) break;
+              mbar_arrive(&sh.full[i]);
+              sh.issued = ++seq;
+            }
+            if (!ok) break;
+            mbar_arrive(&sh.c_grant);
           }
           if (j == s.k1) break;
 #pragma unroll 1
@@ -545,16 +562,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             sh.issued = ++seq;
           }
-        }
-        if (s.mom && a.order == 1) {  // C' goes into the next slots
-          const int n = a.C16 != nullptr ? 1 : 2;
-          for (int j = 0; ok && j < n; ++j) {
-            const int i = slot();
-            if (!ok) break;
-            mbar_arrive(&sh.full[i]);
-            sh.issued = ++seq;
-          }
-          if (ok) mbar_arrive(&sh.c_grant);
         }
       }
       wait_prior();
@@ -593,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         f_read = false;
         int t = k0 + (BLOCKS == 2 ? 0 : g);
-        int i = seq + 2 * (t - k0);  // slot and phase of the K tile; V is in the next slot
+        int i = seq + s.slot(t);  // slot and phase of the K tile; V is in the next slot
         uint32_t ph = (i / NS) & 1;
         i %= NS;
         uint32_t add = 0;
@@ -606,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         while (ok && t < k1) {
           const int steps = n16 >> 4;
-          int vi = i + 1, ni = i + kStep;
+          int vi = i + 1, ni = i + s.slot(t + kStep / 2) - s.slot(t);
           uint32_t vph = ph, nph = ph;
           if (vi >= NS) vi -= NS, vph ^= 1;
           if (ni >= NS) ni -= NS, nph ^= 1;
@@ -638,9 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           i = ni, ph = nph;
         }
-        seq += 2 * (k1 - k0);
-        if (ok && s.mom && a.order == 1) {  // the moment term's value, Q C'^T, in the place of S
-          const int n = a.C16 != nullptr ? 1 : 2;
+        if (ok && s.c_slots > 0) {  // the moment term's value, Q C'^T, in the place of S
           if (reads_c) {
             ok = pwait(&sh.c_full, cph, sh, a);
             cph ^= 1;
@@ -648,19 +653,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
             constexpr uint32_t id = idesc_bf16(128, D, 0, 0);
 #pragma unroll 1
-            for (int j = 0; j < n; ++j) {
-              const int ci = (seq + j) % NS;
+            for (int j = 0; j < s.c_slots; ++j) {
+              const int ci = (seq + s.c_slot() + j) % NS;
               const uint64_t db = dR + ci * (kSlot >> 4);
-#pragma unroll 1
+#pragma unroll
               for (int kk = 0; kk < D / 16; ++kk)
                 umma_bf16(tP, dQ + (kk >> 2) * (kBox >> 4) + (kk & 3) * 2, db + (kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2,
                           id, (j > 0 || kk > 0) ? 1u : 0u);
               umma_commit(&sh.empty[ci]);
             }
           }
-          seq += n;
           f_read = true;
         }
+        seq += s.slots();
         umma_commit(&sh.q_empty);
         umma_commit(&sh.o_full);
       }
@@ -673,12 +678,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t seq = 0, cph = 0;
     while (walk.next(a, p, s)) {
       if (!s.mom && s.k0 == s.k1) continue;
-      seq += 2 * (s.k1 - s.k0);
-      if (!s.mom || a.order != 1) continue;
+      const uint32_t c_seq = seq + s.c_slot();
+      seq += s.slots();
+      if (s.c_slots == 0) continue;
       const float nf = static_cast<float>(s.it.n_e);
-      uint8_t* hi = ring + (seq % NS) * kSlot;
-      uint8_t* lo = ring + ((seq + 1) % NS) * kSlot;
-      seq += a.C16 != nullptr ? 1 : 2;
+      uint8_t* hi = ring + (c_seq % NS) * kSlot;
+      uint8_t* lo = ring + ((c_seq + 1) % NS) * kSlot;
       const size_t base = (size_t)s.unit * D * D;
 #pragma unroll 1
       for (int k = 0; k < kRounds; ++k) {
@@ -739,6 +744,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tS = tm + lanes + cS + g * 128, tO = tm + lanes + cO + g * D;
     const float scale = rsqrtf(static_cast<float>(D)), qs = scale * kLog2e;
     const int G = 1 << p.g_shift, HQ = a.n_kv << p.g_shift;
+    constexpr int kCols = BLOCKS == 2 ? D : D / 2;  // columns of the output that a thread writes, from c_lo on
+    const int c_lo = BLOCKS == 2 ? 0 : g * (D / 2);
     uint32_t nq = 0, ns = 0, no = 0, vseq = 0;  // phases passed; ring slots of the segments before
     uint32_t tph = 0;
     const bool aligned_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
@@ -754,9 +761,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool mine = BLOCKS == 2 || g == 0;  // the moment term counts in this group's state
       float m = kNegInf, l = 0.f, e = kNegInf;
       bool filled = false;  // O holds something
+      float mv[kCols / 32] = {};  // mu_v: this lane's columns of those that the thread writes
       if (mom) {
         if (tid < D) sh.mu_k[tid] = a.mu_k[(size_t)s.unit * D + tid];
-        if (tid < D / 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.mu_v + (size_t)s.unit * D + tid * 32));
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k) mv[k] = a.mu_v[(size_t)s.unit * D + c_lo + k * 32 + lane];
         named_sync(1, 256);
         (void)pwait(&sh.q_full, nq & 1, sh, a);
         if (mine) {
@@ -787,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(&sh.q_empty);  // (with the MMA threads' commits: Q may be replaced)
       }
       const uint32_t seg_seq = vseq;  // of the first K tile
-      vseq += 2 * (k1 - k0) + (mom && a.order == 1 ? (a.C16 != nullptr ? 1 : 2) : 0);
+      vseq += s.slots();
       // The groups take turns at the exponentials: left to themselves they fell
       // into step, and both waited for the special-function units and then for
       // the tensor cores (4200 cycles a tile of 256 rows instead of 3000).
@@ -824,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // and so must a node's value where its weight is 0: elements that
           // are not are taken out here and reach the nodes that see them at
           // the end
-          const uint32_t sv = seg_seq + 2 * (j - k0) + 1;
+          const uint32_t sv = seg_seq + s.slot(j) + 1;
           uint8_t* tv = ring + (sv % NS) * kSlot;
           (void)pwait(&sh.full[sv % NS], (sv / NS) & 1, sh, a);
           const int end = (valid + 15) & ~15;
@@ -1015,8 +1024,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float wf = w * scale;
       const bool put = node < a.N;
       const size_t orow = ((size_t)b * a.N + node) * HQ + (kv << p.g_shift) + h;
-      constexpr int kCols = BLOCKS == 2 ? D : D / 2;
-      const int c_lo = BLOCKS == 2 ? 0 : g * (D / 2);
       const uint32_t tA = tm + lanes + cO + (BLOCKS == 2 ? g * D : 0) + c_lo, tB = tA + D;
       const uint32_t tF = tm + lanes + cS + (BLOCKS == 2 ? g * 128 : 0) + c_lo;
 #pragma unroll 1
@@ -1039,16 +1046,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_ld();
             keep16(x), keep16(x + 16);
           }
-          const float4* mv = reinterpret_cast<const float4*>(a.mu_v + (size_t)s.unit * D + c_lo + c);
+          float m32 = mv[0];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float4 v4 = mv[i];
-            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+          for (int k = 1; k < kCols / 32; ++k)
+            if (c == 32 * k) m32 = mv[k];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              o[4 * i + k] = fmaf(v[k], w, o[4 * i + k]);
-              if (use_f) o[4 * i + k] = fmaf(__uint_as_float(x[4 * i + k]), wf, o[4 * i + k]);
-            }
+          for (int i = 0; i < 32; ++i) {
+            o[i] = fmaf(__shfl_sync(kAll, m32, i), w, o[i]);
+            if (use_f) o[i] = fmaf(__uint_as_float(x[i]), wf, o[i]);
           }
         }
         if (whole) {
@@ -1208,17 +1213,31 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
 Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   Plan p{};
   const int rows = n_nodes * g.group;
-  p.blocks = rows > kTile ? 2 : 1;
-  p.mb = (rows + p.blocks * kTile - 1) / (p.blocks * kTile);
   p.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
   p.words = tree_words(n_nodes);
   p.kv_inv = ((1ull << 40) + g.n_kv_heads - 1) / g.n_kv_heads;
-  const long units = (long)g.batch * g.n_kv_heads, items = units * p.mb;
-  const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
   p.min_run = 2;
-  p.list = units <= kScanUnits && tiles > 4 && items * tiles < (1L << 30) ? 1 : 0;
-  p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (items * tiles + p.min_run - 1) / p.min_run))
-                  : static_cast<int>(items);
+  const long units = (long)g.batch * g.n_kv_heads;
+  const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
+  const auto items = [&](int blocks) { return units * ((rows + blocks * kTile - 1) / (blocks * kTile)); };
+  // One row block per CTA spreads few, short items over more SMs; two read K and
+  // V once for 256 rows.  Measured, one and two: 4 x 8 heads, 64 nodes of 4
+  // heads, 1024 rows 21.0 and 28.3 us, 4096 rows 41.6 and 43.9; 16 x 8 heads,
+  // 512 rows 46.2 and 30.1; 8 heads, 33 nodes, 131072 rows 166 and 120.
+  p.blocks = rows > kTile && (items(1) > num_sms || items(2) * tiles >= 8l * num_sms) ? 2 : 1;
+  const long n = items(p.blocks);
+  p.mb = static_cast<int>(n / units);
+  // One CTA per item costs the tiles that even runs would save, the list its
+  // records and the merge (3 us, more with the number of items cut).  A tile
+  // takes 0.9 us with one row block.  Measured, list and whole items: 8 items of
+  // 5 tiles 13.9 and 12.4 us, of 10 14.4 and 16.8, of 18 15.3 and 23.5; 64 items
+  // of 11 21.0 and 18.5, of 19 32.4 and 26.1; 32 items of 35 28.5 and 37.5; 128
+  // items of 19 63.5 and 49.1; more items than SMs: 256 of 10 45.2 and 36.0, 320
+  // of 18 75.9 and 89.0, 512 of 18 73.4 and 81.0.
+  const long run = std::max<long>(p.min_run, n * tiles / num_sms);
+  const bool whole = n <= num_sms ? tiles - run <= 3 + n / 5 : tiles <= 12;
+  p.list = units <= kScanUnits && n * tiles < (1L << 30) && !whole ? 1 : 0;
+  p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (n * tiles + p.min_run - 1) / p.min_run)) : static_cast<int>(n);
   return p;
 }
 
