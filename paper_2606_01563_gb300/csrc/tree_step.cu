@@ -16,7 +16,9 @@
 // and with 8 some row of a warp moved in most tiles of a long cache (700
 // cycles each).  P enters
 // the second product rounded to bf16 (2^-8 relative, the output's own
-// rounding); l is summed from the unrounded weights.
+// rounding); l is summed from the unrounded weights, and O is scaled by the
+// ratio of that sum to the rounded weights' (where a few weights dominate,
+// their roundings then cancel: error against 64 bits 0.0023 without it).
 //
 // Work.  The tiles of all (unit, row block) items form one list that is cut
 // into equal runs, one per CTA, wherever the run ends; an item cut by a
@@ -759,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = node < s.it.count;
       const bool warp_live = __any_sync(kAll, live);
       const bool mine = BLOCKS == 2 || g == 0;  // the moment term counts in this group's state
-      float m = kNegInf, l = 0.f, e = kNegInf;
+      float m = kNegInf, l = 0.f, lr = 0.f, e = kNegInf;  // lr: the sum of the rounded weights
       bool filled = false;  // O holds something
       float mv[kCols / 32] = {};  // mu_v: this lane's columns of those that the thread writes
       if (mom) {
@@ -787,7 +789,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           e = fmaf(e0 + e1, qs, log2f(static_cast<float>(s.it.n_e)));
           m = ceilf(e);
-          l = fast_exp2(e - m);  // (a NaN passes on)
+          l = lr = fast_exp2(e - m);  // (a NaN passes on)
         }
       }
       if (active) {
@@ -883,12 +885,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float mn = fmaxf(m, ceilf(top));
             const float f = m == kNegInf ? 1.f : pow2(m - mn);
             m = mn;
-            l *= f;
+            l *= f, lr *= f;
             if (filled) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
           }
           const float ref = m == kNegInf ? 0.f : m;
           const uint64_t qs2 = pair(qs, qs), nref = pair(-ref, -ref);
-          uint64_t sum2[2] = {0, 0};
+          uint64_t sum2[2] = {0, 0}, sumr2[2] = {0, 0};
           uint32_t y[4][32];
           tmem_ld32_async(tS, y[0]);
 #pragma unroll
@@ -901,14 +903,19 @@ __global__ void __launch_bounds__(kThreads, 1)
               float t0, t1;
               unpair(fma2(pair(__uint_as_float(y[c][i]), __uint_as_float(y[c][i + 1])), qs2, nref), t0, t1);
               const float p0 = fast_exp2(t0), p1 = fast_exp2(t1);
+              const uint32_t pr = pack_bf16x2(p0, p1);
               sum2[(i >> 1) & 1] = add2(sum2[(i >> 1) & 1], pair(p0, p1));
-              y[c][i >> 1] = pack_bf16x2(p0, p1);
+              sumr2[(i >> 1) & 1] =
+                  add2(sumr2[(i >> 1) & 1], pair(__uint_as_float(pr << 16), __uint_as_float(pr & 0xffff0000u)));
+              y[c][i >> 1] = pr;
             }
             tmem_st16(tS + c * 16, y[c]);
           }
           float lo, hi;
           unpair(add2(sum2[0], sum2[1]), lo, hi);
           l += lo + hi;
+          unpair(add2(sumr2[0], sumr2[1]), lo, hi);
+          lr += lo + hi;
           tmem_wait_st();
         } else if (warp_live) {
           // 32 columns at a time; a reference that has to move (by a whole
@@ -916,9 +923,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           // written of this tile along.  (P's columns lie below those of S that
           // are still to be read.)
           const uint64_t qs2 = pair(qs, qs);
-          uint64_t sum2[2] = {0, 0};
 #pragma unroll 1
           for (int c = 0; c * 32 < valid; ++c) {
+            uint64_t sum2 = 0, sumr2 = 0;
             uint32_t x[32];
             tmem_ld32_async(tS + c * 32, x);
             const uint32_t word = c == 0 ? words[0] : c == 1 ? words[1] : c == 2 ? words[2] : words[3];
@@ -938,10 +945,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float mn = fmaxf(m, ceilf(top));
               const float f = m == kNegInf ? 1.f : pow2(m - mn);
               m = mn;
-              float lo, hi;
-              unpair(add2(sum2[0], sum2[1]), lo, hi);
-              l = (l + lo + hi) * f;
-              sum2[0] = sum2[1] = 0;
+              l *= f, lr *= f;
               if (filled) scale_columns<D>(tO, f);  // (S of this tile is complete, so every product into O is)
               scale_weights(tS, c, f);
             }
@@ -952,14 +956,18 @@ __global__ void __launch_bounds__(kThreads, 1)
               float t0, t1;
               unpair(fma2(pair(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), qs2, nref), t0, t1);
               const float p0 = fast_exp2(t0), p1 = fast_exp2(t1);
-              sum2[(i >> 1) & 1] = add2(sum2[(i >> 1) & 1], pair(p0, p1));
-              x[i >> 1] = pack_bf16x2(p0, p1);
+              const uint32_t pr = pack_bf16x2(p0, p1);
+              sum2 = add2(sum2, pair(p0, p1));
+              sumr2 = add2(sumr2, pair(__uint_as_float(pr << 16), __uint_as_float(pr & 0xffff0000u)));
+              x[i >> 1] = pr;
             }
             tmem_st16(tS + c * 16, x);
+            float lo, hi;
+            unpair(sum2, lo, hi);
+            l += lo + hi;
+            unpair(sumr2, lo, hi);
+            lr += lo + hi;
           }
-          float lo, hi;
-          unpair(add2(sum2[0], sum2[1]), lo, hi);
-          l += lo + hi;
           tmem_wait_st();
         }
         filled = true;
@@ -987,7 +995,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int part = 2 * blockIdx.x + (s.begin == 0 ? 1 : 0);  // an item's start: this CTA's last segment; else its first
       constexpr int R = BLOCKS * kTile;
       bool any_odd = false;
-      if (BLOCKS == 1 && g == 1) sh.ml[r] = make_float2(m, l);
+      const float even = lr != 0.f ? l / lr : 1.f;  // what O lacks for the weights' roundings
+      if (BLOCKS == 1 && g == 1) {
+        sh.ml[r] = make_float2(m, l);
+        if (k1 > k0 + 1) sh.w[r] = even;  // (group 0 is past its use of mu_k: it has taken a turn)
+      }
       named_sync(1, 256);  // the other group's state; the nodes' odd values are known
       auto seen_odd = [&](int w) {
         return w < p.words ? sh.odd[seg & 1][w] & a.mask[((size_t)b * a.N + node) * p.words + w] : 0u;
@@ -997,7 +1009,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 8; ++i) any_odd |= sh.odd[seg & 1][i] != 0;
       }
       // output = f0 O_0 + f1 O_1 + w (mu_v + scale F) over the columns this thread writes
-      float M = m, L = l, f0 = L != 0.f ? 1.f : 0.f, f1 = 0.f;
+      float M = m, L = l, f0 = L != 0.f ? even : 0.f, f1 = 0.f;
       if (BLOCKS == 1 && g == 0) {
         const float2 y = sh.ml[r];
         M = fmaxf(L != 0.f ? m : kNegInf, y.y != 0.f ? y.x : kNegInf);
@@ -1005,8 +1017,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         f0 = L != 0.f ? fast_exp2(m - ref) : 0.f;
         f1 = y.y != 0.f ? fast_exp2(y.x - ref) : 0.f;
         L = (L != 0.f ? L * f0 : 0.f) + (y.y != 0.f ? y.y * f1 : 0.f);
+        f0 *= even;
+        if (k1 > k0 + 1) f1 *= sh.w[r];
       }
-      float w = mom && mine ? fast_exp2(e - M) : 0.f;
+      float w = mom && mine ? fast_exp2(e - M) * even : 0.f;
       if (whole) {
         const float inv = L != 0.f ? 1.f / L : 0.f;
         f0 *= inv, f1 *= inv, w *= inv;
