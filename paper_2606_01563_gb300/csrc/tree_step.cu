@@ -90,7 +90,7 @@ struct Raw {  // a unit's sizes as read
 
 struct Shared {
   uint64_t full[kMaxSlots], empty[kMaxSlots];
-  uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], turn[2], o_full, mma_done;
+  uint64_t q_full, q_empty, c_grant, c_full, s_full[2], p_ready[2], turn[2], p_half[2], o_full, mma_done;
   uint32_t tmem;
   int32_t abort, issued, q_issued;
   int32_t unit, mb, t0, start, end;  // the CTA's run of the list: first item, tile in it, the list's tiles [start, end)
@@ -448,6 +448,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                      const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const __grid_constant__ CUtensorMap tmKt, const __grid_constant__ CUtensorMap tmVt) {
   constexpr int kSlot = slot_bytes(D), NS = ring_slots(D, BLOCKS), BX = D / 64;
+  // With two row blocks P is handed over in halves, so that its product with V
+  // starts during the second half's exponentials (131072 rows, 256-row blocks:
+  // 129 -> 118 us; with one block, where the ring is the limit, 2% slower).
+  constexpr bool kHalf = BLOCKS == 2;
   constexpr uint32_t cS = 0, cO = 256;  // TMEM columns: S / P of group s at 128 s, O at 256 + D s
   extern __shared__ __align__(1024) uint8_t smraw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
@@ -470,6 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&sh.s_full[tid - 32], 1);
     mbar_init(&sh.p_ready[tid - 32], 4);
     mbar_init(&sh.turn[tid - 32], 4);
+    mbar_init(&sh.p_half[tid - 32], 4);
   } else if (tid == 64) {
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_empty, 2 + 8);
@@ -578,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t idS = idesc_bf16(128, kTile, 0, 0), idP = idesc_bf16(128, D, 0, 1);
       constexpr int kStep = BLOCKS == 2 ? 2 : 4;  // ring slots from one K tile of this group to the next
       int seq = 0;                                // ring slots of the segments before
-      uint32_t qph = 0, cph = 0, pph = 0;
+      uint32_t qph = 0, cph = 0, pph = 0, f_ph = 0;  // (with halves: pph is p_half's, f_ph p_ready's)
       bool ok = true, f_read = false;
       // S = Q K^T of the tile in slot i (n16 keys)
       auto issue_s = [&](int i, int n16) {
@@ -597,8 +602,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = pwait(&sh.q_full, qph, sh, a);
         qph ^= 1;
         if (f_read && reads_c) {  // the last segment's Q C'^T has been read
-          ok = ok && pwait(&sh.p_ready[g], pph, sh, a);
-          pph ^= 1;
+          uint32_t& ready = kHalf ? f_ph : pph;
+          ok = ok && pwait(&sh.p_ready[g], ready, sh, a);
+          ready ^= 1;
         }
         f_read = false;
         int t = k0 + (BLOCKS == 2 ? 0 : g);
@@ -625,19 +631,29 @@ __global__ void __launch_bounds__(kThreads, 1)
           // (P first: it is ready only after the slot's use before has been
           // consumed -- with one row block that is the other thread's, and a
           // phase's parity alone would not tell the two apart)
-          ok = pwait(&sh.p_ready[g], pph, sh, a) && pwait(&sh.full[vi], vph, sh, a);
-          pph ^= 1;
+          ok = pwait(kHalf ? &sh.p_half[g] : &sh.p_ready[g], pph, sh, a) && pwait(&sh.full[vi], vph, sh, a);
           if (!ok) break;
           tc_fence_after();
-          umma_bf16_ts(tO, tP, db, idP, add);
-          add = 1;
+          if (steps == 8) {
+            umma_bf16_ts(tO, tP, db, idP, add);
+#pragma unroll
+            for (int kk = 1; kk < 4; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
+          }
+          if (kHalf) {
+            ok = pwait(&sh.p_ready[g], f_ph, sh, a);
+            f_ph ^= 1;
+            if (!ok) break;
+            tc_fence_after();
+          }
+          pph ^= 1;
           if (steps == 8) {
 #pragma unroll
-            for (int kk = 1; kk < 8; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
+            for (int kk = 4; kk < 8; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
           } else {
 #pragma unroll 1
-            for (int kk = 1; kk < steps; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, 1u);
+            for (int kk = 0; kk < steps; ++kk) umma_bf16_ts(tO, tP + kk * 8, db + kk * 128, idP, kk == 0 ? add : 1u);
           }
+          add = 1;
           umma_commit(&sh.empty[vi]);
           if (n16 > 0) {
             ok = pwait(&sh.full[ni], nph, sh, a);
@@ -910,6 +926,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               y[c][i >> 1] = pr;
             }
             tmem_st16(tS + c * 16, y[c]);
+            if (kHalf && c == 1) {  // the first half of the product with V may begin
+              tmem_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.p_half[g]);
+            }
           }
           float lo, hi;
           unpair(add2(sum2[0], sum2[1]), lo, hi);
@@ -974,6 +996,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
+          if (kHalf && (!warp_live || tree || valid < kTile)) mbar_arrive(&sh.p_half[g]);
           mbar_arrive(&sh.p_ready[g]);
           mbar_arrive(&sh.turn[g ^ 1]);
         }
