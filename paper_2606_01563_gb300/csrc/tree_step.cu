@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kWarpTma) {
     if (lane == 0) {  // ---- TMA
-      int seq = 0, nq = 0;
+      int seq = 0, nq = 0, c_last = -1;  // c_last: the last slot given to C'
       bool ok = true, waited = !a.early;
       const uint64_t pol = l2_evict_first();
       auto wait_prior = [&] {
@@ -545,6 +545,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             q_due = false;
           }
           if (j == s.c_tile && s.c_slots > 0) {
+            // one C' at a time: the phases of c_grant and c_full do not tell one
+            // from the next but one (a slot used again since has been waited for)
+            if (c_last >= 0 && seq <= c_last + NS && !pwait(&sh.empty[c_last % NS], (c_last / NS) & 1, sh, a)) {
+              ok = false;
+              break;
+            }
             for (int k = 0; ok && k < s.c_slots; ++k) {
               const int i = slot();
               if (!ok) break;
@@ -552,6 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               sh.issued = ++seq;
             }
             if (!ok) break;
+            c_last = seq - 1;
             mbar_arrive(&sh.c_grant);
           }
           if (j == s.k1) break;

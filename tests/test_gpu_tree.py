@@ -334,3 +334,72 @@ def test_corrupt_lengths_and_counts_are_recorded():
     c.tree.count[1] = 5
     c.step()
     c.check()
+
+
+@pytest.mark.parametrize("rows,b,h,n", [(300, 1, 2, 9), (9000, 1, 2, 20), (2000, 2, 2, 100), (700, 30, 8, 40)])
+def test_waits_that_run_out_are_reported_and_leave_the_context_usable(rows, b, h, n):
+    """One item per CTA, the list of tiles with its merge, two row blocks, many items: with the poll limit at zero the
+    first wait of every CTA gives up, and the same call is right again afterwards."""
+    c = Case(rows, b=b, h=h, n=n, rows=rows, c="f32").device()
+    default = mkv.mkv_debug_set_poll_limit(0)
+    try:
+        c.step()
+        assert mkv.mkv_get_device_error(c.ws)[0] == 5
+    finally:
+        assert mkv.mkv_debug_set_poll_limit(default) == 0
+    for _ in range(2):
+        c.step()
+    c.check()
+
+
+@pytest.mark.parametrize("b,h,g,d,n,rows,c", [
+    (1, 8, 4, 128, 33, 4200, "none"), (1, 8, 4, 128, 64, 9000, "f32"), (2, 5, 8, 64, 70, 3000, "split"),
+    (1, 3, 1, 128, 256, 2500, "bf16"), (20, 8, 2, 64, 12, 2000, "f32"), (1, 1, 8, 128, 256, 700, "f32"),
+    (3, 8, 4, 128, 40, 1500, "f32"), (25, 8, 4, 64, 40, 1300, "none")])
+def test_every_plan(b, h, g, d, n, rows, c):
+    """Whole items and lists, one and two row blocks, few items of many parts and many of few, several items in a
+    CTA's run; unequal lengths and counts."""
+    Case(rows + n, b=b, h=h, g=g, d=d, n=n, rows=rows, c=c, ragged=True).run()
+
+
+def test_one_long_item_among_short_ones():
+    """The list cuts the long item into many parts; the others are whole."""
+    c = Case(77, b=12, h=2, g=2, d=128, n=6, rows=6000, c="f32")
+    c.length[:] = 40
+    c.length[5, 1] = 6000
+    c.K[:, :, 40:] = np.where((np.arange(12)[:, None] == 5)[..., None, None] & (np.arange(2)[None, :] == 1)[..., None, None],
+                              c.K[:, :, 40:], np.nan)
+    c.V[:, :, 40:] = np.where(np.isnan(c.K[:, :, 40:]), np.nan, c.V[:, :, 40:])
+    c.run()
+
+
+def test_rows_that_see_nothing_in_a_cut_item():
+    """Nodes that are not in use and nodes without a bit, in items that several CTAs share."""
+    c = Case(78, b=1, h=2, n=50, rows=6000, c="none", masks="none")
+    c.length[0, 1] = 0  # the second head's nodes see nothing at all
+    c.K[0, 1], c.V[0, 1] = np.nan, np.nan
+    c.count[0] = 41
+    c.sees = [[[] for _ in range(50)]]
+    c.run()
+
+
+def test_units_beyond_the_list():
+    """More than 4096 units: one item per CTA whatever their lengths."""
+    c = Case(79, b=520, h=8, g=1, d=64, n=2, rows=24, c="none", ragged=True)
+    c.run()
+
+
+@pytest.mark.parametrize("c", ["none", "f32", "bf16", "split"])
+@pytest.mark.parametrize("d,g,n", [(64, 4, 9), (128, 4, 9), (64, 8, 40), (128, 8, 40)])
+def test_short_items_in_a_list(d, g, n, c):
+    """Runs of many items of one to four tiles, as a long capacity with short contents has them: what is asked for
+    ahead (tiles, the moment matrices' slots, the next queries) crosses item after item."""
+    case = Case(d + n, b=30, h=8, g=g, d=d, n=n, rows=1700, c=c, ragged=True)
+    rng = np.random.default_rng(n)
+    case.length[:] = rng.choice([0, 1, 100, 128, 129, 300], size=case.length.shape)
+    case.count[::5] = rng.integers(0, n + 1, size=case.count[::5].shape)
+    case.sees = [[[a for a in row if a < m] for row in rows_] for rows_, m in zip(case.sees, case.count.tolist())]
+    case.device()
+    for _ in range(3):
+        case.step()
+    case.check()
