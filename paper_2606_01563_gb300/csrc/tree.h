@@ -116,7 +116,6 @@ struct RopeArgs {
   RopeTensor x[MKV_ROPE_MAX_TENSORS];
   const int32_t* pos;
   int64_t pos_axis, pos_batch;
-  int32_t n_tensors;
   int32_t heads;  // of all tensors
   int32_t batch;
   int32_t tokens;

@@ -201,7 +201,6 @@ mkv_status mkv_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32
   a.pos = pos;
   a.pos_axis = pos_axis;
   a.pos_batch = pos_batch;
-  a.n_tensors = n_tensors;
   a.heads = static_cast<int32_t>(heads);
   a.batch = batch;
   a.tokens = tokens;
