@@ -22,8 +22,8 @@ extern "C" {
 
 /*
  * Poll limit of the kernels' pipeline waits (tile copies and tensor-core
- * commits in mkv_compress and mkv_decode_step / mkv_decode_evict_step /
- * mkv_decode_step_noalloc).  polls < 0 restores the default (over a second
+ * commits in mkv_compress, mkv_decode_step / mkv_decode_evict_step /
+ * mkv_decode_step_noalloc and mkv_tree_step).  polls < 0 restores the default (over a second
  * of polling); polls = 0 makes the first such wait of every CTA give up at
  * once, so the call records MKV_ERR_TIMEOUT and its outputs are undefined.
  * The eviction kernels have no such waits (their CTAs synchronise through

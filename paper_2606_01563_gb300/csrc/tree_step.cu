@@ -320,7 +320,8 @@ struct Walk {
     t = 0;
     if (++mb == p.mb) {
       mb = 0;
-      ++unit;
+      // (lengths written while the call runs cannot lead past the last unit)
+      if (++unit == a.batch * a.n_kv) left = 0;
     }
     if (left > 0) raw = load_raw(a, p, unit);
     return true;
@@ -1026,7 +1027,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // An item's first part says where the others are: the last boundary that
       // stays inside it is the last at or below its tile tiles - 2.
       if (p.list && s.begin == 0 && tid == 0)
-        parts.desc[s.unit * p.mb + s.mb] = make_int2(blockIdx.x, whole ? blockIdx.x : (at + s.tiles - 2) / sh.run);
+        parts.desc[s.unit * p.mb + s.mb] = make_int2(blockIdx.x, whole ? blockIdx.x : min((at + s.tiles - 2) / sh.run, p.grid - 1));
       at += s.end - s.begin;
       const int part = 2 * blockIdx.x + (s.begin == 0 ? 1 : 0);  // an item's start: this CTA's last segment; else its first
       constexpr int R = BLOCKS * kTile;
@@ -1272,8 +1273,9 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   const auto items = [&](int blocks) { return units * ((rows + blocks * kTile - 1) / (blocks * kTile)); };
   // One row block per CTA spreads few, short items over more SMs; two read K and
   // V once for 256 rows.  Measured, one and two: 4 x 8 heads, 64 nodes of 4
-  // heads, 1024 rows 21.0 and 28.3 us, 4096 rows 41.6 and 43.9; 16 x 8 heads,
-  // 512 rows 46.2 and 30.1; 8 heads, 33 nodes, 131072 rows 166 and 120.
+  // heads, 1024 rows 19.6 and 28.2 us, 4096 rows 41.7 and 40.5; 16 x 8 heads,
+  // 512 rows 35.1 and 25.5; 8 heads, 33 nodes, 131072 rows 164 and 112; 8 x 8
+  // heads, 256 nodes, 4096 rows 203 and 165.
   p.blocks = rows > kTile && (items(1) > num_sms || items(2) * tiles >= 8l * num_sms) ? 2 : 1;
   const long n = items(p.blocks);
   p.mb = static_cast<int>(n / units);
