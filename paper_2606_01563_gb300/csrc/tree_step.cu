@@ -457,8 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                      const __grid_constant__ CUtensorMap tmKt, const __grid_constant__ CUtensorMap tmVt) {
   constexpr int kSlot = slot_bytes(D), NS = ring_slots(D, BLOCKS), BX = D / 64;
   // With two row blocks P is handed over in halves, so that its product with V
-  // starts during the second half's exponentials (131072 rows, 256-row blocks:
-  // 129 -> 118 us; with one block, where the ring is the limit, 2% slower).
+  // starts during the second half's exponentials (131072 rows: 123 us without,
+  // 112 with it; with one block, where the ring is the limit, 2% slower).
   constexpr bool kHalf = BLOCKS == 2;
   constexpr uint32_t cS = 0, cO = 256;  // TMEM columns: S / P of group s at 128 s, O at 256 + D s
   extern __shared__ __align__(1024) uint8_t smraw[];
@@ -1279,15 +1279,19 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   p.blocks = rows > kTile && (items(1) > num_sms || items(2) * tiles >= 8l * num_sms) ? 2 : 1;
   const long n = items(p.blocks);
   p.mb = static_cast<int>(n / units);
-  // One CTA per item costs the tiles that even runs would save, the list its
-  // records and the merge (3 us, more with the number of items cut).  A tile
-  // takes 0.9 us with one row block.  Measured, list and whole items: 8 items of
-  // 5 tiles 13.9 and 12.4 us, of 10 14.4 and 16.8, of 18 15.3 and 23.5; 64 items
-  // of 11 21.0 and 18.5, of 19 32.4 and 26.1; 32 items of 35 28.5 and 37.5; 128
-  // items of 19 63.5 and 49.1; more items than SMs: 256 of 10 45.2 and 36.0, 320
-  // of 18 75.9 and 89.0, 512 of 18 73.4 and 81.0.
-  const long run = std::max<long>(p.min_run, n * tiles / num_sms);
-  const bool whole = n <= num_sms ? tiles - run <= 3 + n / 5 : tiles <= 12;
+  // One CTA per item leaves SMs idle in the last wave, by the tiles that even
+  // runs would save; the list costs its records, the cut items' second ends and
+  // the merge.  A tile takes 0.9 us with one row block (1.4 where HBM bounds
+  // it).  Measured, list and whole items, (idle tiles): 8 items of 5 tiles 13.9
+  // and 11.7 us (3), of 10 14.5 and 16.7 (8), of 18 15.3 and 23.8 (16); 64 items
+  // of 10 22.0 and 19.5 (6), of 18 33.7 and 27.1 (11); 32 items of 35 29.8 and
+  // 40.0 (28); 128 items of 18 42.5 and 32.1 (3).  More items than SMs: 256 of
+  // 10 56.2 and 42.3 (4), of 34 ragged 93.5 and 89.7 (11), of 66 170 and 174
+  // (21); 512 of 18 135 and 123 (12); 320 of 18 87.9 and 89.1 (17); 192 of 34
+  // 82.5 and 92.3 (26); with two row blocks 256 of 18 105 and 93 (6), of 35 164
+  // and 163 (12), 320 of 18 122 and 131 (17).
+  const long run = std::max<long>(p.min_run, n * tiles / num_sms), waves = (n + num_sms - 1) / num_sms;
+  const bool whole = waves * tiles - run <= (n <= num_sms ? 3 + n / 5 : 13);
   p.list = units <= kScanUnits && n * tiles < (1L << 30) && !whole ? 1 : 0;
   p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (n * tiles + p.min_run - 1) / p.min_run)) : static_cast<int>(n);
   return p;

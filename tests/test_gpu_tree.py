@@ -394,11 +394,12 @@ def test_units_beyond_the_list():
 
 
 @pytest.mark.parametrize("c", ["none", "f32", "bf16", "split"])
-@pytest.mark.parametrize("d,g,n", [(64, 4, 9), (128, 4, 9), (64, 8, 40), (128, 8, 40)])
-def test_short_items_in_a_list(d, g, n, c):
+@pytest.mark.parametrize("d,g,n,b", [(64, 4, 9, 30), (128, 4, 9, 30), (64, 8, 40, 30), (128, 8, 40, 30),
+                                     (64, 4, 9, 20), (128, 4, 9, 20), (64, 8, 40, 25), (128, 8, 40, 25)])
+def test_short_items_in_a_list(d, g, n, b, c):
     """Runs of many items of one to four tiles, as a long capacity with short contents has them: what is asked for
     ahead (tiles, the moment matrices' slots, the next queries) crosses item after item."""
-    case = Case(d + n, b=30, h=8, g=g, d=d, n=n, rows=1700, c=c)
+    case = Case(d + n, b=b, h=8, g=g, d=d, n=n, rows=1700, c=c)
     rng = np.random.default_rng(n)
     case.length[:] = rng.choice([0, 1, 100, 128, 129, 300], size=case.length.shape)
     case.count[::5] = rng.integers(0, n + 1, size=case.count[::5].shape)
