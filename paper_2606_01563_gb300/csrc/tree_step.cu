@@ -24,7 +24,8 @@
 // into equal runs, one per CTA, wherever the run ends; an item cut by a
 // boundary leaves (m, l, O) of its parts in the workspace, and
 // tree_merge_kernel joins them.  Lengths of any raggedness so cost what their
-// tiles cost.  A CTA holds one or two row blocks: with two every K and V tile
+// tiles cost.  Where one CTA per item would leave few tiles idle, that is taken
+// instead (make_plan).  A CTA holds one or two row blocks: with two every K and V tile
 // is read once for 256 rows, with one the two softmax groups take the tiles
 // alternately and merge at the end.
 //
@@ -34,9 +35,9 @@
 // with V and its next S, so that one group's softmax runs beside the other's
 // products (one thread for both groups: its own instructions, some 10 cycles
 // each, left the tensor cores idle between the batches); warps 12-15 turn C'
-// into operands, in slots of the ring, while the last tiles are worked on.  Code that runs once per item is kept in loops: unrolled, it
-// waited for its own instructions (a masked tile took 9000 cycles instead of
-// 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
+// into operands, in slots of the ring, while the last tiles are worked on.  Code
+// that runs once per item is kept in loops: unrolled, it waited for its own
+// instructions (a masked tile took 9000 cycles instead of 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
 // 128 columns each, and O of the two, D columns each.
 //
 // What bounds it: with few query rows HBM (16 x 8 heads, 8 nodes of 4 heads, 8192
