@@ -679,7 +679,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           add = 1;
           umma_commit(&sh.empty[vi]);
           if (n16 > 0) {
-            ok = pwait(&sh.full[ni], nph, sh, a);
+            // (K's slot: with one row block and one slot of C' the ring is shifted
+            // by an odd number, so that V of the other thread's tile t - 3 had it,
+            // which nothing this thread has waited for implies.  Until that use is
+            // released K's phase must not be asked for: its parity is that of the
+            // use before.  With 0 or 2 slots of C', or 10 in the ring, this thread's
+            // or an earlier tile had the slot, and S or P of t - 2 implies its release.)
+            if (BLOCKS == 1 && s.c_slots == 1 && seq + s.slot(t) >= NS)
+              ok = pwait(&sh.empty[ni], nph ^ 1, sh, a);
+            ok = ok && pwait(&sh.full[ni], nph, sh, a);
             if (!ok) break;
             tc_fence_after();
             issue_s(ni, n16);
