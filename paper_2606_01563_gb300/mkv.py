@@ -196,8 +196,11 @@ def _nodes(t, what):
     """(node, batch) strides in elements of a [b, N, heads, d] bf16 tensor whose heads lie densely."""
     _need(t.dtype is _BF16 and t.dim() == 4 and t.stride(3) == 1 and
           (t.shape[2] == 1 or t.stride(2) == t.shape[3]), f"{what}: bf16 [b, N, heads, d] with dense heads")
-    # (a stride over an extent of one is never used: the dense value stands for it)
-    return (t.stride(1) if t.shape[1] > 1 else 0), (t.stride(0) if t.shape[0] > 1 else 0)
+    # (a stride over an extent of one is never used: 0, the dense value, stands for it; over a larger
+    # extent 0 would be taken for the dense value, past the end of an expanded tensor)
+    node, batch = (t.stride(1) if t.shape[1] > 1 else None), (t.stride(0) if t.shape[0] > 1 else None)
+    _need(node != 0 and batch != 0, f"{what}: not expanded over nodes or batch items")
+    return node or 0, batch or 0
 
 
 # ----------------------------------------------------------------- state
@@ -421,7 +424,10 @@ def mkv_tree_step(g, tree: Tree, q, k, v, cache: Cache, mom: Moments | None, p: 
         raise ValueError("q, k, v, out: bf16 with dense heads, k and v of the same strides, out contiguous")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (b, n, heads) or not lse.is_contiguous()):
         raise ValueError("lse: contiguous float32 [b, N, g*h_kv]")
-    # (a stride over an extent of one is never used: 0, the dense value, stands for it)
+    # (a stride over an extent of one is never used: 0, the dense value, stands for it; over a larger
+    # extent 0 would be taken for the dense value, past the end of an expanded tensor)
+    if (n > 1 and (qs[1] == 0 or ks[1] == 0)) or (b > 1 and (qs[0] == 0 or ks[0] == 0)):
+        raise ValueError("q, k, v: not expanded over nodes or batch items")
     t = _I64x7(n, 0 if tree.count is None else tree.count.data_ptr(), tree.mask.data_ptr(), qs[1] if n > 1 else 0,
                qs[0] if b > 1 else 0, ks[1] if n > 1 else 0, ks[0] if b > 1 else 0)
     code = lib().mkv_tree_step(g, t, q.data_ptr(), k.data_ptr(), v.data_ptr(), cache.c(),
