@@ -417,9 +417,12 @@ def mkv_tree_step(g, tree: Tree, q, k, v, cache: Cache, mom: Moments | None, p: 
     want, want_kv = (b, n, heads, d), (b, n, h, d)
     if g.batch != b or q.shape != want or out.shape != want or k.shape != want_kv or v.shape != want_kv:
         raise ValueError("q, out: [b, N, g*h_kv, d]; k, v: [b, N, h_kv, d], of the tree's b and N")
-    qs, ks = q.stride(), k.stride()
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    # (strides over an extent of one are never used and may differ)
     if (q.dtype is not _BF16 or k.dtype is not _BF16 or v.dtype is not _BF16 or out.dtype is not _BF16
-            or v.stride() != ks or not out.is_contiguous() or qs[3] != 1 or ks[3] != 1
+            or (vs != ks and (vs[3] != 1 or (h > 1 and vs[2] != ks[2]) or (n > 1 and vs[1] != ks[1])
+                              or (b > 1 and vs[0] != ks[0])))
+            or not out.is_contiguous() or qs[3] != 1 or ks[3] != 1
             or (heads > 1 and qs[2] != d) or (h > 1 and ks[2] != d)):
         raise ValueError("q, k, v, out: bf16 with dense heads, k and v of the same strides, out contiguous")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (b, n, heads) or not lse.is_contiguous()):

@@ -86,3 +86,25 @@ def test_extents_of_one_may_have_any_stride(recorder):
     _step(1, 1, h, g, d, x, k, k)
     assert list(recorder.calls.pop()[1][1])[3:] == [0, 0, 0, 0]
     assert isinstance(_commit(1, 1, h, d, k, k).array, ctypes.Array)
+
+
+def test_keys_and_values_of_one_batch_item_from_two_parents(recorder):
+    """Their strides differ only where an extent is one: the same addresses are meant."""
+    n, h, g, d = 5, 2, 2, 64
+    k = torch.zeros(1, n, h, d, dtype=BF)
+    v = torch.zeros(1, n + 4, h, d, dtype=BF)[:, :n]
+    assert k.stride() != v.stride()
+    _step(1, n, h, g, d, k=k, v=v)
+    assert list(recorder.calls.pop()[1][1])[5:] == [h * d, 0]
+    _commit(1, n, h, d, k, v)
+    one = torch.zeros(3, 1, 1, d, dtype=BF)  # one node, one head
+    _step(3, 1, 1, g, d, k=one, v=one.as_strided((3, 1, 1, d), (d, 7, 7, 1)))
+    assert list(recorder.calls.pop()[1][1])[5:] == [0, d]
+
+
+@pytest.mark.parametrize("v", [torch.zeros(2, 6, 2, 64, dtype=BF)[:, :5], torch.zeros(2, 5, 3, 64, dtype=BF)[:, :, :2],
+                               torch.zeros(2, 5, 2, 128, dtype=BF)[..., ::2], torch.zeros(2, 2, 5, 64, dtype=BF).transpose(1, 2)])
+def test_keys_and_values_of_unlike_strides_are_refused(recorder, v):
+    with pytest.raises(ValueError):
+        _step(2, 5, 2, 2, 64, v=v)
+    assert not recorder.calls
