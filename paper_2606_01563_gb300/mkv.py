@@ -446,7 +446,9 @@ def tree_layers(layers):
     _need(len(layers) > 0, "at least one layer")
     k0 = layers[0][1]
     kv = _nodes(k0, "k")
-    for _, k, v in layers:
+    b, _, h, d = k0.shape
+    for c, k, v in layers:
+        _need(c.K.shape == c.V.shape == (b, h, c.capacity, d), "caches of the batch, heads and dims of k and v")
         _need(k.shape == k0.shape and v.shape == k0.shape and _nodes(k, "k") == kv and _nodes(v, "v") == kv,
               "k and v: the same shape and strides in every layer")
     array = (mkv_tree_layer * len(layers))(*(mkv_tree_layer(c.c(), k.data_ptr(), v.data_ptr()) for c, k, v in layers))

@@ -108,3 +108,13 @@ def test_keys_and_values_of_unlike_strides_are_refused(recorder, v):
     with pytest.raises(ValueError):
         _step(2, 5, 2, 2, 64, v=v)
     assert not recorder.calls
+
+
+@pytest.mark.parametrize("geo", [(1, 2, 64), (2, 1, 64), (2, 2, 128)])
+def test_layers_with_a_cache_of_another_geometry_are_refused(geo):
+    """A commit would write past such a cache's end."""
+    kv = torch.zeros(2, 3, 2, 64, dtype=BF)
+    cache = mkv.alloc_cache(mkv.geom(geo[0], geo[1], 1, geo[2]), 8, "cpu")
+    with pytest.raises(ValueError):
+        mkv.tree_layers([(cache, kv, kv)])
+    mkv.tree_layers([(mkv.alloc_cache(mkv.geom(2, 2, 1, 64), 8, "cpu"), kv, kv)])
