@@ -202,9 +202,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ float pow2(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
 }
-// O's columns of this warp's rows times the row's factor.
+// O's columns of this warp's rows times the row's factor.  (Stores to tensor
+// memory are not ordered before loads that follow them: those of an earlier
+// scaling of the same tile are waited for.)
 template <int D>
 __device__ __forceinline__ void scale_columns(uint32_t tO, float f) {
+  tmem_wait_st();
 #pragma unroll 1
   for (int c = 0; c < D; c += 16) {
     uint32_t o[16];
@@ -221,7 +224,9 @@ __device__ __forceinline__ void scale_columns(uint32_t tO, float f) {
   }
 }
 // The weights (pairs of bf16) of the first n times 32 columns times the row's factor, a power of two.
+// (They were stored by this warp a moment ago, which has to be complete.)
 __device__ __forceinline__ void scale_weights(uint32_t tS, int n, float f) {
+  tmem_wait_st();
 #pragma unroll 1
   for (int c = 0; c < n; ++c) {
     uint32_t o[16];

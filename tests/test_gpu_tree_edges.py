@@ -9,6 +9,7 @@ import torch
 
 import tree_ref as R
 from paper_2606_01563_gb300 import mkv
+from paper_2606_01563_gb300.inputs import bf16_round
 from gpu_util import host
 from test_gpu_tree import Case
 
@@ -25,4 +26,23 @@ def test_one_slot_of_moments_in_a_ring_of_six(b, n, rows):
     for _ in range(40):
         c.step()
         assert torch.equal(c.out, first) and torch.equal(c.lse, lse)
+    c.check(own_sum=True)
+
+
+@pytest.mark.parametrize("g,n,rows", [(4, 20, 127), (4, 70, 127), (1, 40, 100), (8, 20, 255)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_reference_moves_several_times_in_a_masked_tile(g, n, rows, d):
+    """One node of a warp has scores that rise by 50 octaves every 32 keys, so the warp's reference moves in every
+    group of 32 columns; the other rows, whose scores rise by one or two, take O and the weights already written
+    of the tile along each time."""
+    c = Case(50 + n, h=2, g=g, d=d, n=n, rows=rows, c="none", masks="all")
+    rng = np.random.default_rng(d)
+    way = rng.choice([-1.0, 1.0], d) / np.sqrt(d)
+    large = np.arange(n) % (32 // g) == 0
+    c.q = bf16_round(rng.standard_normal(c.q.shape) + way)
+    c.q[0, large] = bf16_round(40 * way * np.sqrt(d / 128))
+    rise = 10 * np.sqrt(d / 128)
+    c.K[:, :, :rows] = bf16_round(0.5 * rng.standard_normal((1, 2, rows, d)) + rise * (np.arange(rows) // 32)[:, None] * way)
+    c.k = bf16_round(0.5 * rng.standard_normal(c.k.shape) + rise * (rows / 32 + np.arange(n) // 32)[:, None, None] * way)
+    c.device().step()
     c.check(own_sum=True)
