@@ -99,8 +99,9 @@ MKV_API size_t mkv_tree_workspace_size(mkv_geom geom, int32_t n_nodes, int32_t c
  * moment term with logit log n + scale q.mu_k and value mu_v + scale C' q
  * (p->order 1) or mu_v (order 0), as in mkv_decode_step; p->C16, p->C_split
  * and p->early_load have that call's meaning (with early_load the caller's
- * guarantee also covers tree->count and tree->mask; q, k and v are read after
- * the dependency wait).  A node that sees
+ * guarantee also covers tree->count and tree->mask, and a count or a number of
+ * evicted tokens that changed is recorded as a length is; q, k and v are read
+ * after the dependency wait).  A node that sees
  * nothing at all gets zeros and lse -infinity.  A node's key or value that is
  * not finite reaches only the nodes that see it; queries and keys of nodes
  * that are not in use and cache rows at or above len reach nothing.  A length

@@ -46,6 +46,7 @@
 // nodes, 131072 rows: 112 us, HBM's floor 79; 8 x 8 heads, 256 nodes, 4096 rows: 163
 // us, the tensor cores' floor 77); short items an item's start and end (4 x 8 heads,
 // 64 nodes, 1024 rows: 19 us).
+#include <limits.h>
 #include <stddef.h>
 
 #include <algorithm>
@@ -63,8 +64,8 @@ namespace {
 
 constexpr int kTile = 128;                   // keys per tile, rows per block
 constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
-constexpr int kWarpTma = 8, kWarpMma = 9, kWarpC = 12;
-constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps and an idle one; four for C'
+constexpr int kWarpTma = 8, kWarpMma = 9, kWarpCheck = 11, kWarpC = 12;
+constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps, one for early loads; four for C'
 constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
 constexpr float kSlack = 32.f;               // log2 headroom of the reference: weights are at most 2^32
 constexpr float kNegInf = -INFINITY;
@@ -103,10 +104,13 @@ struct Shared {
   int32_t abort, issued, q_issued;
   int32_t unit, mb, t0, start, end;  // the CTA's run of the list: first item, tile in it, the list's tiles [start, end)
   Raw raw;                     // of the first unit
-  int32_t scan[kThreads / 32];
   int32_t run;                 // tiles per CTA before the ends are moved
+  uint32_t seen[kThreads / 32];  // (early loads) the sizes that the run was made from, summed with weights
   uint32_t odd[2][8];          // nodes with a value that is not finite, of this segment and the next
-  float2 ml[kTile];            // (one row block) group 1's (m, l), then the two groups' factors
+  union {
+    float2 ml[kTile];          // (one row block) group 1's (m, l), then the two groups' factors
+    int32_t scan[kThreads / 32];  // (find_run, before that)
+  };
   union alignas(16) {   // (read as float4)
     float mu_k[kTile];  // from a segment's start
     float w[kTile];     // (one row block) at its end: the moment term's factor
@@ -276,6 +280,18 @@ __device__ __forceinline__ int batch_of(const Plan& p, int u) {
 __device__ __forceinline__ Raw load_raw(const TreeArgs& a, const Plan& p, int u) {
   return Raw{a.len[u], a.count != nullptr ? a.count[batch_of(p, u)] : a.N, a.n != nullptr ? a.n[u] : 0};
 }
+// The same from L2: what an early load left in L1 may be old.
+__device__ __forceinline__ Raw reload_raw(const TreeArgs& a, const Plan& p, int u) {
+  return Raw{__ldcg(a.len + u), a.count != nullptr ? __ldcg(a.count + batch_of(p, u)) : a.N,
+             a.n != nullptr ? __ldcg(a.n + u) : 0};
+}
+// A unit's share of the sum by which sizes that changed under an early load are
+// found: lengths that grow always change it, whichever they are (the sum of odd
+// multiples stays below 2^32), anything else but for one case in 2^32.
+__device__ __forceinline__ uint32_t raw_sum(int u, const Raw& r) {
+  return (2u * u + 1u) * (static_cast<uint32_t>(r.len) + 0x9e3779b1u * static_cast<uint32_t>(r.count) +
+                          0x85ebca6bu * static_cast<uint32_t>(r.n_e));
+}
 __device__ __forceinline__ Item make_item(const TreeArgs& a, const Raw& r) {
   Item it;
   it.len = min(max(r.len, 0), a.cap);
@@ -313,8 +329,16 @@ struct Segment {
 struct Walk {
   int unit, mb, t, left;
   Raw raw;  // (read while the segment before is worked on)
+  // With early loads the first unit's sizes are those that find_run read, the
+  // same for every role, and the others are read when they are due, after the
+  // dependency wait: the roles cannot disagree about sizes that changed.
+  static constexpr int kDue = INT_MIN;  // as a count
   __device__ __forceinline__ bool next(const TreeArgs& a, const Plan& p, Segment& s) {
     if (left <= 0) return false;
+    if (a.early && raw.count == kDue) {
+      grid_dependency_wait();
+      raw = reload_raw(a, p, unit);
+    }
     s.unit = unit;
     s.mb = mb;
     s.first = mb * ((p.blocks * kTile) >> p.g_shift);
@@ -336,7 +360,8 @@ struct Walk {
       // (lengths written while the call runs cannot lead past the last unit)
       if (++unit == a.batch * a.n_kv) left = 0;
     }
-    if (left > 0) raw = load_raw(a, p, unit);
+    if (a.early) raw.count = kDue;
+    else if (left > 0) raw = load_raw(a, p, unit);
     return true;
   }
 };
@@ -387,13 +412,19 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
   };
   const int chunk = (units + kThreads - 1) / kThreads, u0 = min(units, tid * chunk), u1 = min(units, u0 + chunk);
   int sum = 0;
+  uint32_t seen = 0;
 #pragma unroll 1
   for (int u = u0; u < u1; ++u) {
     const Raw r = chunk == 1 ? mine : load_raw(a, p, u);
     int tiles;
     const int alive = weigh(r, tiles);
     sum += alive * tiles + (p.mb - alive);
+    seen += raw_sum(u, r);
     if (blockIdx.x == 0) record(u, r);
+  }
+  if (a.early) {
+    seen = __reduce_add_sync(kAll, seen);
+    if ((tid & 31) == 0) sh.seen[tid >> 5] = seen;
   }
   int incl = sum;
 #pragma unroll
@@ -431,12 +462,12 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
       r = chunk == 1 ? mine : load_raw(a, p, u);
       alive = weigh(r, tiles);
       w = alive * tiles + (p.mb - alive);
-      if (pos < base + w) break;
+      if (pos < base + w || u + 1 == u1) break;  // (sizes read anew may have changed: no further)
       base += w;
     }
     int in = pos - base, mb = 0;  // the unit's tiles before `pos`
     while (mb < alive && in >= tiles) in -= tiles, ++mb;
-    if (mb == alive) mb += in, in = 0;
+    if (mb == alive) mb = min(mb + in, p.mb - 1), in = 0;
     const int item = pos - in;  // where the item starts
     int snap = pos;
     if (in > 0) {
@@ -444,13 +475,17 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
       else if (in <= 1) snap = item;
     }
     if (edge == 1) {
-      sh.end = snap;
+      sh.end = min(snap, total);
       continue;
     }
     if (snap == item + tiles && in > 0) {  // the next item
       if (++mb == p.mb) {
         mb = 0;
-        if (++u < units) r = load_raw(a, p, u);
+        if (++u == units) {  // there is none
+          sh.start = total;
+          continue;
+        }
+        r = load_raw(a, p, u);
       }
     }
     sh.unit = u;
@@ -460,6 +495,26 @@ __device__ __forceinline__ void find_run(const TreeArgs& a, const Plan& p, Share
     sh.start = snap;
   }
   __syncthreads();
+}
+
+// With early loads, one warp after the dependency wait: sizes that differ from
+// those that this CTA's run was made from are recorded.
+__device__ __noinline__ void check_early(const TreeArgs& a, const Plan& p, const Shared& sh) {
+  const int lane = threadIdx.x & 31, units = a.batch * a.n_kv;
+  grid_dependency_wait();
+  uint32_t diff = 0;
+  if (p.list) {
+    if (lane < kThreads / 32) diff = 0u - sh.seen[lane];
+#pragma unroll 4
+    for (int u = lane; u < units; u += 32) diff += raw_sum(u, reload_raw(a, p, u));
+    diff = __reduce_add_sync(kAll, diff);
+  }
+  if (lane != 0) return;
+  if (sh.end > sh.start) {
+    const Raw r = reload_raw(a, p, sh.unit);
+    diff |= (r.len ^ sh.raw.len) | (r.count ^ sh.raw.count) | (r.n_e ^ sh.raw.n_e);
+  }
+  if (diff != 0) record_bad(a.ws, MKV_ERR_INVALID_ARG, sh.end > sh.start ? sh.unit : 0);
 }
 
 template <int D, int BLOCKS>
@@ -791,6 +846,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.c_full);
     }
+  } else if (warp == kWarpCheck) {
+    if (a.early) check_early(a, p, sh);
   } else if (warp < kWarpTma) {
     // ---- softmax groups: thread r of group g has row r of a block
     const int g = warp >> 2, r = tid & 127;
@@ -1217,6 +1274,9 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   const int u = item / p.mb, mb = item - u * p.mb;
   const int2 d = parts.desc[item];  // (the same item in all warps of a block: it has at least 16 groups)
   if (d.x == d.y) return;
+  // (an item that no CTA began, as lengths that changed during the call can leave it, has an old record)
+  if (static_cast<uint32_t>(d.x) >= static_cast<uint32_t>(p.grid) || static_cast<uint32_t>(d.y) >= static_cast<uint32_t>(p.grid))
+    return;
   const int R = p.blocks * kTile, row = z * kTile + (id & 3) * 32 + lane;
   const int G = 1 << p.g_shift, b = batch_of(p, u), kv = u - b * a.n_kv;
   const int node = mb * (R >> p.g_shift) + (row >> p.g_shift), h = row & (G - 1);

@@ -46,3 +46,53 @@ def test_reference_moves_several_times_in_a_masked_tile(g, n, rows, d):
     c.k = bf16_round(0.5 * rng.standard_normal(c.k.shape) + rise * (rows / 32 + np.arange(n) // 32)[:, None, None] * way)
     c.device().step()
     c.check(own_sum=True)
+
+
+@pytest.mark.parametrize("b,h,n,rows,c", [(1, 2, 9, 300, "f32"),       # an item per CTA
+                                          (1, 2, 20, 20000, "f32"),    # the list of tiles: 2 units in many parts
+                                          (2, 8, 40, 3000, "none"),    # two row blocks
+                                          (70, 8, 5, 600, "bf16")])    # more units than threads in a CTA
+def test_a_length_that_changes_under_an_early_load_is_recorded(b, h, n, rows, c):
+    """A decode step, whose kernel is still running, appends a row to the cache that the call behind it reads with
+    early_load.  Either the call read the new length everywhere, then it is right, or MKV_ERR_INVALID_ARG is recorded;
+    no wait runs out, and the same call without early_load is right afterwards."""
+    case = Case(b + n, b=b, h=h, n=n, rows=rows, c=c, spare=0.0).device()
+    _, _, g, d = case.geo
+    ws = mkv.alloc_workspace(mkv.mkv_decode_workspace_size(case.g, case.cap))
+    q, k, v = (x[:, 0].contiguous() for x in (case.dq, case.dk, case.dv))
+    y = torch.empty(b, h * g, d, device="cuda")
+
+    def pair():
+        case.p.early_load = 0
+        mkv.mkv_decode_step(case.g, q, k, v, case.cache, case.mom, case.p, y, None, ws)
+        case.p.early_load = 1
+        case.step()
+
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):  # (no host time between the two)
+        pair()
+    recorded = 0
+    for _ in range(20):
+        case.cache.len.fill_(rows)
+        case.out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        code, _ = mkv.mkv_get_device_error(case.ws)
+        assert code in (0, 1)
+        assert (case.cache.len == rows + 1).all()
+        out, lse = case.out.clone(), case.lse.clone()
+        case.p.early_load = 0
+        case.step()
+        assert mkv.mkv_get_device_error(case.ws)[0] == 0
+        if code == 0:
+            assert torch.equal(out, case.out) and torch.equal(lse, case.lse)
+        recorded += code
+    print(f"{recorded} of 20 recorded")
+    # lengths that stay: nothing is recorded, and the outputs are those of the call that waits
+    case.p.early_load = 1
+    out.copy_(case.out), lse.copy_(case.lse)
+    torch.cuda.synchronize()
+    case.step()
+    assert mkv.mkv_get_device_error(case.ws)[0] == 0
+    assert torch.equal(out, case.out) and torch.equal(lse, case.lse)
