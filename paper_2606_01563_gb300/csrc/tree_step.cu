@@ -898,7 +898,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           e = fmaf(e0 + e1, qs, log2f(static_cast<float>(s.it.n_e)));
           m = ceilf(e);
-          l = lr = fast_exp2(e - m);  // (a NaN passes on)
+          l = lr = e != kNegInf ? fast_exp2(e - m) : 0.f;  // (without weight no term; a NaN passes on)
         }
       }
       if (active) {
@@ -1135,7 +1135,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         f0 *= even;
         if (k1 > k0 + 1) f1 *= sh.w[r];
       }
-      float w = mom && mine ? fast_exp2(e - M) * even : 0.f;
+      float w = mom && mine && e != kNegInf ? fast_exp2(e - M) * even : 0.f;
       if (whole) {
         const float inv = L != 0.f ? 1.f / L : 0.f;
         f0 *= inv, f1 *= inv, w *= inv;
@@ -1151,6 +1151,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // a factor of 0 stands for a state without content: its columns may hold anything
       const bool use0 = f0 != 0.f && k1 > k0, use1 = f1 != 0.f && k1 > k0 + 1, use_f = mom && a.order == 1;
       const float wf = w * scale;
+      const bool absent = __any_sync(kAll, wf == 0.f);  // a term without weight is absent, whatever Q C'^T came to
       const bool put = node < a.N;
       const size_t orow = ((size_t)b * a.N + node) * HQ + (kv << p.g_shift) + h;
       const uint32_t tA = tm + lanes + cO + (BLOCKS == 2 ? g * D : 0) + c_lo, tB = tA + D;
@@ -1174,6 +1175,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld32_async(tF + c, x);
             tmem_wait_ld();
             keep16(x), keep16(x + 16);
+            if (absent) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = wf == 0.f ? 0u : x[i];
+            }
           }
           float m32 = mv[0];
 #pragma unroll

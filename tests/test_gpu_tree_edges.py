@@ -96,3 +96,22 @@ def test_a_length_that_changes_under_an_early_load_is_recorded(b, h, n, rows, c)
     case.step()
     assert mkv.mkv_get_device_error(case.ws)[0] == 0
     assert torch.equal(out, case.out) and torch.equal(lse, case.lse)
+
+
+@pytest.mark.parametrize("masks,rows", [("tree", 100), ("self", 0), ("none", 0), ("all", 3000)])
+@pytest.mark.parametrize("n", [9, 70])
+@pytest.mark.parametrize("large_c", [False, True])
+def test_a_moment_logit_of_minus_infinity_is_no_term(masks, rows, n, large_c):
+    """q.mu_k below the range of 32 bits: the term has no weight, whatever its value, and a row that sees nothing
+    else gets zeros and a log-normaliser of -infinity."""
+    c = Case(60 + n, h=2, n=n, rows=rows, c="f32", masks=masks)
+    c.q = np.abs(c.q) + np.float32(0.5)
+    c.q = bf16_round(c.q)
+    nn, mk, mv, C = c.moments
+    nn[:] = 100
+    mk[:] = -1e38
+    if large_c:
+        C[:] = 3e38  # its product with q overflows
+    c.device().step()
+    c.moments = None  # the reference's: no term
+    c.check(own_sum=True)
