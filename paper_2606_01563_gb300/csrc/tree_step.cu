@@ -10,11 +10,12 @@
 // row, with logit e = log n + scale q.mu_k and value mu_v + scale C' q: its
 // weight starts m and l, and its value joins at the end, the product Q C'^T
 // running on the tensor cores with C' as bf16 hi + lo parts.  m only has to be
-// common to a row's keys, so it moves (by a whole number, with a rescaling of
-// O and l) only when a score exceeds it by more than 32 in log2 units: a
-// floating-point sum of weights up to 2^32 is as exact as one of weights up to 1,
-// and with 8 some row of a warp moved in most tiles of a long cache (700
-// cycles each).  P enters
+// common to a row's keys, so it is set 32 above the largest score so far in log2
+// units and moves (by a whole number, with a rescaling of O and l) only when a
+// score exceeds it: weights are at most 1, so that no sum overflows whose terms
+// do not, and above 2^-33 for the largest score, which a floating-point sum
+// holds as exactly (with 8 some row of a warp moved in most tiles of a long
+// cache, 700 cycles each).  P enters
 // the second product rounded to bf16 (2^-8 relative, the output's own
 // rounding); l is summed from the unrounded weights, and O is scaled by the
 // ratio of that sum to the rounded weights' (where a few weights dominate,
@@ -67,7 +68,7 @@ constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpCheck = 11, kWarpC = 12;
 constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps, one for early loads; four for C'
 constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
-constexpr float kSlack = 32.f;               // log2 headroom of the reference: weights are at most 2^32
+constexpr float kSlack = 32.f;               // the reference lies this far (log2) above the score that set it
 constexpr float kNegInf = -INFINITY;
 constexpr uint32_t kAll = 0xffffffffu;
 
@@ -117,6 +118,7 @@ struct Shared {
   };
 };
 constexpr int kSharedBytes = 2048;
+static_assert(kSlack == 32.f, "log_sum");
 static_assert(sizeof(Shared) <= kSharedBytes, "shared variables");
 static_assert(offsetof(Shared, mu_k) % 16 == 0 && kSharedBytes % 16 == 0, "mu_k is read 16 bytes at a time");
 __host__ __device__ constexpr int smem_bytes(int D, int blocks) {
@@ -205,6 +207,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // 2^d of a whole number d <= 0, exactly (0 below the smallest normal number).
 __device__ __forceinline__ float pow2(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + static_cast<int>(d)) << 23);
+}
+// The natural log of a normaliser l about the reference m (the reference's headroom goes into l, exactly).
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l != 0.f ? (m - kSlack + log2f(l * 0x1p32f)) * kLn2 : kNegInf;
 }
 // O's columns of this warp's rows times the row's factor.  (Stores to tensor
 // memory are not ordered before loads that follow them: those of an earlier
@@ -897,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           e = fmaf(e0 + e1, qs, log2f(static_cast<float>(s.it.n_e)));
-          m = ceilf(e);
+          m = ceilf(e) + kSlack;
           l = lr = e != kNegInf ? fast_exp2(e - m) : 0.f;  // (without weight no term; a NaN passes on)
         }
       }
@@ -990,8 +996,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
           }
           const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * qs;
-          if (__any_sync(kAll, top > m + kSlack)) {
-            const float mn = fmaxf(m, ceilf(top));
+          if (__any_sync(kAll, top > m)) {
+            const float mn = fmaxf(m, ceilf(top) + kSlack);
             const float f = m == kNegInf ? 1.f : pow2(m - mn);
             m = mn;
             l *= f, lr *= f;
@@ -1056,8 +1062,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qs;
-            if (__any_sync(kAll, top > m + kSlack)) {
-              const float mn = fmaxf(m, ceilf(top));
+            if (__any_sync(kAll, top > m)) {
+              const float mn = fmaxf(m, ceilf(top) + kSlack);
               const float f = m == kNegInf ? 1.f : pow2(m - mn);
               m = mn;
               l *= f, lr *= f;
@@ -1229,7 +1235,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (BLOCKS == 2 || g == 0) {
         if (whole) {
-          if (put && a.lse != nullptr) a.lse[orow] = live && L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
+          if (put && a.lse != nullptr) a.lse[orow] = live ? log_sum(M, L) : kNegInf;
         } else if (warp_live) {
           parts.ml[(size_t)part * R + (BLOCKS == 2 ? g * kTile + r : r)] = make_float2(M, L);
         }
@@ -1344,7 +1350,7 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
         L != 0.f ? make_uint2(pack_bf16x2(acc[4 * k] * inv, acc[4 * k + 1] * inv),
                               pack_bf16x2(acc[4 * k + 2] * inv, acc[4 * k + 3] * inv))
                  : make_uint2(0, 0);
-  if (c4 == 0 && a.lse != nullptr) a.lse[orow] = L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
+  if (c4 == 0 && a.lse != nullptr) a.lse[orow] = log_sum(M, L);
 }
 
 Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {

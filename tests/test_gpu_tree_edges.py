@@ -115,3 +115,26 @@ def test_a_moment_logit_of_minus_infinity_is_no_term(masks, rows, n, large_c):
     c.device().step()
     c.moments = None  # the reference's: no term
     c.check(own_sum=True)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 105, 2.0 ** -90])
+@pytest.mark.parametrize("b,h,g,n,rows,c", [(1, 2, 4, 9, 300, "none"), (1, 2, 4, 9, 300, "f32"), (8, 8, 4, 64, 700, "none"),
+                                            (1, 1, 4, 20, 6000, "none")])
+def test_values_near_the_ends_of_the_range(size, b, h, g, n, rows, c):
+    """Scores that rise by 20 to 35 octaves after the first tile, with values of 2^105 and 2^-90: no weighted sum
+    leaves the range, as none does whose weights are at most 1."""
+    case = Case(70 + n, b=b, h=h, g=g, n=n, rows=rows, c=c)
+    rng = np.random.default_rng(1)
+    way = rng.choice([-1.0, 1.0], 128) / np.sqrt(128)
+    case.q = bf16_round(0.5 * rng.standard_normal(case.q.shape) + 4 * way)
+    case.K[:, :, 128:rows] = bf16_round(0.5 * rng.standard_normal((b, h, rows - 128, 128)) + 55 * way)
+    case.V[:, :, :rows] *= size
+    case.v *= size
+    if case.moments is not None:
+        case.moments[2][:] *= size  # mu_v, C
+        case.moments[3][:] *= size
+        if size < 1:
+            case.moments[0][:] = 0  # (tau would clamp such a C)
+    case.device().step()
+    case.check(own_sum=True)
+    assert np.abs(host(case.out).astype(np.float64)).max() > size / 8
