@@ -81,8 +81,9 @@ MKV_API mkv_status mkv_tree_build(int32_t batch, int32_t n_nodes, const int32_t*
 
 /*
  * Bytes of device workspace mkv_tree_step needs for this geometry, N and cache
- * capacity on the current device.  Returns 0 if the arguments are invalid.
- * The workspace must be zero-filled before its first use; every call leaves
+ * capacity on the current device, and for every smaller batch, N and capacity
+ * (one workspace sized for the largest serves them all).  Returns 0 if the
+ * arguments are invalid.  The workspace must be zero-filled before its first use; every call leaves
  * it ready for the next one.
  */
 MKV_API size_t mkv_tree_workspace_size(mkv_geom geom, int32_t n_nodes, int32_t capacity);

@@ -68,6 +68,7 @@ constexpr int kBox = kTile * 128;            // bytes of 128 rows x 64 bf16
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpCheck = 11, kWarpC = 12;
 constexpr int kThreads = 512;                // 2 softmax groups; a TMA warp, two MMA warps, one for early loads; four for C'
 constexpr int kScanUnits = 4096;             // units (and 2^30 tiles) above which every item has a CTA of its own
+constexpr int kMinRun = 2;                   // tiles of a list's run at least
 constexpr float kSlack = 32.f;               // the reference lies this far (log2) above the score that set it
 constexpr float kNegInf = -INFINITY;
 constexpr uint32_t kAll = 0xffffffffu;
@@ -1353,15 +1354,24 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   if (c4 == 0 && a.lse != nullptr) a.lse[orow] = log_sum(M, L);
 }
 
+// Tiles of an item at most.
+long max_tiles(int n_nodes, int capacity) {
+  return 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
+}
+// CTAs of a list of so many tiles at most.
+int list_grid(long tiles, int num_sms) {
+  return static_cast<int>(std::min<long>(num_sms, (tiles + kMinRun - 1) / kMinRun));
+}
+
 Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   Plan p{};
   const int rows = n_nodes * g.group;
   p.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
   p.words = tree_words(n_nodes);
   p.kv_inv = ((1ull << 40) + g.n_kv_heads - 1) / g.n_kv_heads;
-  p.min_run = 2;
+  p.min_run = kMinRun;
   const long units = (long)g.batch * g.n_kv_heads;
-  const long tiles = 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
+  const long tiles = max_tiles(n_nodes, capacity);
   const auto items = [&](int blocks) { return units * ((rows + blocks * kTile - 1) / (blocks * kTile)); };
   // One row block per CTA spreads few, short items over more SMs; two read K and
   // V once for 256 rows.  Measured, one and two: 4 x 8 heads, 64 nodes of 4
@@ -1385,14 +1395,14 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   const long run = std::max<long>(p.min_run, n * tiles / num_sms), waves = (n + num_sms - 1) / num_sms;
   const bool whole = waves * tiles - run <= (n <= num_sms ? 3 + n / 5 : 13);
   p.list = units <= kScanUnits && n * tiles < (1L << 30) && !whole ? 1 : 0;
-  p.grid = p.list ? static_cast<int>(std::min<long>(num_sms, (n * tiles + p.min_run - 1) / p.min_run)) : static_cast<int>(n);
+  p.grid = p.list ? list_grid(n * tiles, num_sms) : static_cast<int>(n);
   return p;
 }
 
-size_t parts_bytes(const mkv_geom& g, const Plan& p) {
-  if (!p.list) return 0;
-  const size_t R = (size_t)p.blocks * kTile;
-  return align_up((size_t)g.batch * g.n_kv_heads * p.mb * sizeof(int2), 256) + 2 * (size_t)p.grid * R * (8 + (size_t)g.head_dim * 4);
+// Bytes of the parts' records of a list plan.
+size_t parts_bytes(long items, int blocks, int grid, int D) {
+  return align_up(static_cast<size_t>(items) * sizeof(int2), 256) +
+         2 * static_cast<size_t>(grid) * blocks * kTile * (8 + static_cast<size_t>(D) * 4);
 }
 
 // bf16 [n3][n2][n1][inner] with the strides of n1, n2, n3 in elements; boxes of b1 x b2 rows of 64 elements.
@@ -1440,8 +1450,18 @@ cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, co
 
 }  // namespace
 
+// Enough for the plan of every batch, number of nodes and capacity up to these:
+// plans change with each of them, and only lists have parts, so that a smaller
+// tree can need more than a larger one.
 size_t tree_workspace_bytes(const mkv_geom& g, int32_t n_nodes, int32_t capacity, int num_sms) {
-  return kHeaderBytes + parts_bytes(g, make_plan(g, n_nodes, capacity, num_sms));
+  const long units = std::min<long>((long)g.batch * g.n_kv_heads, kScanUnits), rows = (long)n_nodes * g.group;
+  const long tiles = max_tiles(n_nodes, capacity);
+  size_t most = 0;
+  for (int blocks = 1; blocks <= (rows > kTile ? 2 : 1); ++blocks) {
+    const long items = units * ((rows + blocks * kTile - 1) / (blocks * kTile));
+    most = std::max(most, parts_bytes(items, blocks, list_grid(items * tiles, num_sms), g.head_dim));
+  }
+  return kHeaderBytes + most;
 }
 
 cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {

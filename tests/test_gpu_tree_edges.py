@@ -138,3 +138,20 @@ def test_values_near_the_ends_of_the_range(size, b, h, g, n, rows, c):
     case.device().step()
     case.check(own_sum=True)
     assert np.abs(host(case.out).astype(np.float64)).max() > size / 8
+
+
+def test_one_workspace_for_trees_of_every_size():
+    """A workspace of the largest tree's and capacity's size, with a guard behind it, serves smaller ones: lists and
+    whole items, one and two row blocks, one after another."""
+    size = mkv.mkv_tree_workspace_size(mkv.geom(4, 8, 4, 128), 256, 4096)
+    room = torch.zeros(size + 4096, dtype=torch.uint8, device="cuda")
+    room[size:] = 77
+    for b, n, rows, cap in [(4, 256, 4000, 4096), (4, 32, 2000, 2064), (4, 64, 2000, 2064), (1, 65, 1000, 1040),
+                            (1, 128, 1000, 1040), (1, 8, 2200, 2304), (1, 1, 4000, 4096), (2, 9, 30, 4096), (4, 13, 700, 800)]:
+        c = Case(b + n, b=b, h=8, g=4, n=n, rows=rows, cap=cap, c="f32" if n < 100 else "none", ragged=n < 256).device()
+        c.ws = room[:size]
+        c.step()
+        if n < 256:
+            c.check(own_sum=True)
+    assert mkv.mkv_get_device_error(room)[0] == 0
+    assert (room[size:] == 77).all()

@@ -118,3 +118,15 @@ def test_layers_with_a_cache_of_another_geometry_are_refused(geo):
     with pytest.raises(ValueError):
         mkv.tree_layers([(cache, kv, kv)])
     mkv.tree_layers([(mkv.alloc_cache(mkv.geom(2, 2, 1, 64), 8, "cpu"), kv, kv)])
+
+
+@pytest.mark.parametrize("h,g,d", [(8, 4, 128), (2, 8, 64), (5, 1, 128), (1, 2, 64)])
+def test_a_workspace_serves_every_smaller_call(h, g, d):
+    """Sized once for the largest batch, tree and capacity; the plans of smaller ones may need parts where it needs none."""
+    caps, nodes = [1, 64, 128, 129, 500, 1040, 2064, 2304, 9000, 131072], [1, 8, 16, 31, 32, 33, 64, 65, 100, 128, 200, 256]
+    batches = [1, 2, 4, 9, 32, 100, 600]
+    size = {(b, n, c): mkv.mkv_tree_workspace_size(mkv.geom(b, h, g, d), n, c) for b in batches for n in nodes for c in caps}
+    for b, n, c in size:
+        assert size[b, n, c] >= 256 and size[b, n, c] <= 50 << 20
+        for smaller in ((x, n, c) for x in batches if x < b), ((b, x, c) for x in nodes if x < n), ((b, n, x) for x in caps if x < c):
+            assert all(size[s] <= size[b, n, c] for s in smaller), (b, n, c)
