@@ -155,3 +155,75 @@ def test_one_workspace_for_trees_of_every_size():
             c.check(own_sum=True)
     assert mkv.mkv_get_device_error(room)[0] == 0
     assert (room[size:] == 77).all()
+
+
+def _not_finite(c, rng):
+    """Puts values that are not finite, and a NaN key, into some units' nodes: what every row has to be is
+    (key, {column: value}) per (item, KV head, node)."""
+    b, h, _, d = c.geo
+    bad_v, bad_k = {}, {}
+    for bi in range(b):
+        for hi in range(h):
+            m = int(c.count[bi])
+            if m < 3 or rng.random() < 0.4:
+                continue
+            for value in (np.inf, -np.inf, np.nan, np.inf):  # (of both node tiles where there are two)
+                node = int(rng.integers(0, m)) if rng.random() < 0.5 else m - 1 - int(rng.integers(0, min(m, 5)))
+                col = int(rng.choice([3, 3, 62, d - 1]))
+                c.v[bi, node, hi, col] = value
+                bad_v[bi, hi, node, col] = value
+            if rng.random() < 0.3:
+                node = int(rng.integers(0, m))
+                c.k[bi, node, hi, 8] = np.nan
+                bad_k[bi, hi, node] = True
+    return bad_v, bad_k
+
+
+@pytest.mark.parametrize("b,h,g,d,n,rows,masks,short", [
+    (1, 2, 4, 128, 40, 6000, "random", False),   # cut items, one row block
+    (1, 8, 4, 128, 64, 9000, "random", False),   # cut items, two row blocks
+    (2, 8, 2, 128, 256, 500, "random", False),   # two node tiles, two row blocks, whole items
+    (1, 2, 1, 64, 200, 4000, "tree", False),     # two node tiles in cut items
+    (1, 1, 8, 128, 200, 300, "odd", False),      # several row blocks of one unit
+    (30, 8, 4, 128, 9, 1700, "random", True),    # runs of short items: some units have such values, the next have none
+    (30, 8, 8, 64, 40, 1700, "tree", True),
+    (12, 8, 4, 64, 140, 900, "random", True)])
+@pytest.mark.parametrize("moments", ["none", "f32"])
+def test_not_finite_values_in_every_plan(b, h, g, d, n, rows, masks, short, moments):
+    """As in whole items of one row block: they reach the rows that see them, and no others.  The others differ from
+    those of a run without such values by one rounding at most (a row that holds a NaN may leave its warp's reference
+    elsewhere)."""
+    runs = []
+    for bad in (False, True):
+        c = Case(80 + n, b=b, h=h, g=g, d=d, n=n, rows=rows, c=moments, masks=masks, spare=0.0)
+        rng = np.random.default_rng(n)
+        if short:
+            c.length[:] = rng.choice([0, 1, 100, 128, 129, 300], size=c.length.shape)
+            c.count[::5] = rng.integers(0, n + 1, size=c.count[::5].shape)
+            c.sees = [[[a for a in row if a < m] for row in rows_] for rows_, m in zip(c.sees, c.count.tolist())]
+        if bad:
+            bad_v, bad_k = _not_finite(c, rng)
+            assert bad_v
+        c.device().step()
+        assert mkv.mkv_get_device_error(c.ws)[0] == 0
+        runs.append((host(c.out).astype(np.float64), host(c.lse).astype(np.float64)))
+    (want, want_lse), (got, got_lse) = runs
+    with np.errstate(invalid="ignore"):
+        for bi in range(b):
+            for i in range(int(c.count[bi])):
+                see = set(c.sees[bi][i])
+                for (x, hi, node, col), _ in bad_v.items():
+                    if x == bi and node in see:  # (the last one written there)
+                        want[bi, i, hi * g:(hi + 1) * g, col] += c.v[bi, node, hi, col]
+                for x, hi, node in bad_k:
+                    if x == bi and node in see:
+                        want[bi, i, hi * g:(hi + 1) * g], want_lse[bi, i, hi * g:(hi + 1) * g] = np.nan, np.nan
+    assert (np.isnan(got) == np.isnan(want)).all() and (np.isnan(got_lse) == np.isnan(want_lse)).all()
+    ok = ~np.isnan(want)
+    fin = ok & np.isfinite(want)
+    assert (got[ok & ~fin] == want[ok & ~fin]).all()
+    assert (np.abs(got[fin] - want[fin]) <= 2.0 ** -8 * np.abs(want[fin]) + 1e-6).all()
+    ok = np.isfinite(want_lse)
+    assert (np.isneginf(got_lse) == np.isneginf(want_lse)).all()
+    assert (np.abs(got_lse[ok] - want_lse[ok]) <= 1e-5).all()
+    assert not np.isfinite(want).all()
