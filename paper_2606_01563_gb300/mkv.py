@@ -441,16 +441,20 @@ def mkv_tree_step(g, tree: Tree, q, k, v, cache: Cache, mom: Moments | None, p: 
 
 
 def tree_layers(layers):
-    """(cache, k, v) of every layer, k and v as given to mkv_tree_step: made once and kept beside the caches."""
+    """(cache, k, v) of every layer, k and v as given to mkv_tree_step.  It holds their addresses: made once and kept
+    beside the caches where a program's k and v stay in their buffers, and made again (36 layers: some 0.1 ms on the
+    host) where a step has new ones."""
     layers = list(layers)
     _need(len(layers) > 0, "at least one layer")
     k0 = layers[0][1]
-    kv = _nodes(k0, "k")
-    b, _, h, d = k0.shape
+    kv, shape, stride = _nodes(k0, "k"), k0.shape, k0.stride()
+    b, _, h, d = shape
     for c, k, v in layers:
-        _need(c.K.shape == c.V.shape == (b, h, c.capacity, d), "caches of the batch, heads and dims of k and v")
-        _need(k.shape == k0.shape and v.shape == k0.shape and _nodes(k, "k") == kv and _nodes(v, "v") == kv,
-              "k and v: the same shape and strides in every layer")
+        for t, what in ((k, "k"), (v, "v")):
+            _need(t.shape == shape and ((t.stride() == stride and t.dtype is _BF16) or _nodes(t, what) == kv),
+                  "k and v: the same shape and strides in every layer")
+        cap = c.K.shape
+        _need(cap[0] == b and cap[1] == h and cap[3] == d and c.V.shape == cap, "caches of the batch, heads and dims of k and v")
     array = (mkv_tree_layer * len(layers))(*(mkv_tree_layer(c.c(), k.data_ptr(), v.data_ptr()) for c, k, v in layers))
     return TreeLayers(array, mkv_tree(k0.shape[1], None, None, 0, 0, *kv), k0.shape[0], layers)
 
