@@ -108,7 +108,9 @@ MKV_API size_t mkv_tree_workspace_size(mkv_geom geom, int32_t n_nodes, int32_t c
  * that are not in use and cache rows at or above len reach nothing.  A length
  * outside 0..capacity is recorded as MKV_ERR_CAPACITY and taken as the nearer
  * end.  Scores, statistics and sums are fp32; the softmax weights enter the
- * product with the values rounded to bf16, as the output is.
+ * product with the values rounded to bf16, as the output is, and the order-1
+ * product takes an fp32 C' as two bf16 parts (16 to 17 significant bits, those of
+ * mkv_moments_pack_split).
  * Requirements: q, k, v and out 16-byte aligned, lse and mask 4; mom may be
  * NULL if p->correction is 0.
  */
@@ -129,7 +131,8 @@ typedef struct {
  * each of its KV heads, row len + j = node path[i][j] (keys, values, position
  * seen + j) for j < n_path[i]; then len and seen grow by n_path[i].  The
  * caches' y rows stay valid (rows are added above y_len).
- *   layers    HOST array of n_layers entries, copied during the call; k and v
+ *   layers    HOST array of n_layers entries (new addresses at every step where
+ *             k and v are new tensors), copied during the call; k and v
  *             have the strides tree->kv_node and kv_batch in every layer
  *   path      int32 [b, path_len]  node indices, root first
  *   n_path    int32 [b]            accepted nodes, 0..path_len

@@ -35,18 +35,19 @@
 // and 10 the MMAs of a group each: S of its first tile, then in turn its product
 // with V and its next S, so that one group's softmax runs beside the other's
 // products (one thread for both groups: its own instructions, some 10 cycles
-// each, left the tensor cores idle between the batches); warps 12-15 turn C'
+// each, left the tensor cores idle between the batches); warp 11 looks after
+// sizes that were read early; warps 12-15 turn C'
 // into operands, in slots of the ring, while the last tiles are worked on.  Code
 // that runs once per item is kept in loops: unrolled, it waited for its own
 // instructions (a masked tile took 9000 cycles instead of 2000).  Tensor memory: S (then P over it, at last Q C'^T) of the two groups,
 // 128 columns each, and O of the two, D columns each.
 //
 // What bounds it: with few query rows HBM (16 x 8 heads, 8 nodes of 4 heads, 8192
-// rows: 87 us, 0.92 of the copy rate); with 256 rows per tile the chain of a tile
+// rows: 89 us, 0.90 of the copy rate); with 256 rows per tile the chain of a tile
 // in each group, between the floors of HBM and the tensor cores (8 heads, 33
 // nodes, 131072 rows: 112 us, HBM's floor 79; 8 x 8 heads, 256 nodes, 4096 rows: 163
 // us, the tensor cores' floor 77); short items an item's start and end (4 x 8 heads,
-// 64 nodes, 1024 rows: 19 us).
+// 64 nodes, 1024 rows: 19.5 us).
 #include <limits.h>
 #include <stddef.h>
 
