@@ -11,6 +11,9 @@
  *                     keys: of the drafted nodes before mkv_tree_step, of a
  *                     prompt before mkv_compress, of one token before
  *                     mkv_decode_step; inverse = 1 is its gradient
+ *   mkv_norm_rope     the same with the norms of queries and keys per head in
+ *                     front, for models that have them; mkv_norm_rope_grad is
+ *                     its gradient
  *   mkv_tree_step     attention of every node over the retained cache, the
  *                     nodes it sees and the moment term of the evicted tokens,
  *                     in one normaliser; the cache is not changed
@@ -184,6 +187,65 @@ typedef struct {
 MKV_API mkv_status mkv_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
                             int64_t pos_batch, const mkv_rope_params* p, int32_t n_tensors,
                             const mkv_rope_tensor* tensors, void* stream);
+
+/* A tensor of mkv_norm_rope, with the weights of its norm. */
+typedef struct {
+  mkv_rope_tensor t;    /* as in mkv_rope                                                              */
+  const void* weight;   /* bf16 or fp32 [d], or one row for each head; 16-byte aligned; NULL: ones     */
+  int64_t weight_head;  /* elements from one head's row to the next, a multiple of 8 and at least d; 0: */
+                        /* one row for all heads                                                       */
+  int32_t weight_f32;   /* 1: fp32 weights; 0: bf16                                                    */
+} mkv_norm_rope_tensor;
+
+/*
+ * Norms of queries and keys per head, and their rotary positions, in one pass
+ * (one launch on `stream`): for every head of every token, n = x (mean x^2 +
+ * eps)^(-1/2) weight over the d values, then n rotated as mkv_rope does.
+ * Everything is fp32 between x and the one rounding to bf16; sums of squares
+ * that pass fp32's range are taken of smaller values, so that any finite x has
+ * its norm.  Arguments, layouts and requirements as in mkv_rope, with
+ * p->inverse 0 and eps above 0 and finite.
+ */
+MKV_API mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
+                                 int64_t pos_batch, const mkv_rope_params* p, float eps, int32_t n_tensors,
+                                 const mkv_norm_rope_tensor* tensors, void* stream);
+
+/* A tensor of mkv_norm_rope_grad: bf16 [b, tokens, heads, d] each with the strides given.  dx may be x or dy
+ * with the same strides (in place); else it must not overlap them. */
+typedef struct {
+  const void* x;        /* what mkv_norm_rope read                                            */
+  const void* dy;       /* the gradient of what it wrote                                     */
+  void* dx;             /* the gradient of x                                                 */
+  int32_t heads;
+  int64_t x_batch, x_token, x_head;
+  int64_t dy_batch, dy_token, dy_head;
+  int64_t dx_batch, dx_token, dx_head;
+  const void* weight;   /* as in mkv_norm_rope_tensor                                        */
+  int64_t weight_head;
+  int32_t weight_f32;
+  float* dweight;       /* fp32 [d], or dense [heads, d] where weight_head is not 0: the gradient of the */
+                        /* weights, overwritten; NULL: not wanted                           */
+} mkv_norm_rope_grad_tensor;
+
+/*
+ * Bytes of device workspace mkv_norm_rope_grad needs for these tensors (only
+ * heads and weight_head are read) on the current device.  Returns 0 if the
+ * arguments are invalid.  The workspace needs no initialisation.
+ */
+MKV_API size_t mkv_norm_rope_grad_workspace_size(int32_t batch, int32_t tokens, int32_t head_dim, int32_t n_tensors,
+                                                 const mkv_norm_rope_grad_tensor* tensors);
+
+/*
+ * The gradient of mkv_norm_rope, with that call's pos, p and eps: dx of every
+ * tensor, and the sums over tokens (and over heads, where they share weights)
+ * that are dweight.  The sums are fp32 in an order that is the same on every
+ * call with the same sizes.  With tokens 0, dweight becomes zeros.  Two launches on `stream` (one without
+ * dweight).
+ */
+MKV_API mkv_status mkv_norm_rope_grad(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos,
+                                      int64_t pos_axis, int64_t pos_batch, const mkv_rope_params* p, float eps,
+                                      int32_t n_tensors, const mkv_norm_rope_grad_tensor* tensors, void* workspace,
+                                      size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -14,29 +14,14 @@
 // (4 x 32768 tokens, 40 heads of 128 dims: 404 us, 0.98 of 6.8 TB/s).
 #include <algorithm>
 
-#include "common.cuh"
 #include "kernels.h"
-#include "tree.h"
-#include "warp_mma.cuh"
+#include "rope.cuh"
 
 namespace mkv {
 
 namespace {
 
 constexpr int kRopeThreads = 256;
-
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
 
 // A thread has one chunk of 16 dims of a head -- 8 pairs that rotate, or 16
 // dims past rot that are copied -- for one token and the heads slot, slot +
@@ -53,16 +38,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
   const int b = static_cast<int>(tok / a.tokens), t = static_cast<int>(tok % a.tokens);
   const bool turn = c < a.rot / 16;
   float cs[8], sn[8];
-  if (turn) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int f = c * 8 + i;
-      const int32_t p = a.pos[a.axis[f] * a.pos_axis + b * a.pos_batch + t];
-      const uint64_t ang = static_cast<uint64_t>(static_cast<int64_t>(p)) * a.turn[f];
-      const float x = static_cast<float>(static_cast<int32_t>(ang >> 32)) * 0x1p-31f;  // half turns in [-1, 1)
-      sincospif(x, &sn[i], &cs[i]);
-    }
-  }
+  if (turn) chunk_angles(a, c, b, t, cs, sn);
   const int o0 = turn ? (a.neighbours ? c * 16 : c * 8) : c * 16;
   const int o1 = turn && !a.neighbours ? o0 + a.rot / 2 : o0 + 8;
   for (int h = slot; h < a.heads; h += slots) {
@@ -77,21 +53,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
       float x0[8], x1[8], y0[8], y1[8];
       unpack8(v0, x0);
       unpack8(v1, x1);
-      if (a.neighbours) {  // pairs (0, 1), (2, 3), ... of the 16 dims
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          y0[2 * j] = x0[2 * j] * cs[j] - x0[2 * j + 1] * sn[j];
-          y0[2 * j + 1] = x0[2 * j] * sn[j] + x0[2 * j + 1] * cs[j];
-          y1[2 * j] = x1[2 * j] * cs[4 + j] - x1[2 * j + 1] * sn[4 + j];
-          y1[2 * j + 1] = x1[2 * j] * sn[4 + j] + x1[2 * j + 1] * cs[4 + j];
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          y0[j] = x0[j] * cs[j] - x1[j] * sn[j];
-          y1[j] = x0[j] * sn[j] + x1[j] * cs[j];
-        }
-      }
+      turn_chunk<false>(a.neighbours != 0, cs, sn, x0, x1, y0, y1);
       v0 = pack8(y0);
       v1 = pack8(y1);
     }

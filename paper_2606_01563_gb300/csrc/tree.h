@@ -124,4 +124,61 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs& a, int head_dim, int num_sms, cudaStream_t stream);
 
+// --------------------------------------------------------------- norm and rope
+struct NormWeight {
+  const void* p;  // null: ones
+  int64_t head;   // elements from one head's weights to the next (0: the same for all)
+  int32_t f32;    // fp32, else bf16
+};
+struct NormRopeArgs {
+  uint64_t turn[kRopeFreqs];
+  uint8_t axis[kRopeFreqs];
+  RopeTensor x[MKV_ROPE_MAX_TENSORS];
+  NormWeight w[MKV_ROPE_MAX_TENSORS];
+  const int32_t* pos;
+  int64_t pos_axis, pos_batch;
+  int32_t heads;  // of all tensors
+  int32_t batch;
+  int32_t tokens;
+  int32_t rot;
+  int32_t neighbours;
+  float eps;
+};
+cudaError_t launch_norm_rope(const NormRopeArgs& a, int head_dim, int num_sms, cudaStream_t stream);
+
+struct NormRopeGradTensor {
+  const void* x;
+  const void* dy;
+  void* dx;
+  int64_t x_batch, x_token, x_head;
+  int64_t dy_batch, dy_token, dy_head;
+  int64_t dx_batch, dx_token, dx_head;
+  NormWeight w;
+  float* dw;  // [groups][d] or null
+  int32_t heads;
+  int32_t per_head;  // 1: every head has weights of its own
+  // filled by norm_rope_grad_plan
+  int32_t groups;       // weight rows
+  int32_t slots;        // (token, head slot) units of a token in a group
+  int32_t blocks;       // per group
+  int32_t first_block;  // of the tensor's first group
+};
+struct NormRopeGradArgs {
+  uint64_t turn[kRopeFreqs];
+  uint8_t axis[kRopeFreqs];
+  NormRopeGradTensor x[MKV_ROPE_MAX_TENSORS];
+  const int32_t* pos;
+  int64_t pos_axis, pos_batch;
+  float* parts;  // [blocks][d]
+  int32_t tensors;
+  int32_t batch;
+  int32_t tokens;
+  int32_t rot;
+  int32_t neighbours;
+  float eps;
+};
+// Fills the tensors' plans (from heads, per_head, batch and tokens); returns the blocks of all groups.
+int norm_rope_grad_plan(NormRopeGradArgs& a, int head_dim, int num_sms);
+cudaError_t launch_norm_rope_grad(const NormRopeGradArgs& a, int head_dim, int blocks, cudaStream_t stream);
+
 }  // namespace mkv

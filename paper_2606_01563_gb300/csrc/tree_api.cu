@@ -39,6 +39,52 @@ uint64_t turns_of(float w, bool inverse) {
   return inverse ? ~t + 1 : t;
 }
 
+// Sizes and parameters that all rotations share, and the angles' fields of their arguments.
+mkv_status rope_sizes(int32_t batch, int32_t tokens, int32_t head_dim, int32_t n_tensors) {
+  if (head_dim != 64 && head_dim != 128) return MKV_ERR_UNSUPPORTED;
+  if (batch < 1 || tokens < 0 || (int64_t)batch * tokens > ((int64_t)1 << 31) || n_tensors < 1 ||
+      n_tensors > MKV_ROPE_MAX_TENSORS)
+    return MKV_ERR_SHAPE;
+  return MKV_OK;
+}
+template <typename Args>
+mkv_status rope_fill(Args& a, int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
+                     int64_t pos_batch, const mkv_rope_params* p) {
+  if (!p || pos_axis < 0 || pos_batch < 0) return MKV_ERR_INVALID_ARG;
+  if (p->rot_dim < 16 || p->rot_dim > head_dim || p->rot_dim % 16 != 0 || p->n_axes < 1 ||
+      p->n_axes > MKV_ROPE_MAX_AXES || (p->neighbours != 0 && p->neighbours != 1) ||
+      (p->inverse != 0 && p->inverse != 1))
+    return MKV_ERR_INVALID_ARG;
+  for (int f = 0; f < p->rot_dim / 2; ++f) {
+    if (!(std::fabs(p->inv_freq[f]) <= 0x1p20f) || p->axis[f] < 0 || p->axis[f] >= p->n_axes)
+      return MKV_ERR_INVALID_ARG;
+    a.turn[f] = turns_of(p->inv_freq[f], p->inverse != 0);
+    a.axis[f] = static_cast<uint8_t>(p->axis[f]);
+  }
+  if (tokens > 0 && (!pos || !aligned(pos, 4))) return MKV_ERR_INVALID_ARG;  // (empty tensors may have no address)
+  a.pos = pos;
+  a.pos_axis = pos_axis;
+  a.pos_batch = pos_batch;
+  a.batch = batch;
+  a.tokens = tokens;
+  a.rot = p->rot_dim;
+  a.neighbours = p->neighbours;
+  return MKV_OK;
+}
+// A tensor of 16-byte rows; one that is written has a place for every head of every token.
+bool rope_strides_ok(const void* at, int32_t batch, int32_t tokens, int32_t heads, int64_t s_batch, int64_t s_token,
+                     int64_t s_head, bool written) {
+  if (!at || !aligned(at, 16)) return false;
+  for (const int64_t s : {s_batch, s_token, s_head})
+    if (s % 8 != 0 || s < 0) return false;
+  return !written || ((batch == 1 || s_batch != 0) && (tokens == 1 || s_token != 0) && (heads == 1 || s_head != 0));
+}
+bool norm_weight_ok(const void* weight, int64_t head, int32_t f32, int32_t head_dim, NormWeight* w) {
+  *w = NormWeight{weight, head, f32};
+  return (f32 == 0 || f32 == 1) && aligned(weight, 16) &&
+         (head == 0 || (weight != nullptr && head >= head_dim && head % 8 == 0));
+}
+
 }  // namespace
 
 extern "C" {
@@ -166,47 +212,123 @@ mkv_status mkv_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32
                     int64_t pos_batch, const mkv_rope_params* p, int32_t n_tensors, const mkv_rope_tensor* tensors,
                     void* stream) {
   NvtxRange nvtx("mkv_rope");
-  if (head_dim != 64 && head_dim != 128) return MKV_ERR_UNSUPPORTED;
-  if (batch < 1 || tokens < 0 || (int64_t)batch * tokens > ((int64_t)1 << 31) || n_tensors < 1 ||
-      n_tensors > MKV_ROPE_MAX_TENSORS)
-    return MKV_ERR_SHAPE;
-  if (!p || !tensors || pos_axis < 0 || pos_batch < 0) return MKV_ERR_INVALID_ARG;
-  if (p->rot_dim < 16 || p->rot_dim > head_dim || p->rot_dim % 16 != 0 || p->n_axes < 1 ||
-      p->n_axes > MKV_ROPE_MAX_AXES || (p->neighbours != 0 && p->neighbours != 1) ||
-      (p->inverse != 0 && p->inverse != 1))
-    return MKV_ERR_INVALID_ARG;
+  mkv_status chk = rope_sizes(batch, tokens, head_dim, n_tensors);
+  if (chk != MKV_OK) return chk;
+  if (!tensors) return MKV_ERR_INVALID_ARG;
   RopeArgs a{};
-  for (int f = 0; f < p->rot_dim / 2; ++f) {
-    if (!(std::fabs(p->inv_freq[f]) <= 0x1p20f) || p->axis[f] < 0 || p->axis[f] >= p->n_axes)
-      return MKV_ERR_INVALID_ARG;
-    a.turn[f] = turns_of(p->inv_freq[f], p->inverse != 0);
-    a.axis[f] = static_cast<uint8_t>(p->axis[f]);
-  }
-  if (tokens == 0) return MKV_OK;  // (empty tensors may have no address)
-  if (!pos || !aligned(pos, 4)) return MKV_ERR_INVALID_ARG;
+  chk = rope_fill(a, batch, tokens, head_dim, pos, pos_axis, pos_batch, p);
+  if (chk != MKV_OK || tokens == 0) return chk;
   int64_t heads = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const mkv_rope_tensor& t = tensors[i];
-    if (!t.in || !t.out || !aligned(t.in, 16) || !aligned(t.out, 16) || t.heads < 1) return MKV_ERR_INVALID_ARG;
-    for (const int64_t s : {t.in_batch, t.in_token, t.in_head, t.out_batch, t.out_token, t.out_head})
-      if (s % 8 != 0 || s < 0) return MKV_ERR_INVALID_ARG;
-    // two tokens or heads that are written to one place
-    if ((batch > 1 && t.out_batch == 0) || (tokens > 1 && t.out_token == 0) || (t.heads > 1 && t.out_head == 0))
+    if (t.heads < 1 || !rope_strides_ok(t.in, batch, tokens, t.heads, t.in_batch, t.in_token, t.in_head, false) ||
+        !rope_strides_ok(t.out, batch, tokens, t.heads, t.out_batch, t.out_token, t.out_head, true))
       return MKV_ERR_INVALID_ARG;
     heads += t.heads;
     a.x[i] = RopeTensor{t.in,        t.out,       t.in_batch, t.in_token, t.in_head,
                         t.out_batch, t.out_token, t.out_head, t.heads};
   }
   if (heads > 65536) return MKV_ERR_SHAPE;
-  a.pos = pos;
-  a.pos_axis = pos_axis;
-  a.pos_batch = pos_batch;
   a.heads = static_cast<int32_t>(heads);
+  return cuda_status(launch_rope(a, head_dim, num_sms_current(), static_cast<cudaStream_t>(stream)));
+}
+
+// ----------------------------------------------------------- norm and rope
+mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
+                         int64_t pos_batch, const mkv_rope_params* p, float eps, int32_t n_tensors,
+                         const mkv_norm_rope_tensor* tensors, void* stream) {
+  NvtxRange nvtx("mkv_norm_rope");
+  mkv_status chk = rope_sizes(batch, tokens, head_dim, n_tensors);
+  if (chk != MKV_OK) return chk;
+  if (!tensors || !(eps > 0.f) || !std::isfinite(eps)) return MKV_ERR_INVALID_ARG;
+  NormRopeArgs a{};
+  chk = rope_fill(a, batch, tokens, head_dim, pos, pos_axis, pos_batch, p);
+  if (chk != MKV_OK) return chk;
+  if (p->inverse != 0) return MKV_ERR_INVALID_ARG;
+  if (tokens == 0) return MKV_OK;
+  int64_t heads = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const mkv_rope_tensor& t = tensors[i].t;
+    if (t.heads < 1 || !rope_strides_ok(t.in, batch, tokens, t.heads, t.in_batch, t.in_token, t.in_head, false) ||
+        !rope_strides_ok(t.out, batch, tokens, t.heads, t.out_batch, t.out_token, t.out_head, true) ||
+        !norm_weight_ok(tensors[i].weight, tensors[i].weight_head, tensors[i].weight_f32, head_dim, &a.w[i]))
+      return MKV_ERR_INVALID_ARG;
+    heads += t.heads;
+    a.x[i] = RopeTensor{t.in,        t.out,       t.in_batch, t.in_token, t.in_head,
+                        t.out_batch, t.out_token, t.out_head, t.heads};
+  }
+  if (heads > 65536) return MKV_ERR_SHAPE;
+  a.heads = static_cast<int32_t>(heads);
+  a.eps = eps;
+  return cuda_status(launch_norm_rope(a, head_dim, num_sms_current(), static_cast<cudaStream_t>(stream)));
+}
+
+// heads of all tensors, and the plan's blocks (0: a tensor without heads, or too many)
+static int norm_rope_grad_blocks(NormRopeGradArgs& a, int32_t batch, int32_t tokens, int32_t head_dim,
+                                 int32_t n_tensors, const mkv_norm_rope_grad_tensor* tensors) {
   a.batch = batch;
   a.tokens = tokens;
-  a.rot = p->rot_dim;
-  a.neighbours = p->neighbours;
-  return cuda_status(launch_rope(a, head_dim, num_sms_current(), static_cast<cudaStream_t>(stream)));
+  a.tensors = n_tensors;
+  int64_t heads = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (tensors[i].heads < 1) return 0;
+    heads += tensors[i].heads;
+    a.x[i].heads = tensors[i].heads;
+    a.x[i].per_head = tensors[i].weight_head != 0;
+  }
+  return heads > 65536 ? 0 : norm_rope_grad_plan(a, head_dim, num_sms_current());
+}
+
+size_t mkv_norm_rope_grad_workspace_size(int32_t batch, int32_t tokens, int32_t head_dim, int32_t n_tensors,
+                                         const mkv_norm_rope_grad_tensor* tensors) {
+  if (rope_sizes(batch, tokens, head_dim, n_tensors) != MKV_OK || !tensors) return 0;
+  NormRopeGradArgs a{};
+  const int blocks = norm_rope_grad_blocks(a, batch, tokens, head_dim, n_tensors, tensors);
+  return blocks == 0 ? 0 : kHeaderBytes + (size_t)blocks * head_dim * sizeof(float);
+}
+
+mkv_status mkv_norm_rope_grad(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
+                              int64_t pos_batch, const mkv_rope_params* p, float eps, int32_t n_tensors,
+                              const mkv_norm_rope_grad_tensor* tensors, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  NvtxRange nvtx("mkv_norm_rope_grad");
+  mkv_status chk = rope_sizes(batch, tokens, head_dim, n_tensors);
+  if (chk != MKV_OK) return chk;
+  if (!tensors || !(eps > 0.f) || !std::isfinite(eps)) return MKV_ERR_INVALID_ARG;
+  NormRopeGradArgs a{};
+  chk = rope_fill(a, batch, tokens, head_dim, pos, pos_axis, pos_batch, p);
+  if (chk != MKV_OK) return chk;
+  if (p->inverse != 0) return MKV_ERR_INVALID_ARG;
+  bool wanted = false;
+  for (int i = 0; i < n_tensors; ++i) {
+    const mkv_norm_rope_grad_tensor& t = tensors[i];
+    NormRopeGradTensor& x = a.x[i];
+    if (t.heads < 1 || !norm_weight_ok(t.weight, t.weight_head, t.weight_f32, head_dim, &x.w) ||
+        !aligned(t.dweight, 4) || (t.dweight && !t.weight))
+      return MKV_ERR_INVALID_ARG;
+    if (tokens > 0 &&
+        (!rope_strides_ok(t.x, batch, tokens, t.heads, t.x_batch, t.x_token, t.x_head, false) ||
+         !rope_strides_ok(t.dy, batch, tokens, t.heads, t.dy_batch, t.dy_token, t.dy_head, false) ||
+         !rope_strides_ok(t.dx, batch, tokens, t.heads, t.dx_batch, t.dx_token, t.dx_head, true)))
+      return MKV_ERR_INVALID_ARG;
+    x.x = t.x;
+    x.dy = t.dy;
+    x.dx = t.dx;
+    x.x_batch = t.x_batch, x.x_token = t.x_token, x.x_head = t.x_head;
+    x.dy_batch = t.dy_batch, x.dy_token = t.dy_token, x.dy_head = t.dy_head;
+    x.dx_batch = t.dx_batch, x.dx_token = t.dx_token, x.dx_head = t.dx_head;
+    x.dw = t.dweight;
+    wanted |= t.dweight != nullptr;
+  }
+  const int blocks = norm_rope_grad_blocks(a, batch, tokens, head_dim, n_tensors, tensors);
+  if (blocks == 0) return MKV_ERR_SHAPE;
+  if (tokens == 0 && !wanted) return MKV_OK;
+  if (!workspace || workspace_bytes < kHeaderBytes + (size_t)blocks * head_dim * sizeof(float) ||
+      !aligned(workspace, 256))
+    return MKV_ERR_WORKSPACE;
+  a.eps = eps;
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
+  return cuda_status(launch_norm_rope_grad(a, head_dim, blocks, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -67,6 +67,17 @@ class mkv_rope_tensor(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("in_batch", "in_token", "in_head", "out_batch", "out_token", "out_head")]
 
 
+class mkv_norm_rope_tensor(ctypes.Structure):
+    _fields_ = [("t", mkv_rope_tensor), ("weight", c_vp), ("weight_head", ctypes.c_int64), ("weight_f32", c_i32)]
+
+
+class mkv_norm_rope_grad_tensor(ctypes.Structure):
+    _fields_ = [("x", c_vp), ("dy", c_vp), ("dx", c_vp), ("heads", c_i32)] + [
+        (n, ctypes.c_int64) for n in ("x_batch", "x_token", "x_head", "dy_batch", "dy_token", "dy_head", "dx_batch",
+                                      "dx_token", "dx_head")] + [
+        ("weight", c_vp), ("weight_head", ctypes.c_int64), ("weight_f32", c_i32), ("dweight", c_vp)]
+
+
 STATUS = {0: "MKV_OK", 1: "MKV_ERR_INVALID_ARG", 2: "MKV_ERR_SHAPE", 3: "MKV_ERR_CAPACITY",
           4: "MKV_ERR_CUDA", 5: "MKV_ERR_TIMEOUT", 6: "MKV_ERR_UNSUPPORTED", 7: "MKV_ERR_WORKSPACE"}
 
@@ -75,7 +86,8 @@ EXPORTS = ("mkv_status_str", "mkv_version", "mkv_compress_workspace_size", "mkv_
            "mkv_evict_append", "mkv_get_device_error", "mkv_decode_step_noalloc", "mkv_moments_pack_bf16",
            "mkv_decode_evict_workspace_size", "mkv_decode_evict_step", "mkv_moments_pack_split")
 # declared in include/mkv_tree.h
-TREE_EXPORTS = ("mkv_tree_build", "mkv_tree_workspace_size", "mkv_tree_step", "mkv_tree_commit", "mkv_rope")
+TREE_EXPORTS = ("mkv_tree_build", "mkv_tree_workspace_size", "mkv_tree_step", "mkv_tree_commit", "mkv_rope",
+                "mkv_norm_rope", "mkv_norm_rope_grad_workspace_size", "mkv_norm_rope_grad")
 # test hooks declared in include/mkv_debug.h
 DEBUG_EXPORTS = ("mkv_debug_set_poll_limit", "mkv_debug_force_ticket_merge")
 
@@ -145,6 +157,14 @@ def lib():
                                       c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.mkv_rope.restype = c_i32
         L.mkv_rope.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params), c_i32, c_vp, c_vp]
+        L.mkv_norm_rope.restype = c_i32
+        L.mkv_norm_rope.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params),
+                                    ctypes.c_float, c_i32, c_vp, c_vp]
+        L.mkv_norm_rope_grad_workspace_size.restype = ctypes.c_size_t
+        L.mkv_norm_rope_grad_workspace_size.argtypes = [c_i32, c_i32, c_i32, c_i32, c_vp]
+        L.mkv_norm_rope_grad.restype = c_i32
+        L.mkv_norm_rope_grad.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params),
+                                         ctypes.c_float, c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.mkv_debug_set_poll_limit.restype = ctypes.c_int64
         L.mkv_debug_set_poll_limit.argtypes = [ctypes.c_int64]
         L.mkv_debug_force_ticket_merge.restype = c_i32
@@ -508,6 +528,110 @@ def mkv_rope(pos, p: mkv_rope_params, tensors, inverse=False, stream=None):
                           _I64x9[len(tensors)](*flat), _stream(stream))
     if code:
         _check(code, "mkv_rope")
+
+
+_I64x12, _I64x17 = ([ctypes.c_int64 * (m * n) for n in range(5)] for m in (12, 17))
+
+
+def _here(*tensors):
+    """Refuses tensors that are not on the current device: the kernels run there, on its stream."""
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"tensors on the current device (cuda:{at}), not on {t.device}")
+
+
+def _positions(pos, p):
+    """Checks pos [axes, b, tokens] and returns b, tokens and the strides of axes and batch items."""
+    _need(pos.dim() == 3, "pos: int32 [axes, b, tokens] with adjacent tokens")
+    axes, b, t = pos.shape
+    ps = pos.stride()
+    if pos.dtype is not torch.int32 or axes < p.n_axes or (ps[2] != 1 and t > 1):
+        raise ValueError("pos: int32 [axes, b, tokens] with adjacent tokens")
+    return b, t, ps[0], ps[1] if b > 1 else 0
+
+
+def _rows(t, b, tokens, d):
+    """The heads of a bf16 [b, tokens, heads, d] tensor with adjacent dims, and its strides in elements."""
+    shape, s = t.shape, t.stride()
+    if t.dtype is not _BF16 or len(shape) != 4 or shape[0] != b or shape[1] != tokens or shape[3] != d or s[3] != 1:
+        raise ValueError("tensors: bf16 [b, tokens, heads, d] with adjacent dims")
+    h = shape[2]
+    # (a stride over an extent of one is never used)
+    return h, s[0] if b > 1 else 0, s[1] if tokens > 1 else 0, s[2] if h > 1 else 0
+
+
+def _norm_weight(w, heads, d):
+    """(address, elements from head to head, fp32 or not) of a norm's weights [d] or [heads, d], or None."""
+    if w is None:
+        return 0, 0, 0
+    if w.dtype not in (_BF16, torch.float32) or w.shape not in ((d,), (heads, d)) or w.stride(-1) != 1:
+        raise ValueError("weights: bf16 or float32, [d] or [heads, d] with adjacent dims")
+    step = w.stride(0) if w.dim() == 2 else 0
+    if w.dim() == 2 and step == 0 and heads > 1:
+        raise ValueError("weights: [heads, d] not expanded over heads ([d] is one row for all)")
+    return w.data_ptr(), step or (d if w.dim() == 2 else 0), int(w.dtype is torch.float32)
+
+
+def mkv_norm_rope(pos, p: mkv_rope_params, tensors, eps, stream=None):
+    """Norms per head, then rotation: (in, out, weight) of every tensor, in and out as in mkv_rope, weight bf16 or
+    float32 [d] or [heads, d], or None (ones); eps is added to the mean square."""
+    b, t, pa, pb = _positions(pos, p)
+    if not 0 < len(tensors) < 5:
+        raise ValueError("tensors: one to four (in, out, weight)")
+    d = tensors[0][0].shape[-1]
+    flat = []
+    for x, y, w in tensors:
+        hx, *xs = _rows(x, b, t, d)
+        hy, *ys = _rows(y, b, t, d)
+        if hx != hy:
+            raise ValueError("tensors: in and out of the same shape")
+        at, step, f32 = _norm_weight(w, hx, d)
+        _here(pos, x, y, w)
+        flat += (x.data_ptr(), y.data_ptr(), hx, *xs, *ys, at, step, f32)
+    code = lib().mkv_norm_rope(b, t, d, pos.data_ptr(), pa, pb, p, eps, len(tensors), _I64x12[len(tensors)](*flat),
+                               _stream(stream))
+    if code:
+        _check(code, "mkv_norm_rope")
+
+
+def _grad_tensors(tensors, b, t, d):
+    """The C structures of mkv_norm_rope_grad's tensors, checked."""
+    if not 0 < len(tensors) < 5:
+        raise ValueError("tensors: one to four (x, dy, dx, weight, dweight)")
+    flat = []
+    for x, dy, dx, w, dw in tensors:
+        hx, *xs = _rows(x, b, t, d)
+        hy, *ys = _rows(dy, b, t, d)
+        hd, *ds = _rows(dx, b, t, d)
+        if hx != hy or hx != hd:
+            raise ValueError("tensors: x, dy and dx of the same shape")
+        at, step, f32 = _norm_weight(w, hx, d)
+        if dw is not None and (w is None or dw.dtype is not torch.float32 or dw.shape != w.shape or not dw.is_contiguous()):
+            raise ValueError("dweight: contiguous float32 of the weights' shape")
+        flat += (x.data_ptr(), dy.data_ptr(), dx.data_ptr(), hx, *xs, *ys, *ds, at, step, f32,
+                 0 if dw is None else dw.data_ptr())
+    return _I64x17[len(tensors)](*flat)
+
+
+def mkv_norm_rope_grad_workspace_size(tensors):
+    """Bytes for mkv_norm_rope_grad of these tensors."""
+    b, t, _, d = tensors[0][0].shape
+    return lib().mkv_norm_rope_grad_workspace_size(b, t, d, len(tensors), _grad_tensors(tensors, b, t, d))
+
+
+def mkv_norm_rope_grad(pos, p: mkv_rope_params, tensors, eps, ws, stream=None):
+    """The gradient of mkv_norm_rope: (x, dy, dx, weight, dweight) of every tensor, x, dy and dx bf16 [b, tokens, heads,
+    d] with adjacent dims (dx may be x or dy), dweight float32 of the weights' shape, overwritten, or None."""
+    b, t, pa, pb = _positions(pos, p)
+    d = tensors[0][0].shape[-1] if tensors else 0
+    flat = _grad_tensors(tensors, b, t, d)
+    for tensor in tensors:
+        _here(pos, ws, *tensor)
+    code = lib().mkv_norm_rope_grad(b, t, d, pos.data_ptr(), pa, pb, p, eps, len(tensors), flat, ws.data_ptr(),
+                                    ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_norm_rope_grad")
 
 
 def mkv_debug_set_poll_limit(polls):
