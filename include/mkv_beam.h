@@ -1,0 +1,97 @@
+/*
+ * mkv_beam.h -- several continuations of one compressed prompt (beam search,
+ * parallel sampling): the calls that sit beside mkv.h's in such a serving step.
+ *
+ *   mkv_beam_select   beam search's selection over beams and vocabulary
+ *   mkv_beam_reorder  the selected beams' states (caches, and moments where
+ *                     there are any) in every layer, in place
+ *
+ * Conventions are those of mkv.h (device pointers, caller-owned memory,
+ * stream order, statuses, the workspace's error word read by
+ * mkv_get_device_error), except that these tensors may be strided as stated.
+ */
+#ifndef MKV_BEAM_H
+#define MKV_BEAM_H
+
+#include "mkv.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define MKV_BEAM_MAX_SEQS 256 /* sequences of a prompt (mkv_beam_reorder) */
+#define MKV_BEAM_MAX_BEAMS 64 /* beams of a batch item (mkv_beam_select)                   */
+#define MKV_BEAM_MAX_OUT 64   /* continuations that it selects                             */
+
+/* The scores of every beam's continuations, read on the host during the call. */
+typedef struct {
+  const void* logits;    /* bf16 or fp32 [batch, beams, vocab]: adjacent tokens, strides below      */
+  int32_t f32;           /* 1: fp32 logits; 0: bf16                                                */
+  int64_t logits_batch;  /* elements from batch item to batch item, any value at least 0           */
+  int64_t logits_beam;   /* and from beam to beam                                                  */
+  const float* score;    /* fp32 [batch, beams]: a beam's score so far; -infinity: not alive       */
+  const int32_t* done;   /* int32 [batch, beams] optional: not 0 where a beam has ended            */
+  int32_t end_token;     /* the token that ends a beam, 0..vocab-1, or -1: none (done is then NULL) */
+} mkv_beam_scores;
+
+/*
+ * Bytes of device workspace mkv_beam_select needs on the current device.
+ * Returns 0 if the arguments are invalid.  Only its first 256 bytes need to be zero before its first use.
+ */
+MKV_API size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out);
+
+/*
+ * The n_out best continuations of every batch item, best first.  A live beam
+ * that has not ended continues with token t at score[beam] + logit[t] -
+ * log sum exp(logits of the beam); one that has ended continues only with
+ * end_token, at its own score (its logits are not read).  Equal ones: the lower beam, then the lower token.
+ *   parent     int32 [batch, n_out]  the beam that is continued
+ *   token      int32 [batch, n_out]  by which token
+ *   score_out  fp32  [batch, n_out]
+ *   done_out   int32 [batch, n_out]  optional: 1 where the beam had ended or the token is end_token
+ * Tokens with a logit of -infinity, and beams whose logits all are, do not take
+ * part.  Where there are fewer continuations than n_out, the slots that are left have parent and
+ * token -1, score -infinity and done 0.  A live beam with a logit that is NaN
+ * or +infinity, or a score that is, takes no part and is recorded as
+ * MKV_ERR_INVALID_ARG (info: batch item * beams + beam).
+ * Sums of exponentials, their logs and the scores are joined in fp64; a term's error of about 1e-7
+ * decides between continuations that are nearer to each other than that.
+ * score_out may be score, and done_out may be done, where n_out = beams; else
+ * outputs do not overlap inputs.
+ * Requirements: batch 1..65535, beams 1..64, n_out 1..64, vocab 1..2^24; logits aligned to their
+ * type, the others to 4 bytes; workspace 256.
+ */
+MKV_API mkv_status mkv_beam_select(int32_t batch, int32_t beams, int32_t vocab, const mkv_beam_scores* scores,
+                                   int32_t n_out, int32_t* parent, int32_t* token, float* score_out, int32_t* done_out,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* One layer's states: (b * N) * h_kv units.  mom.n NULL: no moments. */
+typedef struct {
+  mkv_cache cache;
+  mkv_moments mom;
+} mkv_beam_layer;
+
+/*
+ * Slot j of batch item i takes the state that slot parent[i][j] has, in every
+ * layer, in place: rows 0..len-1 of K, V and pos, len and seen, with y and
+ * y_len where the cache has them (rows 0..y_len-1), and the moments where given.  Rows at or above the new
+ * length are left as they are.  Packed copies of C (mkv_moments_pack_bf16,
+ * mkv_moments_pack_split) are the caller's to make again.  geom.batch is the
+ * number of batch items b; geom's group is not used.
+ *   n_seqs  N: slots per batch item, 1..256
+ *   parent  int32 [b, N]  0..N-1, several slots may have the same; -1: the slot stays as it is
+ *   layers  HOST array of n_layers entries, copied during the call
+ * A batch item with another parent is left as it is and recorded as
+ * MKV_ERR_INVALID_ARG (info: the batch item); a length outside 0..capacity is
+ * recorded as MKV_ERR_CAPACITY and rows are copied up to the nearer end.
+ * Requirements: b * h_kv <= 65535 (else MKV_ERR_SHAPE); as mkv_cache and mkv_moments.
+ * The workspace is 256 bytes, zero-filled before its first use.  Two launches for every 64 layers.
+ */
+MKV_API mkv_status mkv_beam_reorder(mkv_geom geom, int32_t n_seqs, int32_t n_layers, const mkv_beam_layer* layers,
+                                    const int32_t* parent, void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* MKV_BEAM_H */

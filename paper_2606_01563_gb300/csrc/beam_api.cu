@@ -1,0 +1,110 @@
+// C-ABI entry points declared in include/mkv_beam.h: argument validation,
+// workspace sizing and kernel dispatch.
+#include <string.h>
+
+#include "beam.h"
+#include "common.cuh"
+#include "kernels.h"
+#include "validate.h"
+
+using namespace mkv;
+
+namespace {
+
+mkv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MKV_OK : MKV_ERR_CUDA; }
+
+bool select_sizes_ok(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out) {
+  return batch >= 1 && batch <= 65535 && beams >= 1 && beams <= MKV_BEAM_MAX_BEAMS && vocab >= 1 &&
+         vocab <= (1 << 24) && n_out >= 1 && n_out <= MKV_BEAM_MAX_OUT;
+}
+
+}  // namespace
+
+extern "C" {
+
+// ------------------------------------------------------------------ select
+size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out) {
+  if (!select_sizes_ok(batch, beams, vocab, n_out)) return 0;
+  SelectArgs a{};
+  a.beams = beams;
+  a.vocab = vocab;
+  a.out = n_out;
+  return select_plan(a, batch, num_sms_current(), nullptr);
+}
+
+mkv_status mkv_beam_select(int32_t batch, int32_t beams, int32_t vocab, const mkv_beam_scores* s, int32_t n_out,
+                           int32_t* parent, int32_t* token, float* score_out, int32_t* done_out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  NvtxRange nvtx("mkv_beam_select");
+  if (!select_sizes_ok(batch, beams, vocab, n_out)) return MKV_ERR_SHAPE;
+  if (!s || !s->logits || !s->score || !parent || !token || !score_out) return MKV_ERR_INVALID_ARG;
+  if ((s->f32 != 0 && s->f32 != 1) || !aligned(s->logits, s->f32 ? 4 : 2) || !aligned(s->score, 4) ||
+      !aligned(s->done, 4) || !aligned(parent, 4) || !aligned(token, 4) || !aligned(score_out, 4) ||
+      !aligned(done_out, 4))
+    return MKV_ERR_INVALID_ARG;
+  if (s->logits_batch < 0 || s->logits_beam < 0 || s->end_token < -1 || s->end_token >= vocab ||
+      (s->done && s->end_token < 0))
+    return MKV_ERR_INVALID_ARG;
+  SelectArgs a{};
+  a.logits = s->logits;
+  a.s_batch = s->logits_batch;
+  a.s_beam = s->logits_beam;
+  a.score = s->score;
+  a.done = s->done;
+  a.end = s->end_token;
+  a.beams = beams;
+  a.vocab = vocab;
+  a.out = n_out;
+  a.parent = parent;
+  a.token = token;
+  a.score_out = score_out;
+  a.done_out = done_out;
+  if (!workspace || !aligned(workspace, 256) ||
+      workspace_bytes < select_plan(a, batch, num_sms_current(), workspace))
+    return MKV_ERR_WORKSPACE;
+  return cuda_status(launch_beam_select(a, batch, s->f32 != 0, static_cast<cudaStream_t>(stream)));
+}
+
+// ----------------------------------------------------------------- reorder
+mkv_status mkv_beam_reorder(mkv_geom geom, int32_t n_seqs, int32_t n_layers, const mkv_beam_layer* layers,
+                            const int32_t* parent, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange nvtx("mkv_beam_reorder");
+  if (!geom_ok(geom)) return geom_status(geom);
+  if (n_seqs < 1 || n_seqs > MKV_BEAM_MAX_SEQS || (long)geom.batch * geom.n_kv_heads > 65535) return MKV_ERR_SHAPE;
+  if (n_layers < 0 || !layers || !parent || !aligned(parent, 4)) return MKV_ERR_INVALID_ARG;
+  for (int i = 0; i < n_layers; ++i)
+    if (!cache_ok(&layers[i].cache) || (layers[i].mom.n && !moments_ok(&layers[i].mom))) return MKV_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < kHeaderBytes || !aligned(workspace, 256)) return MKV_ERR_WORKSPACE;
+  ReorderArgs a{};
+  a.parent = parent;
+  a.N = n_seqs;
+  a.n_kv = geom.n_kv_heads;
+  a.D = geom.head_dim;
+  a.ws = workspace;
+  const int sms = num_sms_current();
+  for (int first = 0; first < n_layers; first += kReorderLayers) {
+    const int n = n_layers - first < kReorderLayers ? n_layers - first : kReorderLayers;
+    for (int i = 0; i < n; ++i) {
+      const mkv_cache& c = layers[first + i].cache;
+      const mkv_moments& m = layers[first + i].mom;
+      ReorderLayer& l = a.layer[i];
+      l.big[0] = static_cast<uint8_t*>(c.K);
+      l.big[1] = static_cast<uint8_t*>(c.V);
+      l.big[2] = reinterpret_cast<uint8_t*>(c.y);
+      l.big[3] = m.n ? reinterpret_cast<uint8_t*>(m.C) : nullptr;
+      l.pos = c.pos;
+      l.len = c.len;
+      l.seen = c.seen;
+      l.y_len = c.y_len;
+      l.n = m.n;
+      l.mu_k = m.n ? reinterpret_cast<int32_t*>(m.mu_k) : nullptr;
+      l.mu_v = m.n ? reinterpret_cast<int32_t*>(m.mu_v) : nullptr;
+      l.cap = c.capacity;
+    }
+    const cudaError_t e = launch_beam_reorder(a, n, geom.batch, sms, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_status(e);
+  }
+  return MKV_OK;
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""Python binding of the MomentKV C ABI (include/mkv.h, include/mkv_tree.h).
+"""Python binding of the MomentKV C ABI (include/mkv.h, include/mkv_tree.h, include/mkv_beam.h).
 
 Argument marshalling only: every function forwards to the function of the
 same name in libmkv.so, passing device pointers of torch tensors; all work
@@ -78,6 +78,15 @@ class mkv_norm_rope_grad_tensor(ctypes.Structure):
         ("weight", c_vp), ("weight_head", ctypes.c_int64), ("weight_f32", c_i32), ("dweight", c_vp)]
 
 
+class mkv_beam_scores(ctypes.Structure):
+    _fields_ = [("logits", c_vp), ("f32", c_i32), ("logits_batch", ctypes.c_int64), ("logits_beam", ctypes.c_int64),
+                ("score", c_vp), ("done", c_vp), ("end_token", c_i32)]
+
+
+class mkv_beam_layer(ctypes.Structure):
+    _fields_ = [("cache", mkv_cache), ("mom", mkv_moments)]
+
+
 STATUS = {0: "MKV_OK", 1: "MKV_ERR_INVALID_ARG", 2: "MKV_ERR_SHAPE", 3: "MKV_ERR_CAPACITY",
           4: "MKV_ERR_CUDA", 5: "MKV_ERR_TIMEOUT", 6: "MKV_ERR_UNSUPPORTED", 7: "MKV_ERR_WORKSPACE"}
 
@@ -88,6 +97,8 @@ EXPORTS = ("mkv_status_str", "mkv_version", "mkv_compress_workspace_size", "mkv_
 # declared in include/mkv_tree.h
 TREE_EXPORTS = ("mkv_tree_build", "mkv_tree_workspace_size", "mkv_tree_step", "mkv_tree_commit", "mkv_rope",
                 "mkv_norm_rope", "mkv_norm_rope_grad_workspace_size", "mkv_norm_rope_grad")
+# declared in include/mkv_beam.h
+BEAM_EXPORTS = ("mkv_beam_select_workspace_size", "mkv_beam_select", "mkv_beam_reorder")
 # test hooks declared in include/mkv_debug.h
 DEBUG_EXPORTS = ("mkv_debug_set_poll_limit", "mkv_debug_force_ticket_merge")
 
@@ -165,6 +176,13 @@ def lib():
         L.mkv_norm_rope_grad.restype = c_i32
         L.mkv_norm_rope_grad.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params),
                                          ctypes.c_float, c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
+        L.mkv_beam_select_workspace_size.restype = ctypes.c_size_t
+        L.mkv_beam_select_workspace_size.argtypes = [c_i32, c_i32, c_i32, c_i32]
+        L.mkv_beam_select.restype = c_i32
+        L.mkv_beam_select.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
+        L.mkv_beam_reorder.restype = c_i32
+        L.mkv_beam_reorder.argtypes = [mkv_geom, c_i32, c_i32, ctypes.POINTER(mkv_beam_layer), c_vp, c_vp,
+                                       ctypes.c_size_t, c_vp]
         L.mkv_debug_set_poll_limit.restype = ctypes.c_int64
         L.mkv_debug_set_poll_limit.argtypes = [ctypes.c_int64]
         L.mkv_debug_force_ticket_merge.restype = c_i32
@@ -277,6 +295,14 @@ class TreeLayers:
     array: ctypes.Array
     tree: mkv_tree
     batch: int
+    held: list
+
+
+@dataclass
+class BeamLayers:
+    """The layers of a reordering (beam_layers): what mkv_beam_reorder takes, with the tensors it points into."""
+    array: ctypes.Array
+    shape: tuple
     held: list
 
 
@@ -632,6 +658,81 @@ def mkv_norm_rope_grad(pos, p: mkv_rope_params, tensors, eps, ws, stream=None):
                                     ws.numel(), _stream(stream))
     if code:
         _check(code, "mkv_norm_rope_grad")
+
+
+# --------------------------------------------- several continuations of a prompt
+def mkv_beam_select_workspace_size(batch, beams, vocab, n_out):
+    return lib().mkv_beam_select_workspace_size(batch, beams, vocab, n_out)
+
+
+def mkv_beam_select(logits, score, parent, token, score_out, ws, done=None, done_out=None, end_token=-1, stream=None):
+    """The best continuations of every batch item: logits bf16 or float32 [b, beams, vocab] (adjacent tokens), score
+    float32 [b, beams], done int32 [b, beams] or None -> parent, token int32 [b, n_out], score_out float32, done_out
+    int32 or None."""
+    shape, ls, lt = logits.shape, logits.stride(), logits.dtype
+    if len(shape) != 3 or (lt is not _BF16 and lt is not torch.float32) or (ls[2] != 1 and shape[2] > 1):
+        raise ValueError("logits: bf16 or float32 [b, beams, vocab] with adjacent tokens")
+    b, beams, vocab = shape
+    rows, out = (b, beams), parent.shape
+    _need(len(out) == 2 and out[0] == b, "parent: int32 [b, n_out]")
+    for t, of, what in ((score, rows, "score"), (score_out, out, "score_out")):
+        if t.dtype is not torch.float32 or t.shape != of or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous float32 {list(of)}")
+    _int32(parent, out, "parent")
+    _int32(token, out, "token")
+    if done is not None:
+        _int32(done, rows, "done")
+    if done_out is not None:
+        _int32(done_out, out, "done_out")
+    _here(logits, score, done, parent, token, score_out, done_out, ws)
+    # (strides over an extent of one are never used)
+    s = _I64x7(logits.data_ptr(), int(lt is torch.float32), ls[0] if b > 1 else 0, ls[1] if beams > 1 else 0,
+               score.data_ptr(), 0 if done is None else done.data_ptr(), end_token)
+    code = lib().mkv_beam_select(b, beams, vocab, s, out[1], parent.data_ptr(), token.data_ptr(), score_out.data_ptr(),
+                                 _ptr(done_out), ws.data_ptr(), ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_beam_select")
+
+
+def beam_layers(layers):
+    """(cache, moments or None) of every layer's states, [b * N, h_kv, ...] each.  It holds their addresses: made once
+    and kept beside the caches."""
+    layers = list(layers)
+    _need(len(layers) > 0, "at least one layer")
+    k = layers[0][0].K.shape
+    states, h, d = k[0], k[1], k[3]
+    for c, m in layers:
+        cap = c.K.shape
+        _need(len(cap) == 4 and (cap[0], cap[1], cap[3]) == (states, h, d) and c.V.shape == cap
+              and c.pos.shape == cap[:3] and c.len.shape == cap[:2] and c.seen.shape == cap[:2],
+              "caches of the same states, heads and dims in every layer")
+        _need(all(t.is_contiguous() for t in (c.K, c.V, c.pos, c.len, c.seen)) and c.K.dtype is _BF16
+              and c.V.dtype is _BF16 and all(t.dtype is torch.int32 for t in (c.pos, c.len, c.seen)),
+              "caches: contiguous K, V (bf16), pos, len and seen (int32)")
+        if c.y is not None:
+            _need(c.y.shape == cap and c.y.dtype is torch.float32 and c.y.is_contiguous(), "y: contiguous float32 like K")
+            _int32(c.y_len, cap[:2], "y_len")
+        if m is not None:
+            _int32(m.n, cap[:2], "n")
+            for t, of, what in ((m.mu_k, (states, h, d), "mu_k"), (m.mu_v, (states, h, d), "mu_v"), (m.C, (states, h, d, d), "C")):
+                _need(t.shape == of and t.dtype is torch.float32 and t.is_contiguous(), f"{what}: contiguous float32 {list(of)}")
+            _here(m.n, m.mu_k, m.mu_v, m.C)
+        _here(c.K, c.V, c.pos, c.len, c.seen, c.y, c.y_len)
+    array = (mkv_beam_layer * len(layers))(*(mkv_beam_layer(c.c(), mkv_moments() if m is None else m.c()) for c, m in layers))
+    return BeamLayers(array, (states, h, d), layers)
+
+
+def mkv_beam_reorder(g, layers: BeamLayers, parent, ws, stream=None):
+    """Slot j of batch item i takes the state of slot parent[i, j] (int32 [b, N]; -1: stays) in every layer, in place."""
+    _need(parent.dim() == 2, "parent: int32 [b, N]")
+    b, n = parent.shape
+    _int32(parent, (g.batch, n), "parent")
+    _need(layers.shape == (b * n, g.n_kv_heads, g.head_dim), "layers: states [b * N, h_kv] of this geometry")
+    _here(parent, ws)
+    code = lib().mkv_beam_reorder(g, n, len(layers.array), layers.array, parent.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  _stream(stream))
+    if code:
+        _check(code, "mkv_beam_reorder")
 
 
 def mkv_debug_set_poll_limit(polls):
