@@ -2,9 +2,20 @@
  * mkv_beam.h -- several continuations of one compressed prompt (beam search,
  * parallel sampling): the calls that sit beside mkv.h's in such a serving step.
  *
+ * A batch item is a prompt; N sequences continue it.  The prompt's retained rows and
+ * moments (mkv_compress) are held once per prompt and shared; each sequence has
+ * a tail, an mkv_cache of its own for the tokens generated since.
+ *
+ *   mkv_prefix_step   one decoding step of all sequences: attention over the
+ *                     shared rows and moments, read once for all of them, and
+ *                     over each sequence's tail, which the new token joins
  *   mkv_beam_select   beam search's selection over beams and vocabulary
  *   mkv_beam_reorder  the selected beams' states (caches, and moments where
  *                     there are any) in every layer, in place
+ *
+ * In beam search a step runs mkv_norm_rope or mkv_rope (mkv_tree.h) on the new
+ * tokens' queries and keys and mkv_prefix_step, for every layer, then
+ * mkv_beam_select on the model's logits and mkv_beam_reorder on the tails.
  *
  * Conventions are those of mkv.h (device pointers, caller-owned memory,
  * stream order, statuses, the workspace's error word read by
@@ -19,9 +30,70 @@
 extern "C" {
 #endif
 
-#define MKV_BEAM_MAX_SEQS 256 /* sequences of a prompt (mkv_beam_reorder) */
+#define MKV_BEAM_MAX_SEQS 256 /* sequences of a prompt (mkv_prefix_step, mkv_beam_reorder) */
 #define MKV_BEAM_MAX_BEAMS 64 /* beams of a batch item (mkv_beam_select)                   */
 #define MKV_BEAM_MAX_OUT 64   /* continuations that it selects                             */
+
+/*
+ * The sequences of every prompt.
+ *   n_seqs  N: sequences per prompt in the tensors, 1..256
+ *   count   int32 [b]  optional: the sequences in use of each prompt, 0..N (NULL: all N).  The outputs of
+ *           those at or above it are zeros and their lse -infinity, and their
+ *           tails are neither read nor changed.  A count outside 0..N is taken
+ *           as the nearer end and recorded as MKV_ERR_INVALID_ARG.
+ * Strides of the tensors below, in elements; 0 stands for the dense value.
+ * All are multiples of 8 and not below it.
+ *   q_seq, q_batch    q [b, N, g*h_kv, d]: from sequence to sequence (dense
+ *                     g*h_kv*d), from prompt to prompt (dense N * q_seq)
+ *   kv_seq, kv_batch  k_new and v_new [b, N, h_kv, d] (dense h_kv*d, N * kv_seq)
+ */
+typedef struct {
+  int32_t n_seqs;
+  const int32_t* count;
+  int64_t q_seq;
+  int64_t q_batch;
+  int64_t kv_seq;
+  int64_t kv_batch;
+} mkv_seqs;
+
+/*
+ * Bytes of device workspace mkv_prefix_step needs for this geometry (batch:
+ * prompts), N and capacities of the shared and the tail caches on the current
+ * device, and for every smaller batch, N and capacity.
+ * Returns 0 if the arguments are invalid.  The workspace must be zero-filled
+ * before its first use; every call leaves it ready for the next one.
+ */
+MKV_API size_t mkv_prefix_workspace_size(mkv_geom geom, int32_t n_seqs, int32_t capacity, int32_t tail_capacity);
+
+/*
+ * One layer's decoding step of every sequence (Algorithm 1 Phase 2 over two
+ * sets of rows).  geom.batch is the number of prompts b.
+ *   q             bf16 [b, N, g*h_kv, d]  the new tokens' queries
+ *   k_new, v_new  bf16 [b, N, h_kv, d]    optional (both NULL or both set): the new tokens, appended to their tails
+ *                                         at row len with position seen, as mkv_decode_step does
+ *   prefix        the shared rows: an mkv_cache of b * h_kv units; not changed
+ *   mom           their moments (b * h_kv units); may be NULL if p->correction is 0
+ *   tail          the sequences' own rows: an mkv_cache of (b * N) * h_kv units; y and y_len are not used
+ *   out           bf16 [b, N, g*h_kv, d]  dense
+ *   lse           fp32 [b, N, g*h_kv]     optional: natural log of the normaliser
+ * For query head h of sequence i, unit (b, kv): the softmax over the shared
+ * rows 0..len-1, the tail's rows 0..len-1, the new token and, if p->correction
+ * and n > 0, the moment term with logit log n + scale q.mu_k and value mu_v +
+ * scale C' q (p->order 1) or mu_v (order 0), as in mkv_decode_step; p->C16 and
+ * p->C_split have that call's meaning.  p->early_load: the caller's guarantee of that call for the shared cache
+ * and moments.  A sequence with nothing at all to attend to gets zeros and lse -infinity.
+ * An append past the tail's capacity records MKV_ERR_CAPACITY (info: the tail's
+ * unit), still attends over the new token and leaves the tail as it is; a length outside 0..capacity is
+ * recorded as MKV_ERR_CAPACITY and taken as the nearer end.  Scores,
+ * statistics and sums are fp32; the softmax weights enter the product with the
+ * values as bf16 (one part, with a normaliser of the rounded weights, or two), and the output is rounded to bf16.
+ * Requirements: q, k_new, v_new and out 16-byte aligned, lse 4; p as in
+ * mkv_decode_step.
+ */
+MKV_API mkv_status mkv_prefix_step(mkv_geom geom, const mkv_seqs* seqs, const void* q, const void* k_new,
+                                   const void* v_new, const mkv_cache* prefix, const mkv_moments* mom,
+                                   const mkv_cache* tail, const mkv_decode_params* p, void* out, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* The scores of every beam's continuations, read on the host during the call. */
 typedef struct {

@@ -11,6 +11,55 @@
 
 namespace mkv {
 
+// ------------------------------------------------------------------ prefix
+struct PrefixArgs {
+  const void* q;  // bf16 [b, N, Hkv*G, D], strides in elements
+  int64_t q_seq, q_batch;
+  const void* k_new;  // bf16 [b, N, Hkv, D] or null
+  const void* v_new;
+  int64_t kv_seq, kv_batch;
+  int32_t N;
+  const int32_t* count;  // [b] or null
+  const void* K;         // the shared rows: bf16 [b, Hkv, cap, D]
+  const void* V;
+  const int32_t* len;
+  int32_t cap;
+  const int32_t* n;  // null: no moment term
+  const float* mu_k;
+  const float* mu_v;
+  const float* C;
+  const __nv_bfloat16* C16;
+  const uint2* Cs;
+  int32_t order;
+  float tau;
+  void* Kt;  // the tails: bf16 [b * N, Hkv, cap_t, D]
+  void* Vt;
+  int32_t* pos_t;
+  int32_t* len_t;
+  int32_t* seen_t;
+  int32_t cap_t;
+  __nv_bfloat16* out;  // [b, N, Hkv*G, D]
+  float* lse;
+  int32_t batch;
+  int32_t n_kv;
+  int32_t group;
+  int32_t early;
+  uint32_t polls;
+  void* ws;
+  // filled by the launcher: parts of every query row, row-major as out's rows
+  float2* ml;        // [parts][rows]: reference and sum, log2 domain
+  float* o;          // [parts][rows][D]: sum of weighted values about the reference
+  int32_t rows;      // b * N * Hkv * G
+  int32_t blocks;    // column blocks of a unit's query rows
+  int32_t splits;    // parts of the shared rows (of a column block); part 0 is the first
+  int32_t moments;   // the moment term's part, or -1
+  int32_t tail;      // the tails' first part
+  int32_t splits_t;  // parts of a tail
+  int32_t parts;
+};
+size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity, int num_sms);
+cudaError_t launch_prefix_step(const PrefixArgs& a, const mkv_geom& g, int num_sms, cudaStream_t stream);
+
 // ------------------------------------------------------------------ select
 struct SelectArgs {
   const void* logits;  // [b, beams, vocab], strides in elements

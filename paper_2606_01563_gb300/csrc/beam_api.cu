@@ -13,6 +13,14 @@ namespace {
 
 mkv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MKV_OK : MKV_ERR_CUDA; }
 
+// Sizes of a step, and rows of K and V that a tensor map's coordinates reach.
+bool prefix_sizes_ok(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity) {
+  const int64_t units = (int64_t)g.batch * g.n_kv_heads;
+  return n_seqs >= 1 && n_seqs <= MKV_BEAM_MAX_SEQS && capacity >= 1 && tail_capacity >= 1 &&
+         units * capacity < ((int64_t)1 << 31) && units * n_seqs * tail_capacity < ((int64_t)1 << 31) &&
+         units * n_seqs * g.group < ((int64_t)1 << 30);
+}
+
 bool select_sizes_ok(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out) {
   return batch >= 1 && batch <= 65535 && beams >= 1 && beams <= MKV_BEAM_MAX_BEAMS && vocab >= 1 &&
          vocab <= (1 << 24) && n_out >= 1 && n_out <= MKV_BEAM_MAX_OUT;
@@ -21,6 +29,66 @@ bool select_sizes_ok(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out)
 }  // namespace
 
 extern "C" {
+
+// ------------------------------------------------------------------ prefix
+size_t mkv_prefix_workspace_size(mkv_geom geom, int32_t n_seqs, int32_t capacity, int32_t tail_capacity) {
+  if (!geom_ok(geom) || !prefix_sizes_ok(geom, n_seqs, capacity, tail_capacity)) return 0;
+  return prefix_workspace_bytes(geom, n_seqs, capacity, tail_capacity, num_sms_current());
+}
+
+mkv_status mkv_prefix_step(mkv_geom geom, const mkv_seqs* seqs, const void* q, const void* k_new, const void* v_new,
+                           const mkv_cache* prefix, const mkv_moments* mom, const mkv_cache* tail,
+                           const mkv_decode_params* p, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  NvtxRange nvtx("mkv_prefix_step");
+  const mkv_status chk =
+      decode_args_status(geom, q, k_new, v_new, prefix, mom, p, static_cast<const float*>(out));
+  if (chk != MKV_OK) return chk;
+  if (!seqs || !cache_ok(tail) || !aligned(seqs->count, 4) || !aligned(lse, 4)) return MKV_ERR_INVALID_ARG;
+  if (!prefix_sizes_ok(geom, seqs->n_seqs, prefix->capacity, tail->capacity)) return MKV_ERR_SHAPE;
+  PrefixArgs a{};
+  const int64_t kv = (int64_t)geom.n_kv_heads * geom.head_dim, N = seqs->n_seqs;
+  if (!stride_of(seqs->q_seq, kv * geom.group, &a.q_seq) || !stride_of(seqs->q_batch, N * a.q_seq, &a.q_batch) ||
+      !stride_of(seqs->kv_seq, kv, &a.kv_seq) || !stride_of(seqs->kv_batch, N * a.kv_seq, &a.kv_batch))
+    return MKV_ERR_INVALID_ARG;
+  const int sms = num_sms_current();
+  if (!workspace || !aligned(workspace, 256) ||
+      workspace_bytes < prefix_workspace_bytes(geom, seqs->n_seqs, prefix->capacity, tail->capacity, sms))
+    return MKV_ERR_WORKSPACE;
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.N = seqs->n_seqs;
+  a.count = seqs->count;
+  a.K = prefix->K;
+  a.V = prefix->V;
+  a.len = prefix->len;
+  a.cap = prefix->capacity;
+  if (p->correction) {
+    a.n = mom->n;
+    a.mu_k = mom->mu_k;
+    a.mu_v = mom->mu_v;
+    a.C = mom->C;
+    a.C16 = static_cast<const __nv_bfloat16*>(p->C16);
+    a.Cs = static_cast<const uint2*>(p->C_split);
+  }
+  a.order = p->order;
+  a.tau = p->tau;
+  a.Kt = tail->K;
+  a.Vt = tail->V;
+  a.pos_t = tail->pos;
+  a.len_t = tail->len;
+  a.seen_t = tail->seen;
+  a.cap_t = tail->capacity;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.lse = lse;
+  a.batch = geom.batch;
+  a.n_kv = geom.n_kv_heads;
+  a.group = geom.group;
+  a.early = p->early_load;
+  a.ws = workspace;
+  return cuda_status(launch_prefix_step(a, geom, sms, static_cast<cudaStream_t>(stream)));
+}
 
 // ------------------------------------------------------------------ select
 size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out) {

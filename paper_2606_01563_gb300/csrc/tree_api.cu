@@ -15,13 +15,6 @@ mkv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MKV_OK : MKV_E
 
 bool header_ok(const void* ws, size_t bytes) { return ws && bytes >= kHeaderBytes && aligned(ws, 256); }
 
-// A stride as used: the dense value for 0, else the caller's, which 16-byte
-// copies must be able to step by and tensor maps to hold (below 2^40 bytes).
-bool stride_of(int64_t given, int64_t dense, int64_t* used) {
-  *used = given == 0 ? dense : given;
-  return *used >= dense && *used % 8 == 0 && *used < ((int64_t)1 << 38);
-}
-
 // 1 / 2 pi as the sum of two doubles
 constexpr double kTurnHi = 0x1.45f306dc9c883p-3, kTurnLo = -0x1.6b01ec5417056p-57;
 

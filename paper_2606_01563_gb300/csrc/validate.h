@@ -20,6 +20,13 @@ struct NvtxRange {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// A stride as used: the dense value for 0, else the caller's, which 16-byte
+// copies must be able to step by and tensor maps to hold (below 2^40 bytes).
+inline bool stride_of(int64_t given, int64_t dense, int64_t* used) {
+  *used = given == 0 ? dense : given;
+  return *used >= dense && *used % 8 == 0 && *used < ((int64_t)1 << 38);
+}
+
 // batch and KV heads are grid dimensions of the decode launch (z and y), so
 // each stays within 65535
 inline bool geom_ok(const mkv_geom& g) {

@@ -78,6 +78,11 @@ class mkv_norm_rope_grad_tensor(ctypes.Structure):
         ("weight", c_vp), ("weight_head", ctypes.c_int64), ("weight_f32", c_i32), ("dweight", c_vp)]
 
 
+class mkv_seqs(ctypes.Structure):
+    _fields_ = [("n_seqs", c_i32), ("count", c_vp), ("q_seq", ctypes.c_int64), ("q_batch", ctypes.c_int64),
+                ("kv_seq", ctypes.c_int64), ("kv_batch", ctypes.c_int64)]
+
+
 class mkv_beam_scores(ctypes.Structure):
     _fields_ = [("logits", c_vp), ("f32", c_i32), ("logits_batch", ctypes.c_int64), ("logits_beam", ctypes.c_int64),
                 ("score", c_vp), ("done", c_vp), ("end_token", c_i32)]
@@ -98,7 +103,8 @@ EXPORTS = ("mkv_status_str", "mkv_version", "mkv_compress_workspace_size", "mkv_
 TREE_EXPORTS = ("mkv_tree_build", "mkv_tree_workspace_size", "mkv_tree_step", "mkv_tree_commit", "mkv_rope",
                 "mkv_norm_rope", "mkv_norm_rope_grad_workspace_size", "mkv_norm_rope_grad")
 # declared in include/mkv_beam.h
-BEAM_EXPORTS = ("mkv_beam_select_workspace_size", "mkv_beam_select", "mkv_beam_reorder")
+BEAM_EXPORTS = ("mkv_prefix_workspace_size", "mkv_prefix_step", "mkv_beam_select_workspace_size", "mkv_beam_select",
+                "mkv_beam_reorder")
 # test hooks declared in include/mkv_debug.h
 DEBUG_EXPORTS = ("mkv_debug_set_poll_limit", "mkv_debug_force_ticket_merge")
 
@@ -176,6 +182,12 @@ def lib():
         L.mkv_norm_rope_grad.restype = c_i32
         L.mkv_norm_rope_grad.argtypes = [c_i32, c_i32, c_i32, c_vp, c_i64, c_i64, ctypes.POINTER(mkv_rope_params),
                                          ctypes.c_float, c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
+        L.mkv_prefix_workspace_size.restype = ctypes.c_size_t
+        L.mkv_prefix_workspace_size.argtypes = [mkv_geom, c_i32, c_i32, c_i32]
+        L.mkv_prefix_step.restype = c_i32
+        L.mkv_prefix_step.argtypes = [mkv_geom, c_vp, c_vp, c_vp, c_vp, ctypes.POINTER(mkv_cache),
+                                      ctypes.POINTER(mkv_moments), ctypes.POINTER(mkv_cache),
+                                      ctypes.POINTER(mkv_decode_params), c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.mkv_beam_select_workspace_size.restype = ctypes.c_size_t
         L.mkv_beam_select_workspace_size.argtypes = [c_i32, c_i32, c_i32, c_i32]
         L.mkv_beam_select.restype = c_i32
@@ -296,6 +308,15 @@ class TreeLayers:
     tree: mkv_tree
     batch: int
     held: list
+
+
+class Seqs:
+    """The sequences of every prompt (mkv_seqs): n of them, and count int32 [b], those in use (None: all n)."""
+    __slots__ = ("n", "count", "usable")
+
+    def __init__(self, n, count=None):
+        self.n, self.count = n, count
+        self.usable = count is None or (count.dtype is torch.int32 and count.dim() == 1 and count.is_contiguous())
 
 
 @dataclass
@@ -661,6 +682,57 @@ def mkv_norm_rope_grad(pos, p: mkv_rope_params, tensors, eps, ws, stream=None):
 
 
 # --------------------------------------------- several continuations of a prompt
+_I64x6 = ctypes.c_int64 * 6
+
+
+def mkv_prefix_workspace_size(g, n_seqs, capacity, tail_capacity):
+    return lib().mkv_prefix_workspace_size(g, n_seqs, capacity, tail_capacity)
+
+
+def _strides(t, shape, what):
+    """(sequence, batch) strides in elements of a bf16 [b, N, heads, d] tensor with dense heads, 0 where one is not used."""
+    s = t.stride()
+    if t.dtype is not _BF16 or t.shape != shape or s[3] != 1 or (shape[2] > 1 and s[2] != shape[3]):
+        raise ValueError(f"{what}: bf16 {list(shape)} with dense heads")
+    b, n = shape[0] > 1, shape[1] > 1
+    # (over a larger extent 0 would be taken for the dense value, past the end of an expanded tensor)
+    if (n and s[1] == 0) or (b and s[0] == 0):
+        raise ValueError(f"{what}: not expanded over sequences or prompts")
+    return s[1] if n else 0, s[0] if b else 0
+
+
+def mkv_prefix_step(g, seqs: Seqs, q, k_new, v_new, prefix: Cache, mom: Moments | None, tail: Cache,
+                    p: mkv_decode_params, out, lse, ws, stream=None):
+    """One decoding step of N sequences per prompt: q bf16 [b, N, g*h_kv, d], k_new and v_new bf16 [b, N, h_kv, d] or
+    None (sequences and prompts may be strided), prefix and its moments [b, h_kv, ...], tail [b * N, h_kv, ...], out
+    bf16 [b, N, g*h_kv, d], lse float32 [b, N, g*h_kv] or None."""
+    b, h, d, n = g.batch, g.n_kv_heads, g.head_dim, seqs.n
+    heads = g.group * h
+    if not seqs.usable or (seqs.count is not None and seqs.count.shape[0] != b):
+        raise ValueError("seqs: count contiguous int32 [b]")
+    of = (b, n, heads, d)
+    qs = _strides(q, of, "q")
+    ks = (0, 0)
+    _need((k_new is None) == (v_new is None), "k_new and v_new: both or neither")
+    if k_new is not None:
+        ks = _strides(k_new, (b, n, h, d), "k_new")
+        _need(_strides(v_new, (b, n, h, d), "v_new") == ks, "k_new and v_new: of the same strides")
+    if out.dtype is not _BF16 or out.shape != of or not out.is_contiguous():
+        raise ValueError(f"out: contiguous bf16 {list(of)}")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != of[:3] or not lse.is_contiguous()):
+        raise ValueError("lse: contiguous float32 [b, N, g*h_kv]")
+    kp, kt = prefix.K.shape, tail.K.shape
+    if (kp[0], kp[1], kp[3]) != (b, h, d) or (kt[0], kt[1], kt[3]) != (b * n, h, d):
+        raise ValueError("prefix: [b, h_kv, ...]; tail: [b * N, h_kv, ...]")
+    _here(q, k_new, v_new, out, lse, ws, prefix.K, tail.K)
+    s = _I64x6(n, 0 if seqs.count is None else seqs.count.data_ptr(), *qs, *ks)
+    code = lib().mkv_prefix_step(g, s, q.data_ptr(), _ptr(k_new), _ptr(v_new), prefix.c(),
+                                 None if mom is None else mom.c(), tail.c(), p, out.data_ptr(), _ptr(lse),
+                                 ws.data_ptr(), ws.numel(), _stream(stream))
+    if code:
+        _check(code, "mkv_prefix_step")
+
+
 def mkv_beam_select_workspace_size(batch, beams, vocab, n_out):
     return lib().mkv_beam_select_workspace_size(batch, beams, vocab, n_out)
 

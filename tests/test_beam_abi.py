@@ -102,3 +102,91 @@ def test_reorder_binding_refusals():
     for name, x in (("n", m.n.float()), ("mu_k", m.mu_k[:, :, :32]), ("C", m.C.transpose(2, 3))):
         with pytest.raises(ValueError):
             mkv.beam_layers([(cache(K=cache().K), mkv.Moments(**{**m.__dict__, name: x}))])
+
+
+def test_every_declared_function_is_exported_and_bound(L):
+    src = open(os.path.join(ROOT, "include", "mkv_beam.h")).read()
+    names = set(re.findall(r"MKV_API\s+[\w\s\*]+?\b(mkv_\w+)\s*\(", src))
+    assert names == set(mkv.BEAM_EXPORTS)
+    for n in names:
+        assert hasattr(L, n) and hasattr(mkv, n), n
+
+
+CLIENT = r"""
+#include <stddef.h>
+#include <stdio.h>
+#include "mkv_beam.h"
+#define CHECK(c) do { if (!(c)) { printf("FAIL %d: %s\n", __LINE__, #c); return 1; } } while (0)
+int main(void) {
+  CHECK(sizeof(mkv_seqs) == 48 && offsetof(mkv_seqs, count) == 8 && offsetof(mkv_seqs, kv_batch) == 40);
+  CHECK(sizeof(mkv_beam_scores) == 56 && offsetof(mkv_beam_scores, score) == 32 && offsetof(mkv_beam_scores, end_token) == 48);
+  CHECK(sizeof(mkv_beam_layer) == 96 && offsetof(mkv_beam_layer, mom) == 64);
+  CHECK(MKV_BEAM_MAX_SEQS == 256 && MKV_BEAM_MAX_BEAMS == 64 && MKV_BEAM_MAX_OUT == 64);
+  return 0;
+}
+"""
+
+
+@pytest.mark.parametrize("compiler,std,ext", [("gcc", "c99", "c"), ("g++", "c++17", "cpp")])
+def test_header_layouts(tmp_path, compiler, std, ext):
+    if shutil.which(compiler) is None:
+        pytest.skip(f"no {compiler}")
+    src = tmp_path / f"client.{ext}"
+    src.write_text(CLIENT)
+    exe = tmp_path / "client"
+    subprocess.run([compiler, f"-std={std}", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(ROOT, "include"), str(src),
+                    "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0
+    assert [ctypes.sizeof(x) for x in (mkv.mkv_seqs, mkv.mkv_beam_scores, mkv.mkv_beam_layer)] == [48, 56, 96]
+
+
+def test_prefix_refusals(L):
+    C = mkv.mkv_cache
+
+    def call(g=mkv.geom(2, 3, 4, 128), n=5, count=None, strides=(0, 0, 0, 0), q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=FAKE,
+             prefix=C(FAKE, FAKE, FAKE, FAKE, FAKE, 64), tail=C(FAKE, FAKE, FAKE, FAKE, FAKE, 9), null=False,
+             mom=mkv.mkv_moments(FAKE, FAKE, FAKE, FAKE), p=mkv.mkv_decode_params(1, 1, 1e-6), ws=FAKE, wsb=1 << 40):
+        s = mkv.mkv_seqs(n, count, *strides)
+        return L.mkv_prefix_step(g, None if null else ctypes.byref(s), q, k, v, prefix, mom, tail, p, out, lse, ws, wsb, None)
+    assert call(g=mkv.geom(2, 3, 4, 96)) == UNSUPPORTED and call(g=mkv.geom(2, 3, 3, 128)) == SHAPE
+    for n in (0, 257, -1):
+        assert call(n=n) == SHAPE and mkv.mkv_prefix_workspace_size(mkv.geom(1, 1, 1, 64), n, 10, 10) == 0
+    sizes = mkv.mkv_prefix_workspace_size
+    assert sizes(mkv.geom(1, 1, 1, 64), 2, 0, 1) == sizes(mkv.geom(1, 1, 1, 64), 2, 1, 0) == sizes(mkv.geom(1, 1, 1, 80), 2, 1, 1) == 0
+    assert call(null=True) == INVALID
+    for name in ("q", "k", "v", "out"):
+        assert call(**{name: None}) == INVALID and call(**{name: FAKE + 8}) == INVALID
+    assert call(lse=FAKE + 2) == INVALID and call(count=FAKE + 1) == INVALID
+    dq, dkv = 12 * 128, 3 * 128
+    for strides in ((dq - 8, 0, 0, 0), (dq + 4, 0, 0, 0), (0, 5 * dq - 8, 0, 0), (0, 0, dkv - 8, 0), (0, 0, 0, 5 * dkv - 8),
+                    (-8, 0, 0, 0), (0, 0, 1 << 40, 0)):
+        assert call(strides=strides) == INVALID, strides
+    for bad in (C(None, FAKE, FAKE, FAKE, FAKE, 64), C(FAKE, FAKE + 8, FAKE, FAKE, FAKE, 64), C(FAKE, FAKE, FAKE, FAKE, FAKE, 0)):
+        assert call(prefix=bad) == INVALID and call(tail=bad) == INVALID
+    assert call(prefix=C(FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 29)) == SHAPE  # rows past a tensor map's coordinates
+    assert call(tail=C(FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 27)) == SHAPE
+    assert call(mom=mkv.mkv_moments(FAKE, FAKE + 4, FAKE, FAKE)) == INVALID
+    assert call(p=mkv.mkv_decode_params(2, 1, 1e-6)) == INVALID and call(p=mkv.mkv_decode_params(1, 1, -1.0)) == INVALID
+    assert call(p=mkv.mkv_decode_params(1, 1, 1e-6, FAKE, 0, FAKE)) == INVALID
+    need = sizes(mkv.geom(2, 3, 4, 128), 5, 64, 9)
+    assert need >= 256 and call(wsb=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE and call(ws=FAKE + 16) == WORKSPACE
+
+
+def test_prefix_binding_refusals():
+    g = mkv.geom(2, 2, 2, 64)
+    b16 = dict(dtype=torch.bfloat16)
+    prefix, tail = mkv.alloc_cache(g, 8, device="cpu"), mkv.alloc_cache(mkv.geom(6, 2, 2, 64), 4, device="cpu")
+    good = dict(seqs=mkv.Seqs(3), q=torch.zeros(2, 3, 4, 64, **b16), k_new=torch.zeros(2, 3, 2, 64, **b16),
+                v_new=torch.zeros(2, 3, 2, 64, **b16), prefix=prefix, tail=tail, out=torch.zeros(2, 3, 4, 64, **b16),
+                lse=torch.zeros(2, 3, 4))
+    bad = dict(seqs=(mkv.Seqs(3, torch.zeros(2)), mkv.Seqs(3, torch.zeros(3, dtype=torch.int32)), mkv.Seqs(2)),
+               q=(good["q"].float(), good["q"][:, :2], good["q"].transpose(2, 3), good["q"][:1].expand(2, -1, -1, -1),
+                  good["q"][:, :1].expand(-1, 3, -1, -1), torch.zeros(2, 3, 4, 128, **b16)[..., ::2], torch.zeros(2, 3, 8, 64, **b16)[:, :, ::2]),
+               k_new=(None, good["k_new"].half(), torch.zeros(2, 3, 4, 64, **b16)[:, :, :2]),
+               v_new=(None, torch.zeros(2, 4, 2, 64, **b16)), out=(good["out"].float(), torch.zeros(2, 6, 4, 64, **b16)[:, ::2]),
+               lse=(torch.zeros(2, 3, 2), torch.zeros(2, 3, 4, dtype=torch.float64)), prefix=(tail,), tail=(prefix,))
+    for name, values in bad.items():
+        for x in values:
+            with pytest.raises(ValueError):
+                mkv.mkv_prefix_step(g, **{**good, name: x}, mom=None, p=mkv.mkv_decode_params(0, 1, 1e-6),
+                                    ws=torch.zeros(1 << 20, dtype=torch.uint8))

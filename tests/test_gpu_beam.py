@@ -251,3 +251,17 @@ def test_tensors_of_another_device_are_refused():
     c, _ = _layer(torch.Generator(device="cuda"), 2, 1, 4, 64, 0, 0)
     with pytest.raises(ValueError):
         mkv.beam_layers([(mkv.Cache(c.K.cpu(), c.V, c.pos, c.len, c.seen), None)])
+
+
+def test_reorder_waits_that_run_out_are_recorded():
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    states = [_layer(gen, 8, 2, 300, 64, 0, 1)]
+    parent = torch.tensor([[1, 2, 3, 0]] * 2, dtype=I32, device="cuda")
+    ws, old = mkv.alloc_workspace(256), mkv.mkv_debug_set_poll_limit(0)
+    try:
+        mkv.mkv_beam_reorder(mkv.geom(2, 2, 1, 64), mkv.beam_layers(states), parent, ws)
+        assert mkv.mkv_get_device_error(ws)[0] == 5
+    finally:
+        mkv.mkv_debug_set_poll_limit(old)
+    _reorder_and_check(states, parent, 2, 64)
