@@ -55,6 +55,8 @@ struct PrefixArgs {
   int32_t moments;   // the moment term's part, or -1
   int32_t tail;      // the tails' first part
   int32_t splits_t;  // parts of a tail
+  int32_t tails;     // tails of a block
+  int32_t late;      // the launch before wrote nothing that this one reads: waited for at the end
   int32_t parts;
 };
 size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity, int num_sms);

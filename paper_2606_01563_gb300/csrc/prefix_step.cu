@@ -16,11 +16,16 @@
 // its unit's heads.  prefix_join_kernel joins each row's parts and the new token and
 // appends that token to its tail.
 //
-// A run, as in decode_cl.cu: a warp issues 64-row TMA copies into a ring; four
-// warps take 16 rows of every tile each, S^T = K q^T with the keys on the 16-row
-// side and the query rows on the 8-column side, then O^T += V^T P^T with P rounded
-// to bf16.  O is scaled by the ratio of the unrounded weights' sum to the rounded
-// ones', so that roundings that are common cancel.
+// A run: a warp issues 64-row TMA copies into a ring; four warps work on every
+// tile together.  Each takes the logits of 16 of its rows, S^T = K q^T with the keys on
+// the 16-row side and the query rows on the 8-column side, and writes their
+// weights, rounded to bf16, to shared memory; then each takes a quarter of the
+// value dims over all 64 rows, O^T += V^T P^T.  So a query row's O is held once (8 NT registers a thread at
+// 128 dims), up to 64 query rows share a shared row's one trip, and no states of
+// warps are merged.  One barrier a tile: the weights have two buffers.  A reference
+// moves when a score exceeds it by more than 8 (log2), which every warp learns
+// at that barrier.  O is scaled by the ratio of the unrounded weights' sum to the
+// rounded ones', so that roundings that are common cancel.
 #include <algorithm>
 
 #include "beam.h"
@@ -32,23 +37,31 @@ namespace mkv {
 
 namespace {
 
-constexpr int kWarps = 4;                   // that attend
-constexpr int kThreads = (kWarps + 1) * 32;  // and one that loads
+constexpr int kWarps = 4;                    // that attend for up to 32 query rows
+// and, in a block with CG groups of them, one that loads
+__host__ __device__ constexpr int threads(int CG) { return (kWarps * CG + 1) * 32; }
 constexpr int kRows = 64;                   // rows of a tile
-constexpr int kStages = 3;
 constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
+constexpr int kMaxTails = 8;   // tails of a block
 constexpr float kSlack = 8.f;  // log2 headroom of a reference (weights at most 2^8)
 constexpr float kNegInf = -INFINITY;
 constexpr int kJoinThreads = 256;
 
 __host__ __device__ constexpr int tile_bytes(int D) { return kRows * D * 2; }
-// q rows in shared memory lie 16 bytes apart beyond their length: ldmatrix meets no bank twice
+__host__ __device__ constexpr int stages(int D, int CG) { return (D == 64 ? 4 : 3) * CG; }
+constexpr int kMaxStages = 8;
+// Rows of q and of the weights lie 16 bytes apart beyond their length: ldmatrix meets no bank twice.
 __host__ __device__ constexpr int q_pitch(int D) { return D * 2 + 16; }
-__host__ __device__ constexpr int parts_smem(int D, int NT) {
-  return kStages * 2 * tile_bytes(D) + 8 * NT * q_pitch(D) + 1024;
+constexpr int kPPitch = kRows * 2 + 16;
+// The query rows go into registers, and their place in shared memory is one of the weights' two buffers.
+__host__ __device__ constexpr int p_offset(int D, int NT, int buffer) { return buffer == 0 ? 0 : 8 * NT * q_pitch(D); }
+__host__ __device__ constexpr int qp_bytes(int D, int NT) { return p_offset(D, NT, 1) + 8 * NT * kPPitch; }
+__host__ __device__ constexpr int parts_smem(int D, int NT, int CG) {
+  return stages(D, CG) * 2 * tile_bytes(D) + CG * qp_bytes(D, NT) + 1024;
 }
-static_assert(2 * (parts_smem(128, 4) + 1024) <= 228 * 1024, "two blocks to an SM");
+static_assert(2 * (parts_smem(128, 4, 1) + 2048) <= 228 * 1024, "two blocks to an SM");
+static_assert(parts_smem(128, 4, 2) + 4096 <= 227 * 1024, "one block to an SM");
 
 // A query row of a unit: sequence r / G, head r % G.
 __device__ __forceinline__ int64_t out_row(const PrefixArgs& a, int b, int kv, int r) {
@@ -59,256 +72,268 @@ __device__ __forceinline__ int live_seqs(const PrefixArgs& a, int b) {
   return a.count != nullptr ? min(max(a.count[b], 0), a.N) : a.N;
 }
 
+struct GroupShared {
+  float l[kWarps][32][2];  // of a warp and column: the weights' sum and the rounded ones'
+  float top[kWarps][32];   // a moving reference: the warps' largest scores
+  float e[32];             // the moment term's logits
+  int moved[2];            // the last tile (counted from 1) of either buffer in which a score passed its reference
+};
+template <int CG>
 struct PartsShared {
-  uint64_t full[kStages], empty[kStages];
-  float ml[kWarps][32][3];  // of a warp and column: reference, sum, sum of the rounded weights
-  float e[32];              // the moment term's logits
+  uint64_t full[kMaxStages], empty[kMaxStages];
+  GroupShared group[CG];
   float mu_k[128];
   int fail;
 };
 
-// The state of the `n` keys from row `row0` of the maps' matrices on, for `cols`
-// query rows (sQ) into part `part`; `row_of(c)` is column c's output row.
-template <int D, int NT, typename RowOf>
-__device__ __forceinline__ void attend_run(const PrefixArgs& a, const CUtensorMap* tmK, const CUtensorMap* tmV, int row0,
-                                           int n, int cols, int part, uint8_t* ring, const uint8_t* sQ,
-                                           PartsShared& sh, RowOf row_of) {
-  constexpr int MT = D / 16, KS = D / 16, kTile = tile_bytes(D);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int tiles = (n + kRows - 1) / kRows;
-  const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e;
-  if (warp == kWarps) {
-    int i = 0;  // tiles asked for
-    if (lane == 0) {
-      const uint64_t pol = l2_evict_first();
-      for (; i < tiles; ++i) {
-        const int st = i % kStages;
-        if (i >= kStages && !mbar_wait(&sh.empty[st], ((i / kStages) - 1) & 1, a.polls)) {
-          *reinterpret_cast<volatile int*>(&sh.fail) = 1;
-          break;
-        }
-        uint8_t* dst = ring + (size_t)st * 2 * kTile;
-        mbar_arrive_expect_tx(&sh.full[st], 2u * kTile);
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) {
-          tma_load_2d_hint(dst + x * kRows * 128, tmK, x * 64, row0 + i * kRows, &sh.full[st], pol);
-          tma_load_2d_hint(dst + kTile + x * kRows * 128, tmV, x * 64, row0 + i * kRows, &sh.full[st], pol);
-        }
-      }
+template <int CG>
+__device__ __forceinline__ bool failed(const PartsShared<CG>& sh) { return *reinterpret_cast<const volatile int*>(&sh.fail) != 0; }
+// A wait on a tile; one that runs out fails the block, whose later waits then
+// pass at once (barriers are met as ever; what is computed from here on is not used).
+template <int NS, int CG>
+__device__ __forceinline__ void wait_tile(PartsShared<CG>& sh, uint32_t seq, uint32_t polls) {
+  uint64_t* bar = &sh.full[seq % NS];
+  const uint32_t parity = (seq / NS) & 1;
+  if (polls > 0 && mbar_try_wait(bar, parity)) return;
+  if (!failed(sh) && !mbar_wait(bar, parity, polls)) *reinterpret_cast<volatile int*>(&sh.fail) = 1;
+}
+
+// The loading warp's part of a run of n rows: one thread, tiles seq, seq + 1, ... of the block.
+template <int D, int NS, int CG>
+__device__ __forceinline__ void load_run(const PrefixArgs& a, const CUtensorMap* tmK, const CUtensorMap* tmV, int row0, int n,
+                                         uint8_t* ring, PartsShared<CG>& sh, uint32_t& seq) {
+  constexpr int kTile = tile_bytes(D);
+  const uint64_t pol = l2_evict_first();
+  for (int i = 0; i * kRows < n; ++i) {
+    const uint32_t st = seq % NS;
+    if (seq >= NS && (failed(sh) || !mbar_wait(&sh.empty[st], ((seq / NS) - 1) & 1, a.polls))) {
+      *reinterpret_cast<volatile int*>(&sh.fail) = 1;
+      return;
     }
-    __syncwarp();
-    named_sync(2, kThreads);
-    // after a wait that gave up: the copies in flight land before the block ends
-    if (lane == 0 && *reinterpret_cast<volatile int*>(&sh.fail))
-      for (int j = max(0, i - kStages); j < i; ++j) (void)mbar_wait(&sh.full[j % kStages], (j / kStages) & 1);
-    return;
+    uint8_t* dst = ring + (size_t)st * 2 * kTile;
+    mbar_arrive_expect_tx(&sh.full[st], 2u * kTile);
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {
+      tma_load_2d_hint(dst + x * kRows * 128, tmK, x * 64, row0 + i * kRows, &sh.full[st], pol);
+      tma_load_2d_hint(dst + kTile + x * kRows * 128, tmV, x * 64, row0 + i * kRows, &sh.full[st], pol);
+    }
+    ++seq;
   }
-  const int r0 = warp * 16;
-  float m[NT][2], l[NT][2], lr[NT][2], o[NT][MT][4];
+}
+
+// Columns nt (and nt + 1, with four registers) of rows of q or of the weights as B
+// operands: 8 columns x 16 values of their rows.
+__device__ __forceinline__ void ldsm_b2(uint32_t& r0, uint32_t& r1, const uint8_t* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(smem_addr(p)));
+}
+
+// The state of a run of n rows for `cols` query rows (in sm, zeros past cols) into
+// part `part`; row_of(c) is column c's output row.  The four warps of a group.
+template <int D, int NT, int NS, int CG, typename RowOf>
+__device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols, int part, uint8_t* ring, uint8_t* sm,
+                                           PartsShared<CG>& sh, int group, uint32_t& seq, RowOf row_of) {
+  constexpr int KS = D / 16, MW = D / 64, kTile = tile_bytes(D);
+  const int tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  GroupShared& gs = sh.group[group];
+  const int tiles = (n + kRows - 1) / kRows, r0 = warp * 16;
+  const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e;
+  float m[NT][2], l[NT][2], lr[NT][2], o[NT][MW][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     m[nt][0] = m[nt][1] = kNegInf;
     l[nt][0] = l[nt][1] = lr[nt][0] = lr[nt][1] = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
+    for (int mt = 0; mt < MW; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
   }
-  // the query rows as the B operand: kept in registers where they are few
-  constexpr bool kKeep = NT <= 2;
-  uint32_t qf[kKeep ? NT : 1][KS][2];
-  auto load_q = [&](int nt, int kk, uint32_t (&b)[2]) {
-    const uint8_t* p = sQ + (nt * 8 + g) * q_pitch(D) + kk * 32 + t * 4;
-    b[0] = *reinterpret_cast<const uint32_t*>(p);
-    b[1] = *reinterpret_cast<const uint32_t*>(p + 16);
-  };
-  if constexpr (kKeep) {
+  const uint8_t* q_at = sm + (lane & 7) * q_pitch(D) + ((lane >> 3) & 1) * 16;  // (lanes 0-15)
+  uint32_t qf[NT][KS][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) load_q(nt, kk, qf[nt][kk]);
-  }
-  bool ok = true;
-  for (int it = 0; it < tiles; ++it) {
-    const int st = it % kStages;
-    const bool got = mbar_wait(&sh.full[st], (it / kStages) & 1, a.polls);
-    if (!__all_sync(0xffffffffu, got)) {
-      ok = false;
-      break;
-    }
+    for (int kk = 0; kk < KS; ++kk) ldsm_b2(qf[nt][kk][0], qf[nt][kk][1], q_at + nt * 8 * q_pitch(D) + kk * 32);
+  named_sync(1 + group, kWarps * 32);  // (the weights may be written over q)
+  const int kr = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
+  const int vr = (lane & 7) + (lane >> 4) * 8, vc = warp * (D / 4) + ((lane >> 3) & 1) * 8;
+  for (int it = 0; it < tiles; ++it, ++seq) {
+    wait_tile<NS>(sh, seq, a.polls);
     const int rows = min(kRows, n - it * kRows);
-    const uint8_t* tK = ring + (size_t)st * 2 * kTile;
-    uint8_t* tV = ring + (size_t)st * 2 * kTile + kTile;
-    if (rows > r0) {
-      if (rows < r0 + 16) {  // V rows past the end are zeroed: their weights are 0, but they may hold anything
-        for (int i = lane; i < (r0 + 16 - rows) * (D / 8); i += 32) {
-          const int r = rows + i / (D / 8), c = (i % (D / 8)) * 8;
-          *reinterpret_cast<uint4*>(tV + (c >> 6) * kRows * 128 + r * 128 + (c & 63) * 2) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        __syncwarp();
+    const uint8_t* tK = ring + (size_t)(seq % NS) * 2 * kTile;
+    uint8_t* tV = ring + (size_t)(seq % NS) * 2 * kTile + kTile;
+    uint8_t* sP = sm + p_offset(D, NT, it & 1);
+    if (rows < r0 + 16) {  // V rows past the end are zeroed: their weights are 0, but they may hold anything
+      const int from = max(rows, r0);
+      for (int i = lane; i < (r0 + 16 - from) * (D / 8); i += 32) {
+        const int r = from + i / (D / 8), c = (i % (D / 8)) * 8;
+        *reinterpret_cast<uint4*>(tV + (c >> 6) * kRows * 128 + r * 128 + (c & 63) * 2) = make_uint4(0u, 0u, 0u, 0u);
       }
-      float s[NT][4];
-      const int kr = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
-      if constexpr (NT == 1) {  // four chains: one would wait for itself
-        float c[4][4] = {};
+    }
+    float s[NT][4];
+    if constexpr (NT == 1) {  // two chains: one would wait for itself
+      float c[2][4] = {};
 #pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          uint32_t k4[4];
-          ldsm_x4(k4, tK + swz_off(kr, kk * 16 + kc, kRows));
-          mma_m16n8k16(c[kk & 3], k4[0], k4[1], k4[2], k4[3], qf[0][kk][0], qf[0][kk][1]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[0][i] = (c[0][i] + c[2][i]) + (c[1][i] + c[3][i]);
-      } else {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          uint32_t k4[4];
-          ldsm_x4(k4, tK + swz_off(kr, kk * 16 + kc, kRows));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if constexpr (kKeep) {
-              mma_m16n8k16(s[nt], k4[0], k4[1], k4[2], k4[3], qf[nt][kk][0], qf[nt][kk][1]);
-            } else {
-              uint32_t b[2];
-              load_q(nt, kk, b);
-              mma_m16n8k16(s[nt], k4[0], k4[1], k4[2], k4[3], b[0], b[1]);
-            }
-          }
-        }
+      for (int kk = 0; kk < KS; ++kk) {
+        uint32_t k4[4];
+        ldsm_x4(k4, tK + swz_off(kr, kk * 16 + kc, kRows));
+        mma_m16n8k16(c[kk & 1], k4[0], k4[1], k4[2], k4[3], qf[0][kk][0], qf[0][kk][1]);
       }
-      // lane (g, t): keys r0 + g (0, 1) and r0 + g + 8 (2, 3), columns 2t (0, 2) and 2t + 1 (1, 3)
-      const bool va = r0 + g < rows, vb = r0 + g + 8 < rows;
-      bool moves = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int i = 0; i < 4; ++i) s[0][i] = c[0][i] + c[1][i];
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[nt][i] = (i < 2 ? va : vb) ? s[nt][i] * qscale : kNegInf;
-        moves |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
-      }
-      // A reference only has to be common to a column's keys: it moves when a score
-      // exceeds it by more than kSlack, so most tiles skip the maximum over the lanes.
-      if (__any_sync(0xffffffffu, moves)) {
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        uint32_t k4[4];
+        ldsm_x4(k4, tK + swz_off(kr, kk * 16 + kc, kRows));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float mx = fmaxf(s[nt][j], s[nt][j + 2]);
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            const float mn = fmaxf(m[nt][j], mx);
-            const float f = mn == kNegInf ? 1.f : fast_exp2(m[nt][j] - mn);
-            m[nt][j] = mn;
-            l[nt][j] *= f, lr[nt][j] *= f;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[nt][mt][j] *= f, o[nt][mt][j + 2] *= f;
-          }
+          mma_m16n8k16(s[nt], k4[0], k4[1], k4[2], k4[3], qf[nt][kk][0], qf[nt][kk][1]);
         }
       }
-      uint32_t p0[NT], p1[NT];
+    }
+    // lane (g, t): keys r0 + g (0, 1) and r0 + g + 8 (2, 3), columns 2t (0, 2) and 2t + 1 (1, 3)
+    bool moves = false;
+    if (rows < kRows) {
+      const bool va = r0 + g < rows, vb = r0 + g + 8 < rows;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        s[nt][0] = va ? s[nt][0] : kNegInf, s[nt][1] = va ? s[nt][1] : kNegInf;
+        s[nt][2] = vb ? s[nt][2] : kNegInf, s[nt][3] = vb ? s[nt][3] : kNegInf;
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[nt][i] *= qscale;
+      moves |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
+    }
+    // the weights, and what they add to the sums (taken once the references are known to hold)
+    float dl[NT][2], dr[NT][2];
+    auto weigh = [&]() {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float ma = m[nt][0] == kNegInf ? 0.f : m[nt][0], mb = m[nt][1] == kNegInf ? 0.f : m[nt][1];
         const float x0 = fast_exp2(s[nt][0] - ma), x1 = fast_exp2(s[nt][1] - mb);
         const float x2 = fast_exp2(s[nt][2] - ma), x3 = fast_exp2(s[nt][3] - mb);
-        l[nt][0] += x0 + x2;
-        l[nt][1] += x1 + x3;
         const uint32_t h0 = pack_bf16x2(x0, x1), h1 = pack_bf16x2(x2, x3);
-        lr[nt][0] += __uint_as_float(h0 << 16) + __uint_as_float(h1 << 16);
-        lr[nt][1] += __uint_as_float(h0 & 0xffff0000u) + __uint_as_float(h1 & 0xffff0000u);
-        p0[nt] = movmatrix_t(h0);
-        p1[nt] = movmatrix_t(h1);
+        dl[nt][0] = x0 + x2;
+        dl[nt][1] = x1 + x3;
+        dr[nt][0] = __uint_as_float(h0 << 16) + __uint_as_float(h1 << 16);
+        dr[nt][1] = __uint_as_float(h0 & 0xffff0000u) + __uint_as_float(h1 & 0xffff0000u);
+        uint8_t* p = sP + (nt * 8 + g) * kPPitch + (r0 + 2 * t) * 2;  // [column][key]
+        *reinterpret_cast<uint32_t*>(p) = movmatrix_t(h0);
+        *reinterpret_cast<uint32_t*>(p + 16) = movmatrix_t(h1);
       }
-      const int vr = r0 + (lane & 7) + (lane >> 4) * 8, vc = ((lane >> 3) & 1) * 8;
+    };
+    if (__any_sync(0xffffffffu, moves)) {
+      if (lane == 0) *reinterpret_cast<volatile int*>(&gs.moved[it & 1]) = it + 1;
+    } else {
+      weigh();
+    }
+    named_sync(1 + group, kWarps * 32);
+    if (*reinterpret_cast<volatile int*>(&gs.moved[it & 1]) == it + 1) {
+      // some column's reference moves: to the largest score of the four warps'
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        uint32_t v4[4];
-        ldsm_x4_t(v4, tV + swz_off(vr, mt * 16 + vc, kRows));
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_m16n8k16(o[nt][mt], v4[0], v4[1], v4[2], v4[3], p0[nt], p1[nt]);
+        for (int j = 0; j < 2; ++j) {
+          float mx = fmaxf(s[nt][j], s[nt][j + 2]);
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+          if (g == 0) gs.top[warp][nt * 8 + 2 * t + j] = mx;
+        }
+      named_sync(1 + group, kWarps * 32);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int c = nt * 8 + 2 * t + j;
+          const float mn = fmaxf(fmaxf(m[nt][j], fmaxf(gs.top[0][c], gs.top[1][c])), fmaxf(gs.top[2][c], gs.top[3][c]));
+          const float f = mn == kNegInf ? 1.f : fast_exp2(m[nt][j] - mn);
+          m[nt][j] = mn;
+          l[nt][j] *= f, lr[nt][j] *= f;
+#pragma unroll
+          for (int mt = 0; mt < MW; ++mt) o[nt][mt][j] *= f, o[nt][mt][j + 2] *= f;
+        }
+      weigh();
+      named_sync(1 + group, kWarps * 32);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) l[nt][j] += dl[nt][j], lr[nt][j] += dr[nt][j];
+    // O^T += V^T P^T over this warp's dims
+    const uint8_t* p_at = sP + (lane & 7) * kPPitch + (lane >> 3) * 16;
+#pragma unroll
+    for (int kk = 0; kk < kRows / 32; ++kk) {
+      uint32_t v4[2][MW][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int mt = 0; mt < MW; ++mt) ldsm_x4_t(v4[x][mt], tV + swz_off(kk * 32 + x * 16 + vr, vc + mt * 16, kRows));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        uint32_t b[4];
+        ldsm_x4(b, p_at + nt * 8 * kPPitch + kk * 64);
+#pragma unroll
+        for (int mt = 0; mt < MW; ++mt) {
+          mma_m16n8k16(o[nt][mt], v4[0][mt][0], v4[0][mt][1], v4[0][mt][2], v4[0][mt][3], b[0], b[1]);
+          mma_m16n8k16(o[nt][mt], v4[1][mt][0], v4[1][mt][1], v4[1][mt][2], v4[1][mt][3], b[2], b[3]);
+        }
       }
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.empty[st]);
+    if (lane == 0) mbar_arrive(&sh.empty[seq % NS]);
   }
-  if (!ok && lane == 0) *reinterpret_cast<volatile int*>(&sh.fail) = 1;
+  // the columns' sums over the warps, and the state
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) {
         l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], off);
         lr[nt][j] += __shfl_xor_sync(0xffffffffu, lr[nt][j], off);
       }
-  // the four warps' states into one, through the ring (free once every warp is
-  // past its tiles, unless a wait gave up and copies may still land there)
-  named_sync(2, kThreads);
-  const bool bad = *reinterpret_cast<volatile int*>(&sh.fail) != 0;
-  float* sW = reinterpret_cast<float*>(ring);  // [4][8 NT][D]
-  if (!bad) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sW[(size_t)(warp * 8 * NT + nt * 8 + 2 * t + (i & 1)) * D + mt * 16 + g + (i >> 1) * 8] = o[nt][mt][i];
-    if (g == 0) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float* x = sh.ml[warp][nt * 8 + 2 * t + j];
-          x[0] = m[nt][j], x[1] = l[nt][j], x[2] = lr[nt][j];
-        }
+      if (g == 0) {
+        gs.l[warp][nt * 8 + 2 * t + j][0] = l[nt][j];
+        gs.l[warp][nt * 8 + 2 * t + j][1] = lr[nt][j];
+      }
     }
-  } else if (tid == 0) {
-    record_error(a.ws, MKV_ERR_TIMEOUT, static_cast<int>(blockIdx.x));
-  }
-  named_sync(1, kWarps * 32);
-  for (int i = tid; i < cols * (D / 4); i += kWarps * 32) {
-    const int c = i / (D / 4), d0 = (i % (D / 4)) * 4;
-    float M = kNegInf, L = 0.f, LR = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!bad) {
+  named_sync(1 + group, kWarps * 32);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w)
-        if (sh.ml[w][c][1] != 0.f) M = fmaxf(M, sh.ml[w][c][0]);
-      const float ref = M == kNegInf ? 0.f : M;
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w)
-        if (sh.ml[w][c][1] != 0.f) {
-          const float f = fast_exp2(sh.ml[w][c][0] - ref);
-          const float4 v = *reinterpret_cast<const float4*>(sW + (size_t)(w * 8 * NT + c) * D + d0);
-          L = fmaf(sh.ml[w][c][1], f, L);
-          LR = fmaf(sh.ml[w][c][2], f, LR);
-          acc.x = fmaf(f, v.x, acc.x);
-          acc.y = fmaf(f, v.y, acc.y);
-          acc.z = fmaf(f, v.z, acc.z);
-          acc.w = fmaf(f, v.w, acc.w);
-        }
-    }
-    const size_t at = (size_t)part * a.rows + row_of(c);
-    if (d0 == 0) a.ml[at] = make_float2(M, L);
-    if (L != 0.f) {
+    for (int j = 0; j < 2; ++j) {
+      const int c = nt * 8 + 2 * t + j;
+      if (c >= cols) continue;
+      float L = 0.f, LR = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) L += gs.l[w][c][0], LR += gs.l[w][c][1];
+      const size_t at = (size_t)part * a.rows + row_of(c);
+      if (warp == 0 && g == 0) a.ml[at] = make_float2(m[nt][j], L);
+      if (L == 0.f) continue;
       const float even = LR != 0.f ? L / LR : 1.f;
-      *reinterpret_cast<float4*>(a.o + at * D + d0) = make_float4(acc.x * even, acc.y * even, acc.z * even, acc.w * even);
+      float* dst = a.o + at * D + warp * (D / 4) + g;
+#pragma unroll
+      for (int mt = 0; mt < MW; ++mt) {
+        dst[mt * 16] = o[nt][mt][j] * even;
+        dst[mt * 16 + 8] = o[nt][mt][j + 2] * even;
+      }
     }
-  }
 }
 
 // The moment term's state of unit u for `cols` query rows (sQ): a warp has 16
 // dims of C' q at a time, C' (clamped) as bf16 hi + lo parts, or in the forms it was packed in.
-template <int D, int NT, typename RowOf>
+template <int D, int NT, int CG, typename RowOf>
 __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, int cols, const uint8_t* sQ,
-                                           PartsShared& sh, RowOf row_of) {
+                                           PartsShared<CG>& sh, int group, RowOf row_of) {
   constexpr int KS = D / 16;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  if (warp == kWarps) return;
+  const int tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const float scale = rsqrtf(static_cast<float>(D));
-  if (n_e > 0)
+  if (n_e > 0)  // (every group writes the same)
     for (int i = tid; i < D; i += kWarps * 32) sh.mu_k[i] = a.mu_k[(size_t)u * D + i];
-  named_sync(1, kWarps * 32);
+  named_sync(1 + group, kWarps * 32);
   // four threads a column (a warp has eight: all of them take every turn, for the shuffles)
   for (int c = tid >> 2; c < 8 * NT; c += kWarps * 8) {
     float e = 0.f;
@@ -323,12 +348,12 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
     e += __shfl_xor_sync(0xffffffffu, e, 2);
     if ((tid & 3) == 0 && c < cols) {
       const float x = n_e > 0 ? fmaf(e, scale * kLog2e, log2f(static_cast<float>(n_e))) : kNegInf;
-      sh.e[c] = x;
+      sh.group[group].e[c] = x;
       a.ml[(size_t)a.moments * a.rows + row_of(c)] = make_float2(x, x != kNegInf ? 1.f : 0.f);
     }
   }
   if (n_e <= 0) return;
-  named_sync(1, kWarps * 32);
+  named_sync(1 + group, kWarps * 32);
   const float nf = static_cast<float>(n_e), tau = a.tau;
   for (int mt = warp; mt < D / 16; mt += kWarps) {
     const int ra = mt * 16 + g, rb = ra + 8;
@@ -382,23 +407,40 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
   }
 }
 
-// Blocks: the shared rows' runs (unit, column block, split), the moment terms (unit, column
-// block), the tails' runs (tail unit, split).
-template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, 2)
+// Query rows of unit (b, kv) from row `first` on into shared memory, `wide` of them, zeros where there is none.
+template <int D>
+__device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int first, int wide, uint8_t* sm) {
+  for (int i = threadIdx.x & 127; i < wide * (D / 8); i += kWarps * 32) {
+    const int c = i / (D / 8), k = i % (D / 8), r = first + c, seq = r / a.group;
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (seq < a.N)
+      w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + seq * a.q_seq +
+                                          (kv * a.group + r - seq * a.group) * D + k * 8);
+    *reinterpret_cast<uint4*>(sm + c * q_pitch(D) + k * 16) = w;
+  }
+}
+
+// Blocks: the shared rows' runs (unit, column block, split), the moment terms
+// (unit, column block), the tails (a run of one, or several short ones), each where
+// this launch has them.  A block of two groups (CG) has 64 columns, and no tails.
+template <int D, int NT, int CG>
+__global__ void __launch_bounds__(threads(CG), 3 - CG)
     prefix_parts_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKt,
                         const __grid_constant__ CUtensorMap tmVt) {
+  constexpr int NS = stages(D, CG), kCols = 8 * NT * CG;
   extern __shared__ __align__(128) uint8_t raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* sQ = ring + kStages * 2 * tile_bytes(D);
-  __shared__ PartsShared sh;
-  const int tid = threadIdx.x;
-  if (tid < kStages) {
+  __shared__ PartsShared<CG> sh;
+  const int tid = threadIdx.x, lane = tid & 31, group = tid >> 7;
+  const bool loads = group == CG;
+  uint8_t* sm = ring + NS * 2 * tile_bytes(D) + group * qp_bytes(D, NT);  // the group's query rows and weights
+  if (tid < NS) {
     mbar_init(&sh.full[tid], 1);
-    mbar_init(&sh.empty[tid], kWarps);
+    mbar_init(&sh.empty[tid], kWarps * CG);
   }
   if (tid == 0) sh.fail = 0;
+  if (tid < 2 * CG) sh.group[tid >> 1].moved[tid & 1] = 0;
   mbar_fence_init();
   // what this block's work is
   const int units = a.batch * a.n_kv, shared_blocks = units * a.blocks * a.splits;
@@ -406,49 +448,78 @@ __global__ void __launch_bounds__(kThreads, 2)
   int x = blockIdx.x, kind = 0;
   if (x >= shared_blocks) x -= shared_blocks, kind = 1;
   if (kind == 1 && x >= moment_blocks) x -= moment_blocks, kind = 2;
-  const int split = kind == 0 ? x % a.splits : kind == 2 ? x % a.splits_t : 0;
-  const int item = kind == 0 ? x / a.splits : kind == 2 ? x / a.splits_t : x;
-  // kinds 0 and 1: unit and column block; kind 2: tail unit (prompt, sequence, head)
-  const int u = kind == 2 ? item : item / a.blocks;
-  const int pair = u / a.n_kv, kv = u - pair * a.n_kv;  // (prompt, or prompt and sequence)
-  const int b = kind == 2 ? pair / a.N : pair;
-  const int first = kind == 2 ? (pair - b * a.N) * a.group : (item - u * a.blocks) * 8 * NT;
-  grid_dependency_wait();
+  __syncthreads();
+  if (!a.late) grid_dependency_wait();
   grid_launch_dependents();
-  const int count = live_seqs(a, b);
-  if (kind == 0 && split == 0 && kv == 0 && first == 0 && tid == 0 && a.count != nullptr && a.count[b] != count)
-    record_error(a.ws, MKV_ERR_INVALID_ARG, b);
-  const int cols = min(kind == 2 ? a.group : 8 * NT, count * a.group - first);
-  if (cols <= 0) return;  // (no sequence in use: nothing is joined)
-  const int cap = kind == 2 ? a.cap_t : a.cap;
-  const int have = kind == 1 ? 0 : kind == 2 ? a.len_t[u] : a.len[u];
-  const int len = min(max(have, 0), cap);
-  if (have != len && split == 0 && (kind == 2 || first == 0) && tid == 0) record_error(a.ws, MKV_ERR_CAPACITY, u);
-  // the query rows into shared memory, zeros past `cols`
-  const int wide = kind == 2 ? 8 : 8 * NT;
-  for (int i = tid; i < wide * (D / 8); i += kThreads) {
-    const int c = i / (D / 8), k = i % (D / 8);
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (c < cols) {
-      const int r = first + c, seq = r / a.group;
-      w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + seq * a.q_seq +
-                                          (kv * a.group + r - seq * a.group) * D + k * 8);
+  uint32_t seq = 0;
+  auto run_of = [](int len, int splits, int split, int& row) {  // this split's rows of `len`
+    const int tiles = (len + kRows - 1) / kRows, per = (tiles + splits - 1) / splits;
+    const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
+    row = t0 * kRows;
+    return max(0, min(len, t1 * kRows) - t0 * kRows);
+  };
+  if (kind < 2) {
+    const int item = kind == 0 ? x / a.splits : x, split = kind == 0 ? x - item * a.splits : 0;
+    const int u = item / a.blocks, b = u / a.n_kv, kv = u - b * a.n_kv, first = (item - u * a.blocks) * kCols;
+    const int counted = a.count != nullptr ? a.count[b] : a.N, have = kind == 0 ? a.len[u] : a.n[u];
+    if (!loads) stage_q<D>(a, b, kv, first + group * 8 * NT, 8 * NT, sm);
+    const int count = min(max(counted, 0), a.N), cols = count * a.group - first;
+    const int len = min(max(have, 0), a.cap);
+    if (kind == 0 && split == 0 && first == 0 && tid == 0) {
+      if (kv == 0 && count != counted) record_error(a.ws, MKV_ERR_INVALID_ARG, b);
+      if (have != len) record_error(a.ws, MKV_ERR_CAPACITY, u);
     }
-    *reinterpret_cast<uint4*>(sQ + c * q_pitch(D) + k * 16) = w;
+    if (cols > 0) {  // (else no sequence is in use: nothing is joined)
+      int row, n = 0;
+      if (kind == 0) n = run_of(len, a.splits, split, row);
+      if (loads) {
+        if (lane == 0 && kind == 0) load_run<D, NS>(a, &tmK, &tmV, u * a.cap + row, n, ring, sh, seq);
+      } else {
+        named_sync(1 + group, kWarps * 32);
+        const int from = first + group * 8 * NT, mine = min(8 * NT, cols - group * 8 * NT);
+        auto row_of = [&](int c) { return out_row(a, b, kv, from + c); };
+        if (kind == 0)
+          attend_run<D, NT, NS>(a, n, mine, split, ring, sm, sh, group, seq, row_of);
+        else
+          moment_run<D, NT>(a, u, have, mine, sm, sh, group, row_of);
+      }
+    }
+  } else if constexpr (CG == 1) {
+    const int item = x / a.splits_t, split = x - item * a.splits_t;
+    const int u0 = item * a.tails, mine = min(a.tails, units * a.N - u0);
+    // the tails' lengths, a lane each (0 of a sequence that is not in use)
+    int len_all = 0, live_all = 0;
+    if (lane < mine) {
+      const int u = u0 + lane, b = u / a.n_kv / a.N, have = a.len_t[u];
+      live_all = u / a.n_kv - b * a.N < (a.count != nullptr ? a.count[b] : a.N);
+      len_all = live_all ? min(max(have, 0), a.cap_t) : 0;
+      if (live_all && have != len_all && split == 0 && loads) record_error(a.ws, MKV_ERR_CAPACITY, u);
+    }
+    for (int i = 0; i < mine; ++i) {
+      const int u = u0 + i, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
+      int row;
+      const int n = run_of(__shfl_sync(0xffffffffu, len_all, i), a.splits_t, split, row);
+      if (!__shfl_sync(0xffffffffu, live_all, i)) continue;
+      if (loads) {
+        if (lane == 0) load_run<D, NS>(a, &tmKt, &tmVt, u * a.cap_t + row, n, ring, sh, seq);
+        __syncwarp();
+      } else {
+        const int first = (pair - b * a.N) * a.group;
+        named_sync(1, kWarps * 32);  // (every warp is past the tail before)
+        stage_q<D>(a, b, kv, first, 8, sm);
+        if (tid < 2) sh.group[0].moved[tid] = 0;
+        named_sync(1, kWarps * 32);
+        attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, 0, seq, [&](int c) { return out_row(a, b, kv, first + c); });
+      }
+    }
   }
   __syncthreads();
-  auto row_of = [&](int c) { return out_row(a, b, kv, first + c); };
-  // this split's run of tiles
-  const int splits = kind == 2 ? a.splits_t : a.splits;
-  const int tiles = (len + kRows - 1) / kRows, per = (tiles + splits - 1) / splits;
-  const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
-  const int n = max(0, min(len, t1 * kRows) - t0 * kRows), row0 = u * cap + t0 * kRows;
-  if (kind == 0)
-    attend_run<D, NT>(a, &tmK, &tmV, row0, n, cols, split, ring, sQ, sh, row_of);
-  else if (kind == 1)
-    moment_run<D, NT>(a, u, a.n[u], cols, sQ, sh, row_of);
-  else
-    attend_run<D, 1>(a, &tmKt, &tmVt, row0, n, cols, a.tail + split, ring, sQ, sh, row_of);
+  if (failed(sh) && loads && lane == 0) {
+    record_error(a.ws, MKV_ERR_TIMEOUT, static_cast<int>(blockIdx.x));
+    // the copies in flight land before the block ends
+    for (uint32_t j = seq > NS ? seq - NS : 0; j < seq; ++j) (void)mbar_wait(&sh.full[j % NS], (j / NS) & 1);
+  }
+  if (a.late) grid_dependency_wait();  // (the join waits for this launch, which stands for the one before too)
 }
 
 // A thread has 4 dims of a query row: the parts, then the new token, joined; the
@@ -481,11 +552,19 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_
     acc[2] = fmaf(v.z, f, acc[2] * f0);
     acc[3] = fmaf(v.w, f, acc[3] * f0);
   };
-#pragma unroll 4
-  for (int p = 0; p < a.parts; ++p) {
-    const size_t at = (size_t)p * a.rows + row;
-    const float2 ml = a.ml[at];
-    if (ml.y != 0.f) join(ml.x, ml.y, *reinterpret_cast<const float4*>(a.o + at * D + d0));
+  // four parts' loads at a time in flight (what an empty part's O holds is not used)
+  for (int p0 = 0; p0 < a.parts; p0 += 4) {
+    float2 ml[4];
+    float4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const size_t at = (size_t)min(p0 + i, a.parts - 1) * a.rows + row;
+      ml[i] = a.ml[at];
+      v[i] = *reinterpret_cast<const float4*>(a.o + at * D + d0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p0 + i < a.parts && ml[i].y != 0.f) join(ml[i].x, ml[i].y, v[i]);
   }
   if (a.k_new != nullptr) {
     const int64_t at = b * a.kv_batch + seq * a.kv_seq + kv * D + d0;
@@ -523,26 +602,52 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_
   if (d0 == 0 && a.lse != nullptr) a.lse[row] = L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
 }
 
-// Columns of a block (8, 16 or 32), the parts of a query row and the splits.
-int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
+// The parts of a query row, the splits, and the 8-column tiles (1, 2 or 4) and
+// groups (1 or 2) of a block.
+struct Shape {
+  int nt, cg;
+};
+Shape plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   const long units = (long)g.batch * g.n_kv_heads, rows = (long)a.N * g.group;
-  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  a.blocks = static_cast<int>((rows + 8 * nt - 1) / (8 * nt));
+  const Shape s{rows <= 8 ? 1 : rows <= 16 ? 2 : 4, rows <= 32 ? 1 : 2};
+  a.blocks = static_cast<int>((rows + 8 * s.nt * s.cg - 1) / (8 * s.nt * s.cg));
   const long tiles = ((long)a.cap + kRows - 1) / kRows, tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
-  // runs of equal length, as many as there are places
-  const long all = units * a.blocks * tiles + units * a.N * tiles_t;
-  const long per = std::max<long>(kMinTiles, (all + 2 * num_sms - 1) / (2 * num_sms));
+  // runs of equal length, as many as there are places (two groups: a launch each for shared rows and tails)
+  const long places = 2 * num_sms, all = units * a.blocks * tiles, all_t = units * a.N * tiles_t;
+  const auto length = [&](long t, long p) { return std::max<long>(kMinTiles, (t + p - 1) / p); };
+  const long per = s.cg == 1 ? length(all + all_t, places) : length(all, num_sms);
+  const long per_t = s.cg == 1 ? per : length(all_t, places);
   a.splits = static_cast<int>(std::min<long>(kMaxSplits, (tiles + per - 1) / per));
-  a.splits_t = static_cast<int>(std::min<long>(kMaxSplits, (tiles_t + per - 1) / per));
+  a.splits_t = static_cast<int>(std::min<long>(kMaxSplits, (tiles_t + per_t - 1) / per_t));
+  a.tails = static_cast<int>(std::clamp<long>(per_t / tiles_t, 1, kMaxTails));
   a.moments = a.n != nullptr ? a.splits : -1;
   a.tail = a.splits + (a.n != nullptr ? 1 : 0);
   a.parts = a.tail + a.splits_t;
   a.rows = static_cast<int>(units * rows);
-  return nt;
+  return s;
 }
 
-template <int D, int NT>
-cudaError_t launch_parts(const PrefixArgs& a, cudaStream_t stream) {
+// One launch: the shared rows and moments, the tails, or both.
+template <int D, int NT, int CG>
+cudaError_t launch_parts(PrefixArgs a, const CUtensorMap (&tm)[4], bool shared, bool tails, bool late, cudaStream_t stream) {
+  constexpr int smem = parts_smem(D, NT, CG);
+  cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const long units = (long)a.batch * a.n_kv;
+  long blocks = 0;
+  if (shared)
+    blocks += units * a.blocks * (a.splits + (a.moments >= 0 ? 1 : 0));
+  else
+    a.blocks = 0, a.moments = -1;
+  if (tails) blocks += (units * a.N + a.tails - 1) / a.tails * a.splits_t;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  a.late = late ? 1 : 0;
+  return launch_pdl(prefix_parts_kernel<D, NT, CG>, dim3(static_cast<unsigned>(blocks)), dim3(threads(CG)), smem, stream,
+                    a, tm[0], tm[1], tm[2], tm[3]);
+}
+
+template <int D>
+cudaError_t launch(const PrefixArgs& a, const Shape& s, cudaStream_t stream) {
   CUtensorMap tm[4];
   const uint64_t rows = (uint64_t)a.batch * a.n_kv * a.cap, rows_t = (uint64_t)a.batch * a.N * a.n_kv * a.cap_t;
   if (!encode_tmap_bf16(&tm[0], a.K, D, rows, (uint64_t)D * 2, 64, kRows) ||
@@ -550,21 +655,15 @@ cudaError_t launch_parts(const PrefixArgs& a, cudaStream_t stream) {
       !encode_tmap_bf16(&tm[2], a.Kt, D, rows_t, (uint64_t)D * 2, 64, kRows) ||
       !encode_tmap_bf16(&tm[3], a.Vt, D, rows_t, (uint64_t)D * 2, 64, kRows))
     return cudaErrorInvalidValue;
-  constexpr int smem = parts_smem(D, NT);
-  cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  const long units = (long)a.batch * a.n_kv;
-  const long blocks = units * a.blocks * (a.splits + (a.moments >= 0 ? 1 : 0)) + units * a.N * a.splits_t;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_pdl(prefix_parts_kernel<D, NT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), smem, stream, a,
-                    tm[0], tm[1], tm[2], tm[3]);
-}
-
-template <int D>
-cudaError_t launch(const PrefixArgs& a, int nt, cudaStream_t stream) {
-  const cudaError_t e = nt == 1   ? launch_parts<D, 1>(a, stream)
-                        : nt == 2 ? launch_parts<D, 2>(a, stream)
-                                  : launch_parts<D, 4>(a, stream);
+  cudaError_t e;
+  if (s.cg == 1) {
+    e = s.nt == 1   ? launch_parts<D, 1, 1>(a, tm, true, true, false, stream)
+        : s.nt == 2 ? launch_parts<D, 2, 1>(a, tm, true, true, false, stream)
+                    : launch_parts<D, 4, 1>(a, tm, true, true, false, stream);
+  } else {
+    e = launch_parts<D, 1, 1>(a, tm, false, true, false, stream);
+    if (e == cudaSuccess) e = launch_parts<D, 4, 2>(a, tm, true, false, true, stream);
+  }
   if (e != cudaSuccess) return e;
   constexpr int kPer = kJoinThreads / (D / 4);
   return launch_pdl(prefix_join_kernel<D>, dim3((a.rows + kPer - 1) / kPer), dim3(kJoinThreads), 0, stream, a);
@@ -577,19 +676,19 @@ cudaError_t launch(const PrefixArgs& a, int nt, cudaStream_t stream) {
 size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity, int num_sms) {
   (void)capacity, (void)tail_capacity;
   const long units = (long)g.batch * g.n_kv_heads, rows = units * n_seqs * g.group;
-  // a column block's parts have at most 32 rows, a tail's at most 8
-  const long part_rows = 3 * rows + 2l * num_sms * 32 + 2l * num_sms * 8;
+  // a column block's parts have at most 64 rows, a tail's at most 8
+  const long part_rows = 3 * rows + 2l * num_sms * 64 + 2l * num_sms * 8;
   return kHeaderBytes + align_up(part_rows * sizeof(float2), 256) + (size_t)part_rows * g.head_dim * 4;
 }
 
 cudaError_t launch_prefix_step(const PrefixArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
   PrefixArgs a = args;
   a.polls = pipeline_poll_limit();
-  const int nt = plan(a, g, num_sms);
+  const Shape s = plan(a, g, num_sms);
   uint8_t* w = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
   a.ml = reinterpret_cast<float2*>(w);
   a.o = reinterpret_cast<float*>(w + align_up((size_t)a.parts * a.rows * sizeof(float2), 256));
-  return g.head_dim == 128 ? launch<128>(a, nt, stream) : launch<64>(a, nt, stream);
+  return g.head_dim == 128 ? launch<128>(a, s, stream) : launch<64>(a, s, stream);
 }
 
 }  // namespace mkv
