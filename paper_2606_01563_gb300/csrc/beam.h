@@ -50,16 +50,15 @@ struct PrefixArgs {
   float2* ml;        // [parts][rows]: reference and sum, log2 domain
   float* o;          // [parts][rows][D]: sum of weighted values about the reference
   int32_t rows;      // b * N * Hkv * G
-  int32_t blocks;    // column blocks of a unit's query rows
-  int32_t splits;    // parts of the shared rows (of a column block); part 0 is the first
+  int32_t blocks;    // 1: the shared rows and moments are prefix_parts_kernel's, 0: another's
+  int32_t splits;    // parts of the shared rows; part 0 is the first
   int32_t moments;   // the moment term's part, or -1
   int32_t tail;      // the tails' first part
   int32_t splits_t;  // parts of a tail
   int32_t tails;     // tails of a block
-  int32_t late;      // the launch before wrote nothing that this one reads: waited for at the end
   int32_t parts;
 };
-size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity, int num_sms);
+size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms);
 cudaError_t launch_prefix_step(const PrefixArgs& a, const mkv_geom& g, int num_sms, cudaStream_t stream);
 
 // ------------------------------------------------------------------ select

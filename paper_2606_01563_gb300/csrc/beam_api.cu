@@ -33,7 +33,7 @@ extern "C" {
 // ------------------------------------------------------------------ prefix
 size_t mkv_prefix_workspace_size(mkv_geom geom, int32_t n_seqs, int32_t capacity, int32_t tail_capacity) {
   if (!geom_ok(geom) || !prefix_sizes_ok(geom, n_seqs, capacity, tail_capacity)) return 0;
-  return prefix_workspace_bytes(geom, n_seqs, capacity, tail_capacity, num_sms_current());
+  return prefix_workspace_bytes(geom, n_seqs, capacity, num_sms_current());
 }
 
 mkv_status mkv_prefix_step(mkv_geom geom, const mkv_seqs* seqs, const void* q, const void* k_new, const void* v_new,
@@ -53,7 +53,7 @@ mkv_status mkv_prefix_step(mkv_geom geom, const mkv_seqs* seqs, const void* q, c
     return MKV_ERR_INVALID_ARG;
   const int sms = num_sms_current();
   if (!workspace || !aligned(workspace, 256) ||
-      workspace_bytes < prefix_workspace_bytes(geom, seqs->n_seqs, prefix->capacity, tail->capacity, sms))
+      workspace_bytes < prefix_workspace_bytes(geom, seqs->n_seqs, prefix->capacity, sms))
     return MKV_ERR_WORKSPACE;
   a.q = q;
   a.k_new = k_new;

@@ -31,37 +31,35 @@
 #include "beam.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "tree.h"
 #include "warp_mma.cuh"
 
 namespace mkv {
 
 namespace {
 
-constexpr int kWarps = 4;                    // that attend for up to 32 query rows
-// and, in a block with CG groups of them, one that loads
-__host__ __device__ constexpr int threads(int CG) { return (kWarps * CG + 1) * 32; }
+constexpr int kWarps = 4;                   // that attend
+constexpr int kThreads = (kWarps + 1) * 32;  // and one that loads
 constexpr int kRows = 64;                   // rows of a tile
 constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
 constexpr int kMaxTails = 8;   // tails of a block
+constexpr long kTreeRows = 16;  // query rows of a unit above which the shared rows run on tcgen05
 constexpr float kSlack = 8.f;  // log2 headroom of a reference (weights at most 2^8)
 constexpr float kNegInf = -INFINITY;
 constexpr int kJoinThreads = 256;
 
 __host__ __device__ constexpr int tile_bytes(int D) { return kRows * D * 2; }
-__host__ __device__ constexpr int stages(int D, int CG) { return (D == 64 ? 4 : 3) * CG; }
-constexpr int kMaxStages = 8;
+__host__ __device__ constexpr int stages(int D) { return D == 64 ? 4 : 3; }
+constexpr int kMaxStages = 4;
 // Rows of q and of the weights lie 16 bytes apart beyond their length: ldmatrix meets no bank twice.
 __host__ __device__ constexpr int q_pitch(int D) { return D * 2 + 16; }
 constexpr int kPPitch = kRows * 2 + 16;
 // The query rows go into registers, and their place in shared memory is one of the weights' two buffers.
 __host__ __device__ constexpr int p_offset(int D, int NT, int buffer) { return buffer == 0 ? 0 : 8 * NT * q_pitch(D); }
 __host__ __device__ constexpr int qp_bytes(int D, int NT) { return p_offset(D, NT, 1) + 8 * NT * kPPitch; }
-__host__ __device__ constexpr int parts_smem(int D, int NT, int CG) {
-  return stages(D, CG) * 2 * tile_bytes(D) + CG * qp_bytes(D, NT) + 1024;
-}
-static_assert(2 * (parts_smem(128, 4, 1) + 2048) <= 228 * 1024, "two blocks to an SM");
-static_assert(parts_smem(128, 4, 2) + 4096 <= 227 * 1024, "one block to an SM");
+__host__ __device__ constexpr int parts_smem(int D, int NT) { return stages(D) * 2 * tile_bytes(D) + qp_bytes(D, NT) + 1024; }
+static_assert(2 * (parts_smem(128, 2) + 3072) <= 228 * 1024, "two blocks to an SM");
 
 // A query row of a unit: sequence r / G, head r % G.
 __device__ __forceinline__ int64_t out_row(const PrefixArgs& a, int b, int kv, int r) {
@@ -72,26 +70,21 @@ __device__ __forceinline__ int live_seqs(const PrefixArgs& a, int b) {
   return a.count != nullptr ? min(max(a.count[b], 0), a.N) : a.N;
 }
 
-struct GroupShared {
-  float l[kWarps][32][2];  // of a warp and column: the weights' sum and the rounded ones'
-  float top[kWarps][32];   // a moving reference: the warps' largest scores
-  float e[32];             // the moment term's logits
-  int moved[2];            // the last tile (counted from 1) of either buffer in which a score passed its reference
-};
-template <int CG>
+constexpr int kMaxCols = kTreeRows;
 struct PartsShared {
   uint64_t full[kMaxStages], empty[kMaxStages];
-  GroupShared group[CG];
+  float l[kWarps][kMaxCols][2];  // of a warp and column: the weights' sum and the rounded ones'
+  float top[kWarps][kMaxCols];   // a moving reference: the warps' largest scores
   float mu_k[128];
+  int moved[2];  // the last tile (counted from 1) of either buffer in which a score passed its reference
   int fail;
 };
 
-template <int CG>
-__device__ __forceinline__ bool failed(const PartsShared<CG>& sh) { return *reinterpret_cast<const volatile int*>(&sh.fail) != 0; }
+__device__ __forceinline__ bool failed(const PartsShared& sh) { return *reinterpret_cast<const volatile int*>(&sh.fail) != 0; }
 // A wait on a tile; one that runs out fails the block, whose later waits then
 // pass at once (barriers are met as ever; what is computed from here on is not used).
-template <int NS, int CG>
-__device__ __forceinline__ void wait_tile(PartsShared<CG>& sh, uint32_t seq, uint32_t polls) {
+template <int NS>
+__device__ __forceinline__ void wait_tile(PartsShared& sh, uint32_t seq, uint32_t polls) {
   uint64_t* bar = &sh.full[seq % NS];
   const uint32_t parity = (seq / NS) & 1;
   if (polls > 0 && mbar_try_wait(bar, parity)) return;
@@ -99,9 +92,9 @@ __device__ __forceinline__ void wait_tile(PartsShared<CG>& sh, uint32_t seq, uin
 }
 
 // The loading warp's part of a run of n rows: one thread, tiles seq, seq + 1, ... of the block.
-template <int D, int NS, int CG>
+template <int D, int NS>
 __device__ __forceinline__ void load_run(const PrefixArgs& a, const CUtensorMap* tmK, const CUtensorMap* tmV, int row0, int n,
-                                         uint8_t* ring, PartsShared<CG>& sh, uint32_t& seq) {
+                                         uint8_t* ring, PartsShared& sh, uint32_t& seq) {
   constexpr int kTile = tile_bytes(D);
   const uint64_t pol = l2_evict_first();
   for (int i = 0; i * kRows < n; ++i) {
@@ -128,13 +121,12 @@ __device__ __forceinline__ void ldsm_b2(uint32_t& r0, uint32_t& r1, const uint8_
 }
 
 // The state of a run of n rows for `cols` query rows (in sm, zeros past cols) into
-// part `part`; row_of(c) is column c's output row.  The four warps of a group.
-template <int D, int NT, int NS, int CG, typename RowOf>
+// part `part`; row_of(c) is column c's output row.  The four attending warps.
+template <int D, int NT, int NS, typename RowOf>
 __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols, int part, uint8_t* ring, uint8_t* sm,
-                                           PartsShared<CG>& sh, int group, uint32_t& seq, RowOf row_of) {
+                                           PartsShared& sh, uint32_t& seq, RowOf row_of) {
   constexpr int KS = D / 16, MW = D / 64, kTile = tile_bytes(D);
-  const int tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  GroupShared& gs = sh.group[group];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int tiles = (n + kRows - 1) / kRows, r0 = warp * 16;
   const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e;
   float m[NT][2], l[NT][2], lr[NT][2], o[NT][MW][4];
@@ -151,7 +143,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) ldsm_b2(qf[nt][kk][0], qf[nt][kk][1], q_at + nt * 8 * q_pitch(D) + kk * 32);
-  named_sync(1 + group, kWarps * 32);  // (the weights may be written over q)
+  named_sync(1, kWarps * 32);  // (the weights may be written over q)
   const int kr = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
   const int vr = (lane & 7) + (lane >> 4) * 8, vc = warp * (D / 4) + ((lane >> 3) & 1) * 8;
   for (int it = 0; it < tiles; ++it, ++seq) {
@@ -226,12 +218,12 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
       }
     };
     if (__any_sync(0xffffffffu, moves)) {
-      if (lane == 0) *reinterpret_cast<volatile int*>(&gs.moved[it & 1]) = it + 1;
+      if (lane == 0) *reinterpret_cast<volatile int*>(&sh.moved[it & 1]) = it + 1;
     } else {
       weigh();
     }
-    named_sync(1 + group, kWarps * 32);
-    if (*reinterpret_cast<volatile int*>(&gs.moved[it & 1]) == it + 1) {
+    named_sync(1, kWarps * 32);
+    if (*reinterpret_cast<volatile int*>(&sh.moved[it & 1]) == it + 1) {
       // some column's reference moves: to the largest score of the four warps'
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -240,15 +232,15 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
           float mx = fmaxf(s[nt][j], s[nt][j + 2]);
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-          if (g == 0) gs.top[warp][nt * 8 + 2 * t + j] = mx;
+          if (g == 0) sh.top[warp][nt * 8 + 2 * t + j] = mx;
         }
-      named_sync(1 + group, kWarps * 32);
+      named_sync(1, kWarps * 32);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int c = nt * 8 + 2 * t + j;
-          const float mn = fmaxf(fmaxf(m[nt][j], fmaxf(gs.top[0][c], gs.top[1][c])), fmaxf(gs.top[2][c], gs.top[3][c]));
+          const float mn = fmaxf(fmaxf(m[nt][j], fmaxf(sh.top[0][c], sh.top[1][c])), fmaxf(sh.top[2][c], sh.top[3][c]));
           const float f = mn == kNegInf ? 1.f : fast_exp2(m[nt][j] - mn);
           m[nt][j] = mn;
           l[nt][j] *= f, lr[nt][j] *= f;
@@ -256,7 +248,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
           for (int mt = 0; mt < MW; ++mt) o[nt][mt][j] *= f, o[nt][mt][j + 2] *= f;
         }
       weigh();
-      named_sync(1 + group, kWarps * 32);
+      named_sync(1, kWarps * 32);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -296,11 +288,11 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
         lr[nt][j] += __shfl_xor_sync(0xffffffffu, lr[nt][j], off);
       }
       if (g == 0) {
-        gs.l[warp][nt * 8 + 2 * t + j][0] = l[nt][j];
-        gs.l[warp][nt * 8 + 2 * t + j][1] = lr[nt][j];
+        sh.l[warp][nt * 8 + 2 * t + j][0] = l[nt][j];
+        sh.l[warp][nt * 8 + 2 * t + j][1] = lr[nt][j];
       }
     }
-  named_sync(1 + group, kWarps * 32);
+  named_sync(1, kWarps * 32);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -309,7 +301,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
       if (c >= cols) continue;
       float L = 0.f, LR = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) L += gs.l[w][c][0], LR += gs.l[w][c][1];
+      for (int w = 0; w < kWarps; ++w) L += sh.l[w][c][0], LR += sh.l[w][c][1];
       const size_t at = (size_t)part * a.rows + row_of(c);
       if (warp == 0 && g == 0) a.ml[at] = make_float2(m[nt][j], L);
       if (L == 0.f) continue;
@@ -325,15 +317,15 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
 
 // The moment term's state of unit u for `cols` query rows (sQ): a warp has 16
 // dims of C' q at a time, C' (clamped) as bf16 hi + lo parts, or in the forms it was packed in.
-template <int D, int NT, int CG, typename RowOf>
+template <int D, int NT, typename RowOf>
 __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, int cols, const uint8_t* sQ,
-                                           PartsShared<CG>& sh, int group, RowOf row_of) {
+                                           PartsShared& sh, RowOf row_of) {
   constexpr int KS = D / 16;
-  const int tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const float scale = rsqrtf(static_cast<float>(D));
-  if (n_e > 0)  // (every group writes the same)
+  if (n_e > 0)
     for (int i = tid; i < D; i += kWarps * 32) sh.mu_k[i] = a.mu_k[(size_t)u * D + i];
-  named_sync(1 + group, kWarps * 32);
+  named_sync(1, kWarps * 32);
   // four threads a column (a warp has eight: all of them take every turn, for the shuffles)
   for (int c = tid >> 2; c < 8 * NT; c += kWarps * 8) {
     float e = 0.f;
@@ -348,12 +340,11 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
     e += __shfl_xor_sync(0xffffffffu, e, 2);
     if ((tid & 3) == 0 && c < cols) {
       const float x = n_e > 0 ? fmaf(e, scale * kLog2e, log2f(static_cast<float>(n_e))) : kNegInf;
-      sh.group[group].e[c] = x;
       a.ml[(size_t)a.moments * a.rows + row_of(c)] = make_float2(x, x != kNegInf ? 1.f : 0.f);
     }
   }
   if (n_e <= 0) return;
-  named_sync(1 + group, kWarps * 32);
+  named_sync(1, kWarps * 32);
   const float nf = static_cast<float>(n_e), tau = a.tau;
   for (int mt = warp; mt < D / 16; mt += kWarps) {
     const int ra = mt * 16 + g, rb = ra + 8;
@@ -410,7 +401,7 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
 // Query rows of unit (b, kv) from row `first` on into shared memory, `wide` of them, zeros where there is none.
 template <int D>
 __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int first, int wide, uint8_t* sm) {
-  for (int i = threadIdx.x & 127; i < wide * (D / 8); i += kWarps * 32) {
+  for (int i = threadIdx.x; i < wide * (D / 8); i += kWarps * 32) {
     const int c = i / (D / 8), k = i % (D / 8), r = first + c, seq = r / a.group;
     uint4 w = make_uint4(0u, 0u, 0u, 0u);
     if (seq < a.N)
@@ -420,36 +411,34 @@ __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int 
   }
 }
 
-// Blocks: the shared rows' runs (unit, column block, split), the moment terms
-// (unit, column block), the tails (a run of one, or several short ones), each where
-// this launch has them.  A block of two groups (CG) has 64 columns, and no tails.
-template <int D, int NT, int CG>
-__global__ void __launch_bounds__(threads(CG), 3 - CG)
+// Blocks: the shared rows' runs (unit, split) and the moment terms (unit), where
+// they are this launch's, and the tails (a run of one, or several short ones).
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, 2)
     prefix_parts_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKt,
                         const __grid_constant__ CUtensorMap tmVt) {
-  constexpr int NS = stages(D, CG), kCols = 8 * NT * CG;
+  constexpr int NS = stages(D);
   extern __shared__ __align__(128) uint8_t raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-  __shared__ PartsShared<CG> sh;
-  const int tid = threadIdx.x, lane = tid & 31, group = tid >> 7;
-  const bool loads = group == CG;
-  uint8_t* sm = ring + NS * 2 * tile_bytes(D) + group * qp_bytes(D, NT);  // the group's query rows and weights
+  uint8_t* sm = ring + NS * 2 * tile_bytes(D);  // the query rows and the weights
+  __shared__ PartsShared sh;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const bool loads = tid >= kWarps * 32;
   if (tid < NS) {
     mbar_init(&sh.full[tid], 1);
-    mbar_init(&sh.empty[tid], kWarps * CG);
+    mbar_init(&sh.empty[tid], kWarps);
   }
-  if (tid == 0) sh.fail = 0;
-  if (tid < 2 * CG) sh.group[tid >> 1].moved[tid & 1] = 0;
+  if (tid == 0) sh.fail = sh.moved[0] = sh.moved[1] = 0;
   mbar_fence_init();
   // what this block's work is
   const int units = a.batch * a.n_kv, shared_blocks = units * a.blocks * a.splits;
-  const int moment_blocks = a.moments >= 0 ? units * a.blocks : 0;
+  const int moment_blocks = a.moments >= 0 ? units : 0;
   int x = blockIdx.x, kind = 0;
   if (x >= shared_blocks) x -= shared_blocks, kind = 1;
   if (kind == 1 && x >= moment_blocks) x -= moment_blocks, kind = 2;
   __syncthreads();
-  if (!a.late) grid_dependency_wait();
+  grid_dependency_wait();
   grid_launch_dependents();
   uint32_t seq = 0;
   auto run_of = [](int len, int splits, int split, int& row) {  // this split's rows of `len`
@@ -459,13 +448,13 @@ __global__ void __launch_bounds__(threads(CG), 3 - CG)
     return max(0, min(len, t1 * kRows) - t0 * kRows);
   };
   if (kind < 2) {
-    const int item = kind == 0 ? x / a.splits : x, split = kind == 0 ? x - item * a.splits : 0;
-    const int u = item / a.blocks, b = u / a.n_kv, kv = u - b * a.n_kv, first = (item - u * a.blocks) * kCols;
+    const int u = kind == 0 ? x / a.splits : x, split = kind == 0 ? x - u * a.splits : 0;
+    const int b = u / a.n_kv, kv = u - b * a.n_kv;
     const int counted = a.count != nullptr ? a.count[b] : a.N, have = kind == 0 ? a.len[u] : a.n[u];
-    if (!loads) stage_q<D>(a, b, kv, first + group * 8 * NT, 8 * NT, sm);
-    const int count = min(max(counted, 0), a.N), cols = count * a.group - first;
+    if (!loads) stage_q<D>(a, b, kv, 0, 8 * NT, sm);
+    const int count = min(max(counted, 0), a.N), cols = count * a.group;
     const int len = min(max(have, 0), a.cap);
-    if (kind == 0 && split == 0 && first == 0 && tid == 0) {
+    if (kind == 0 && split == 0 && tid == 0) {
       if (kv == 0 && count != counted) record_error(a.ws, MKV_ERR_INVALID_ARG, b);
       if (have != len) record_error(a.ws, MKV_ERR_CAPACITY, u);
     }
@@ -475,16 +464,15 @@ __global__ void __launch_bounds__(threads(CG), 3 - CG)
       if (loads) {
         if (lane == 0 && kind == 0) load_run<D, NS>(a, &tmK, &tmV, u * a.cap + row, n, ring, sh, seq);
       } else {
-        named_sync(1 + group, kWarps * 32);
-        const int from = first + group * 8 * NT, mine = min(8 * NT, cols - group * 8 * NT);
-        auto row_of = [&](int c) { return out_row(a, b, kv, from + c); };
+        named_sync(1, kWarps * 32);
+        auto row_of = [&](int c) { return out_row(a, b, kv, c); };
         if (kind == 0)
-          attend_run<D, NT, NS>(a, n, mine, split, ring, sm, sh, group, seq, row_of);
+          attend_run<D, NT, NS>(a, n, cols, split, ring, sm, sh, seq, row_of);
         else
-          moment_run<D, NT>(a, u, have, mine, sm, sh, group, row_of);
+          moment_run<D, NT>(a, u, have, cols, sm, sh, row_of);
       }
     }
-  } else if constexpr (CG == 1) {
+  } else {
     const int item = x / a.splits_t, split = x - item * a.splits_t;
     const int u0 = item * a.tails, mine = min(a.tails, units * a.N - u0);
     // the tails' lengths, a lane each (0 of a sequence that is not in use)
@@ -507,9 +495,9 @@ __global__ void __launch_bounds__(threads(CG), 3 - CG)
         const int first = (pair - b * a.N) * a.group;
         named_sync(1, kWarps * 32);  // (every warp is past the tail before)
         stage_q<D>(a, b, kv, first, 8, sm);
-        if (tid < 2) sh.group[0].moved[tid] = 0;
+        if (tid < 2) sh.moved[tid] = 0;
         named_sync(1, kWarps * 32);
-        attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, 0, seq, [&](int c) { return out_row(a, b, kv, first + c); });
+        attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, seq, [&](int c) { return out_row(a, b, kv, first + c); });
       }
     }
   }
@@ -519,7 +507,6 @@ __global__ void __launch_bounds__(threads(CG), 3 - CG)
     // the copies in flight land before the block ends
     for (uint32_t j = seq > NS ? seq - NS : 0; j < seq; ++j) (void)mbar_wait(&sh.full[j % NS], (j / NS) & 1);
   }
-  if (a.late) grid_dependency_wait();  // (the join waits for this launch, which stands for the one before too)
 }
 
 // A thread has 4 dims of a query row: the parts, then the new token, joined; the
@@ -602,52 +589,38 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_
   if (d0 == 0 && a.lse != nullptr) a.lse[row] = L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
 }
 
-// The parts of a query row, the splits, and the 8-column tiles (1, 2 or 4) and
-// groups (1 or 2) of a block.
-struct Shape {
-  int nt, cg;
-};
-Shape plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
+// The 8-column tiles of a block (1 or 2; 0: the shared rows run on tcgen05, whose
+// state is part 0), the parts of a query row and the splits.
+int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   const long units = (long)g.batch * g.n_kv_heads, rows = (long)a.N * g.group;
-  const Shape s{rows <= 8 ? 1 : rows <= 16 ? 2 : 4, rows <= 32 ? 1 : 2};
-  a.blocks = static_cast<int>((rows + 8 * s.nt * s.cg - 1) / (8 * s.nt * s.cg));
-  const long tiles = ((long)a.cap + kRows - 1) / kRows, tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
-  // runs of equal length, as many as there are places (two groups: a launch each for shared rows and tails)
-  const long places = 2 * num_sms, all = units * a.blocks * tiles, all_t = units * a.N * tiles_t;
-  const auto length = [&](long t, long p) { return std::max<long>(kMinTiles, (t + p - 1) / p); };
-  const long per = s.cg == 1 ? length(all + all_t, places) : length(all, num_sms);
-  const long per_t = s.cg == 1 ? per : length(all_t, places);
-  a.splits = static_cast<int>(std::min<long>(kMaxSplits, (tiles + per - 1) / per));
-  a.splits_t = static_cast<int>(std::min<long>(kMaxSplits, (tiles_t + per_t - 1) / per_t));
-  a.tails = static_cast<int>(std::clamp<long>(per_t / tiles_t, 1, kMaxTails));
-  a.moments = a.n != nullptr ? a.splits : -1;
-  a.tail = a.splits + (a.n != nullptr ? 1 : 0);
+  const int nt = rows <= 8 ? 1 : rows <= kTreeRows ? 2 : 0;
+  const long tiles = nt > 0 ? ((long)a.cap + kRows - 1) / kRows : 0, tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
+  const long moments = nt > 0 && a.n != nullptr ? 1 : 0;
+  // runs of equal length, as many as there are places
+  const long places = 2 * num_sms;
+  long per = std::max<long>(kMinTiles, (units * tiles + units * a.N * tiles_t + places - 1) / places);
+  const auto splits = [&](long t) { return std::min<long>(kMaxSplits, (t + per - 1) / per); };
+  const auto tails = [&] { return std::clamp<long>(per / tiles_t, 1, kMaxTails); };
+  // (a few blocks too many would be a second wave)
+  const auto blocks = [&] { return units * (splits(tiles) + moments) + (units * a.N + tails() - 1) / tails() * splits(tiles_t); };
+  for (const long first = per; blocks() > places; ++per)
+    if (per == 2 * first) {
+      per = first;
+      break;
+    }
+  a.splits = nt > 0 ? static_cast<int>(splits(tiles)) : 1;
+  a.splits_t = static_cast<int>(splits(tiles_t));
+  a.tails = static_cast<int>(tails());
+  a.blocks = nt > 0 ? 1 : 0;
+  a.moments = moments > 0 ? a.splits : -1;
+  a.tail = a.splits + static_cast<int>(moments);
   a.parts = a.tail + a.splits_t;
   a.rows = static_cast<int>(units * rows);
-  return s;
+  return nt;
 }
 
-// One launch: the shared rows and moments, the tails, or both.
-template <int D, int NT, int CG>
-cudaError_t launch_parts(PrefixArgs a, const CUtensorMap (&tm)[4], bool shared, bool tails, bool late, cudaStream_t stream) {
-  constexpr int smem = parts_smem(D, NT, CG);
-  cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  const long units = (long)a.batch * a.n_kv;
-  long blocks = 0;
-  if (shared)
-    blocks += units * a.blocks * (a.splits + (a.moments >= 0 ? 1 : 0));
-  else
-    a.blocks = 0, a.moments = -1;
-  if (tails) blocks += (units * a.N + a.tails - 1) / a.tails * a.splits_t;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  a.late = late ? 1 : 0;
-  return launch_pdl(prefix_parts_kernel<D, NT, CG>, dim3(static_cast<unsigned>(blocks)), dim3(threads(CG)), smem, stream,
-                    a, tm[0], tm[1], tm[2], tm[3]);
-}
-
-template <int D>
-cudaError_t launch(const PrefixArgs& a, const Shape& s, cudaStream_t stream) {
+template <int D, int NT>
+cudaError_t launch_parts(const PrefixArgs& a, cudaStream_t stream) {
   CUtensorMap tm[4];
   const uint64_t rows = (uint64_t)a.batch * a.n_kv * a.cap, rows_t = (uint64_t)a.batch * a.N * a.n_kv * a.cap_t;
   if (!encode_tmap_bf16(&tm[0], a.K, D, rows, (uint64_t)D * 2, 64, kRows) ||
@@ -655,15 +628,53 @@ cudaError_t launch(const PrefixArgs& a, const Shape& s, cudaStream_t stream) {
       !encode_tmap_bf16(&tm[2], a.Kt, D, rows_t, (uint64_t)D * 2, 64, kRows) ||
       !encode_tmap_bf16(&tm[3], a.Vt, D, rows_t, (uint64_t)D * 2, 64, kRows))
     return cudaErrorInvalidValue;
-  cudaError_t e;
-  if (s.cg == 1) {
-    e = s.nt == 1   ? launch_parts<D, 1, 1>(a, tm, true, true, false, stream)
-        : s.nt == 2 ? launch_parts<D, 2, 1>(a, tm, true, true, false, stream)
-                    : launch_parts<D, 4, 1>(a, tm, true, true, false, stream);
-  } else {
-    e = launch_parts<D, 1, 1>(a, tm, false, true, false, stream);
-    if (e == cudaSuccess) e = launch_parts<D, 4, 2>(a, tm, true, false, true, stream);
-  }
+  constexpr int smem = parts_smem(D, NT);
+  cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const long units = (long)a.batch * a.n_kv;
+  const long blocks = units * a.blocks * (a.splits + (a.moments >= 0 ? 1 : 0)) +
+                      (units * a.N + a.tails - 1) / a.tails * a.splits_t;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  return launch_pdl(prefix_parts_kernel<D, NT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), smem, stream, a,
+                    tm[0], tm[1], tm[2], tm[3]);
+}
+
+// The shared rows' and the moment term's states by the kernels of tree_step.cu, the
+// sequences as nodes that are no keys.  It loads early: what precedes it is the
+// tails' launch, which writes nothing that it reads and has waited for what did.
+cudaError_t launch_shared(const PrefixArgs& a, const mkv_geom& g, int num_sms, void* parts, cudaStream_t stream) {
+  TreeArgs t{};
+  t.q = a.q;
+  t.q_node = a.q_seq;
+  t.q_batch = a.q_batch;
+  t.N = a.N;
+  t.count = a.count;
+  t.K = a.K;
+  t.V = a.V;
+  t.len = a.len;
+  t.cap = a.cap;
+  t.n = a.n;
+  t.mu_k = a.mu_k;
+  t.mu_v = a.mu_v;
+  t.C = a.C;
+  t.C16 = a.C16;
+  t.Cs = a.Cs;
+  t.order = a.order;
+  t.tau = a.tau;
+  t.early = 1;
+  t.ws = a.ws;
+  t.parts = parts;
+  t.state_o = a.o;
+  t.state_ml = a.ml;
+  t.batch = a.batch;
+  t.n_kv = a.n_kv;
+  return launch_prefix_tree(t, g, num_sms, stream);
+}
+
+template <int D>
+cudaError_t launch(const PrefixArgs& a, const mkv_geom& g, int nt, int num_sms, void* parts, cudaStream_t stream) {
+  cudaError_t e = nt == 2 ? launch_parts<D, 2>(a, stream) : launch_parts<D, 1>(a, stream);
+  if (e == cudaSuccess && nt == 0) e = launch_shared(a, g, num_sms, parts, stream);
   if (e != cudaSuccess) return e;
   constexpr int kPer = kJoinThreads / (D / 4);
   return launch_pdl(prefix_join_kernel<D>, dim3((a.rows + kPer - 1) / kPer), dim3(kJoinThreads), 0, stream, a);
@@ -671,24 +682,27 @@ cudaError_t launch(const PrefixArgs& a, const Shape& s, cudaStream_t stream) {
 
 }  // namespace
 
-// Bytes of the parts: at most one run a place and one more of every column block
-// and tail, and the moment terms'; more than any smaller call needs.
-size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int32_t tail_capacity, int num_sms) {
-  (void)capacity, (void)tail_capacity;
-  const long units = (long)g.batch * g.n_kv_heads, rows = units * n_seqs * g.group;
-  // a column block's parts have at most 64 rows, a tail's at most 8
-  const long part_rows = 3 * rows + 2l * num_sms * 64 + 2l * num_sms * 8;
-  return kHeaderBytes + align_up(part_rows * sizeof(float2), 256) + (size_t)part_rows * g.head_dim * 4;
+// Bytes of the parts: of every query row one of the shared rows, the moment
+// term's and one of its tail, and as many more as there are places (up to 16 rows of a
+// unit, or 8 of a tail); more than any smaller call needs.
+size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms) {
+  const long rows = (long)g.batch * g.n_kv_heads * n_seqs * g.group;
+  const long part_rows = 3 * rows + 2l * num_sms * (kTreeRows + 8);
+  const size_t tree = prefix_tree_bytes(g, n_seqs, capacity, num_sms);
+  return kHeaderBytes + 256 + tree + align_up(part_rows * sizeof(float2), 256) + (size_t)part_rows * g.head_dim * 4;
 }
 
 cudaError_t launch_prefix_step(const PrefixArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
   PrefixArgs a = args;
   a.polls = pipeline_poll_limit();
-  const Shape s = plan(a, g, num_sms);
+  const int nt = plan(a, g, num_sms);
   uint8_t* w = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
   a.ml = reinterpret_cast<float2*>(w);
-  a.o = reinterpret_cast<float*>(w + align_up((size_t)a.parts * a.rows * sizeof(float2), 256));
-  return g.head_dim == 128 ? launch<128>(a, s, stream) : launch<64>(a, s, stream);
+  w += align_up((size_t)a.parts * a.rows * sizeof(float2), 256);
+  a.o = reinterpret_cast<float*>(w);
+  w += (size_t)a.parts * a.rows * g.head_dim * 4;
+  void* parts = reinterpret_cast<void*>(align_up(reinterpret_cast<uintptr_t>(w), 256));
+  return g.head_dim == 128 ? launch<128>(a, g, nt, num_sms, parts, stream) : launch<64>(a, g, nt, num_sms, parts, stream);
 }
 
 }  // namespace mkv

@@ -39,7 +39,7 @@ struct TreeArgs {
   int64_t q_node, q_batch, kv_node, kv_batch;
   int32_t N;
   const int32_t* count;  // [b] or null
-  const uint32_t* mask;  // [b, N, tree_words(N)]
+  const uint32_t* mask;  // [b, N, tree_words(N)]; null: the nodes are not keys
   const void* K;         // bf16 [b, Hkv, cap, D]
   const void* V;
   const int32_t* len;
@@ -57,10 +57,16 @@ struct TreeArgs {
   float* lse;
   uint32_t polls;  // poll limit of the pipeline waits
   void* ws;
+  void* parts;       // records of the items' parts
+  float* state_o;    // in place of out and lse: the rows' states [b, N, Hkv*G, D]
+  float2* state_ml;  // (reference, sum), log2 domain
   int32_t batch;
   int32_t n_kv;
 };
 
+// Rows of query rows that are not keys, left as states (mkv_prefix_step): the bytes of a.parts, and the launch.
+size_t prefix_tree_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms);
+cudaError_t launch_prefix_tree(const TreeArgs& a, const mkv_geom& g, int num_sms, cudaStream_t stream);
 size_t tree_workspace_bytes(const mkv_geom& g, int32_t n_nodes, int32_t capacity, int num_sms);
 cudaError_t launch_tree_step(const TreeArgs& a, const mkv_geom& g, int num_sms, cudaStream_t stream);
 

@@ -48,6 +48,9 @@
 // nodes, 131072 rows: 112 us, HBM's floor 79; 8 x 8 heads, 256 nodes, 4096 rows: 163
 // us, the tensor cores' floor 77); short items an item's start and end (4 x 8 heads,
 // 64 nodes, 1024 rows: 19.5 us).
+//
+// The same kernel serves mkv_prefix_step (prefix_step.cu): its sequences are nodes without keys
+// (no mask), and with PARTS a row's state (m, l, O), not yet divided by l, is what it leaves.
 #include <limits.h>
 #include <stddef.h>
 
@@ -307,7 +310,7 @@ __device__ __forceinline__ Item make_item(const TreeArgs& a, const Raw& r) {
   it.n_e = r.n_e;
   it.tail = a.n != nullptr ? 1 : 0;
   it.cache = (it.len + kTile - 1) / kTile;
-  it.nodes = (it.count + kTile - 1) / kTile;
+  it.nodes = a.mask != nullptr ? (it.count + kTile - 1) / kTile : 0;
   return it;
 }
 // Tiles of an item whose rows start at node `first` (at least one: its outputs have to be written).
@@ -525,7 +528,7 @@ __device__ __noinline__ void check_early(const TreeArgs& a, const Plan& p, const
   if (diff != 0) record_bad(a.ws, MKV_ERR_INVALID_ARG, sh.end > sh.start ? sh.unit : 0);
 }
 
-template <int D, int BLOCKS>
+template <int D, int BLOCKS, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_step_kernel(const __grid_constant__ TreeArgs a, const __grid_constant__ Plan p,
                      const __grid_constant__ Parts parts, const __grid_constant__ CUtensorMap tmQ,
@@ -1144,7 +1147,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (k1 > k0 + 1) f1 *= sh.w[r];
       }
       float w = mom && mine && e != kNegInf ? fast_exp2(e - M) * even : 0.f;
-      if (whole) {
+      if (whole && !PARTS) {
         const float inv = L != 0.f ? 1.f / L : 0.f;
         f0 *= inv, f1 *= inv, w *= inv;
       }
@@ -1198,7 +1201,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (use_f) o[i] = fmaf(__uint_as_float(x[i]), wf, o[i]);
           }
         }
-        if (whole) {
+        if (PARTS && whole) {
+          if (live) {
+            float* dst = a.state_o + orow * D + c_lo + c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(o[i]);
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store8(dst + i, x + i, true);
+          }
+        } else if (whole) {
           if (put) {
             __nv_bfloat16* dst = a.out + orow * D + c_lo + c;
 #pragma unroll
@@ -1236,7 +1247,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (BLOCKS == 2 || g == 0) {
-        if (whole) {
+        if (PARTS && whole) {
+          if (live) a.state_ml[orow] = make_float2(M, L);
+        } else if (whole) {
           if (put && a.lse != nullptr) a.lse[orow] = live ? log_sum(M, L) : kNegInf;
         } else if (warp_live) {
           parts.ml[(size_t)part * R + (BLOCKS == 2 ? g * kTile + r : r)] = make_float2(M, L);
@@ -1272,7 +1285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // latency: as many threads as the GPU holds at once are best, each with all of
 // its loads in flight.  A warp has 32 rows x 4 Q columns of an item; P warps
 // share them where there are few, every P-th part each.
-template <int D, int P, int Q>
+template <int D, int P, int Q, bool PARTS>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a,
                                                          const __grid_constant__ Plan p,
                                                          const __grid_constant__ Parts parts) {
@@ -1345,6 +1358,14 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   }
   if (node >= a.N) return;
   const size_t orow = ((size_t)b * a.N + node) * (a.n_kv << p.g_shift) + (kv << p.g_shift) + h;
+  if constexpr (PARTS) {
+#pragma unroll
+    for (int k = 0; k < Q; ++k)
+      reinterpret_cast<float4*>(a.state_o + orow * D)[c4 + k] =
+          make_float4(acc[4 * k], acc[4 * k + 1], acc[4 * k + 2], acc[4 * k + 3]);
+    if (c4 == 0) a.state_ml[orow] = make_float2(M, L);
+    return;
+  }
   const float inv = L != 0.f ? 1.f / L : 0.f;
 #pragma unroll
   for (int k = 0; k < Q; ++k)
@@ -1356,15 +1377,16 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
 }
 
 // Tiles of an item at most.
-long max_tiles(int n_nodes, int capacity) {
-  return 1 + ((long)capacity + kTile - 1) / kTile + (n_nodes + kTile - 1) / kTile;
+long max_tiles(int key_nodes, int capacity) {
+  return 1 + ((long)capacity + kTile - 1) / kTile + (key_nodes + kTile - 1) / kTile;
 }
 // CTAs of a list of so many tiles at most.
 int list_grid(long tiles, int num_sms) {
   return static_cast<int>(std::min<long>(num_sms, (tiles + kMinRun - 1) / kMinRun));
 }
 
-Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
+// (key_nodes: the nodes that are keys too, all or none)
+Plan make_plan(const mkv_geom& g, int n_nodes, int key_nodes, int capacity, int num_sms) {
   Plan p{};
   const int rows = n_nodes * g.group;
   p.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
@@ -1372,7 +1394,7 @@ Plan make_plan(const mkv_geom& g, int n_nodes, int capacity, int num_sms) {
   p.kv_inv = ((1ull << 40) + g.n_kv_heads - 1) / g.n_kv_heads;
   p.min_run = kMinRun;
   const long units = (long)g.batch * g.n_kv_heads;
-  const long tiles = max_tiles(n_nodes, capacity);
+  const long tiles = max_tiles(key_nodes, capacity);
   const auto items = [&](int blocks) { return units * ((rows + blocks * kTile - 1) / (blocks * kTile)); };
   // One row block per CTA spreads few, short items over more SMs; two read K and
   // V once for 256 rows.  Measured, one and two: 4 x 8 heads, 64 nodes of 4
@@ -1426,13 +1448,13 @@ bool encode_4d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t n1, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int BLOCKS>
+template <int D, int BLOCKS, bool PARTS>
 cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, const CUtensorMap (&tm)[5],
                         int num_sms, cudaStream_t stream) {
   constexpr int smem = smem_bytes(D, BLOCKS);
-  cudaError_t e = cudaFuncSetAttribute(tree_step_kernel<D, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(tree_step_kernel<D, BLOCKS, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(tree_step_kernel<D, BLOCKS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
+  e = launch_pdl(tree_step_kernel<D, BLOCKS, PARTS>, dim3(p.grid), dim3(kThreads), smem, stream, a, p, parts, tm[0], tm[1], tm[2],
                  tm[3], tm[4]);
   if (e != cudaSuccess || !p.list) return e;
   // threads if each had 4 columns of a row: at most grid - 1 items are cut, and
@@ -1442,36 +1464,21 @@ cudaError_t launch_step(const TreeArgs& a, const Plan& p, const Parts& parts, co
   const auto merge = [&](auto kernel, int P, int Q) {
     return launch_pdl(kernel, dim3(static_cast<unsigned>(units * P / Q / 8)), dim3(256), 0, stream, a, p, parts);
   };
-  if (cut * 8 <= most) return merge(tree_merge_kernel<D, 8, 1>, 8, 1);
-  if (cut * 4 <= most) return merge(tree_merge_kernel<D, 4, 1>, 4, 1);
-  if (cut * 2 <= most) return merge(tree_merge_kernel<D, 2, 1>, 2, 1);
-  if (cut <= most) return merge(tree_merge_kernel<D, 1, 1>, 1, 1);
-  return merge(tree_merge_kernel<D, 1, 4>, 1, 4);
+  if (cut * 8 <= most) return merge(tree_merge_kernel<D, 8, 1, PARTS>, 8, 1);
+  if (cut * 4 <= most) return merge(tree_merge_kernel<D, 4, 1, PARTS>, 4, 1);
+  if (cut * 2 <= most) return merge(tree_merge_kernel<D, 2, 1, PARTS>, 2, 1);
+  if (cut <= most) return merge(tree_merge_kernel<D, 1, 1, PARTS>, 1, 1);
+  return merge(tree_merge_kernel<D, 1, 4, PARTS>, 1, 4);
 }
 
-}  // namespace
-
-// Enough for the plan of every batch, number of nodes and capacity up to these:
-// plans change with each of them, and only lists have parts, so that a smaller
-// tree can need more than a larger one.
-size_t tree_workspace_bytes(const mkv_geom& g, int32_t n_nodes, int32_t capacity, int num_sms) {
-  const long units = std::min<long>((long)g.batch * g.n_kv_heads, kScanUnits), rows = (long)n_nodes * g.group;
-  const long tiles = max_tiles(n_nodes, capacity);
-  size_t most = 0;
-  for (int blocks = 1; blocks <= (rows > kTile ? 2 : 1); ++blocks) {
-    const long items = units * ((rows + blocks * kTile - 1) / (blocks * kTile));
-    most = std::max(most, parts_bytes(items, blocks, list_grid(items * tiles, num_sms), g.head_dim));
-  }
-  return kHeaderBytes + most;
-}
-
-cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
+template <bool PARTS>
+cudaError_t launch_tree(const TreeArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
   TreeArgs a = args;
   a.polls = pipeline_poll_limit();
-  const Plan p = make_plan(g, a.N, a.cap, num_sms);
+  const Plan p = make_plan(g, a.N, a.mask != nullptr ? a.N : 0, a.cap, num_sms);
   Parts parts{};
   const int D = g.head_dim, R = p.blocks * kTile;
-  uint8_t* w = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
+  uint8_t* w = static_cast<uint8_t*>(a.parts);
   parts.desc = reinterpret_cast<int2*>(w);
   w += align_up((size_t)a.batch * a.n_kv * p.mb * sizeof(int2), 256);
   parts.o = reinterpret_cast<float4*>(w);
@@ -1481,13 +1488,52 @@ cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sm
   CUtensorMap tm[5];
   if (!encode_4d(&tm[0], a.q, d, hq, a.N, a.batch, d, a.q_node, a.q_batch, g.group, kTile / g.group) ||
       !encode_tmap_bf16_3d(&tm[1], a.K, d, a.cap, units, d * 2, (uint64_t)a.cap * d * 2, kTile) ||
-      !encode_tmap_bf16_3d(&tm[2], a.V, d, a.cap, units, d * 2, (uint64_t)a.cap * d * 2, kTile) ||
-      !encode_4d(&tm[3], a.k, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile) ||
-      !encode_4d(&tm[4], a.v, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile))
+      !encode_tmap_bf16_3d(&tm[2], a.V, d, a.cap, units, d * 2, (uint64_t)a.cap * d * 2, kTile))
+    return cudaErrorInvalidValue;
+  tm[3] = tm[4] = tm[0];  // (nodes without keys: not read)
+  if (a.mask != nullptr &&
+      (!encode_4d(&tm[3], a.k, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile) ||
+       !encode_4d(&tm[4], a.v, d, a.n_kv, a.N, a.batch, d, a.kv_node, a.kv_batch, 1, kTile)))
     return cudaErrorInvalidValue;
   if (D == 128)
-    return p.blocks == 2 ? launch_step<128, 2>(a, p, parts, tm, num_sms, stream) : launch_step<128, 1>(a, p, parts, tm, num_sms, stream);
-  return p.blocks == 2 ? launch_step<64, 2>(a, p, parts, tm, num_sms, stream) : launch_step<64, 1>(a, p, parts, tm, num_sms, stream);
+    return p.blocks == 2 ? launch_step<128, 2, PARTS>(a, p, parts, tm, num_sms, stream)
+                         : launch_step<128, 1, PARTS>(a, p, parts, tm, num_sms, stream);
+  return p.blocks == 2 ? launch_step<64, 2, PARTS>(a, p, parts, tm, num_sms, stream)
+                       : launch_step<64, 1, PARTS>(a, p, parts, tm, num_sms, stream);
+}
+
+// Bytes of the parts' records, enough for the plan of every batch, number of
+// nodes and capacity up to these: plans change with each of them, and only
+// lists have parts, so that a smaller tree can need more than a larger one.
+size_t tree_parts_bytes(const mkv_geom& g, int32_t n_nodes, int32_t key_nodes, int32_t capacity, int num_sms) {
+  const long units = std::min<long>((long)g.batch * g.n_kv_heads, kScanUnits), rows = (long)n_nodes * g.group;
+  const long tiles = max_tiles(key_nodes, capacity);
+  size_t most = 0;
+  for (int blocks = 1; blocks <= (rows > kTile ? 2 : 1); ++blocks) {
+    const long items = units * ((rows + blocks * kTile - 1) / (blocks * kTile));
+    most = std::max(most, parts_bytes(items, blocks, list_grid(items * tiles, num_sms), g.head_dim));
+  }
+  return most;
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(const mkv_geom& g, int32_t n_nodes, int32_t capacity, int num_sms) {
+  return kHeaderBytes + tree_parts_bytes(g, n_nodes, n_nodes, capacity, num_sms);
+}
+
+cudaError_t launch_tree_step(const TreeArgs& args, const mkv_geom& g, int num_sms, cudaStream_t stream) {
+  TreeArgs a = args;
+  a.parts = static_cast<uint8_t*>(a.ws) + kHeaderBytes;
+  return launch_tree<false>(a, g, num_sms, stream);
+}
+
+size_t prefix_tree_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms) {
+  return tree_parts_bytes(g, n_seqs, 0, capacity, num_sms);
+}
+
+cudaError_t launch_prefix_tree(const TreeArgs& a, const mkv_geom& g, int num_sms, cudaStream_t stream) {
+  return launch_tree<true>(a, g, num_sms, stream);
 }
 
 }  // namespace mkv
