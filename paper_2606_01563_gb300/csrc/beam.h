@@ -50,7 +50,7 @@ struct PrefixArgs {
   float2* ml;        // [parts][rows]: reference and sum, log2 domain
   float* o;          // [parts][rows][D]: sum of weighted values about the reference
   int32_t rows;      // b * N * Hkv * G
-  int32_t blocks;    // 1: the shared rows and moments are prefix_parts_kernel's, 0: another's
+  int32_t blocks;    // column blocks of a unit's query rows (0: the shared rows and moments are another launch's)
   int32_t splits;    // parts of the shared rows; part 0 is the first
   int32_t moments;   // the moment term's part, or -1
   int32_t tail;      // the tails' first part

@@ -44,7 +44,7 @@ constexpr int kRows = 64;                   // rows of a tile
 constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
 constexpr int kMaxTails = 8;   // tails of a block
-constexpr long kTreeRows = 16;  // query rows of a unit above which the shared rows run on tcgen05
+constexpr long kVisits = 100000;
 constexpr float kSlack = 8.f;  // log2 headroom of a reference (weights at most 2^8)
 constexpr float kNegInf = -INFINITY;
 constexpr int kJoinThreads = 256;
@@ -59,7 +59,7 @@ constexpr int kPPitch = kRows * 2 + 16;
 __host__ __device__ constexpr int p_offset(int D, int NT, int buffer) { return buffer == 0 ? 0 : 8 * NT * q_pitch(D); }
 __host__ __device__ constexpr int qp_bytes(int D, int NT) { return p_offset(D, NT, 1) + 8 * NT * kPPitch; }
 __host__ __device__ constexpr int parts_smem(int D, int NT) { return stages(D) * 2 * tile_bytes(D) + qp_bytes(D, NT) + 1024; }
-static_assert(2 * (parts_smem(128, 2) + 3072) <= 228 * 1024, "two blocks to an SM");
+static_assert(2 * (parts_smem(128, 4) + 3072) <= 228 * 1024, "two blocks to an SM");
 
 // A query row of a unit: sequence r / G, head r % G.
 __device__ __forceinline__ int64_t out_row(const PrefixArgs& a, int b, int kv, int r) {
@@ -70,7 +70,7 @@ __device__ __forceinline__ int live_seqs(const PrefixArgs& a, int b) {
   return a.count != nullptr ? min(max(a.count[b], 0), a.N) : a.N;
 }
 
-constexpr int kMaxCols = kTreeRows;
+constexpr int kMaxCols = 32;  // query rows of a block at most
 struct PartsShared {
   uint64_t full[kMaxStages], empty[kMaxStages];
   float l[kWarps][kMaxCols][2];  // of a warp and column: the weights' sum and the rounded ones'
@@ -315,44 +315,23 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
     }
 }
 
-// The moment term's state of unit u for `cols` query rows (sQ): a warp has 16
-// dims of C' q at a time, C' (clamped) as bf16 hi + lo parts, or in the forms it was packed in.
+// The moment term's state of unit u for `cols` query rows (sQ, being written): 64
+// dims of it from 64 `piece` on, 16 of C' q to a warp, C' (clamped) as bf16 hi + lo
+// parts, or in the forms it was packed in; the logits with the first piece.
 template <int D, int NT, typename RowOf>
-__device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, int cols, const uint8_t* sQ,
+__device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, int piece, int cols, const uint8_t* sQ,
                                            PartsShared& sh, RowOf row_of) {
   constexpr int KS = D / 16;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const float scale = rsqrtf(static_cast<float>(D));
-  if (n_e > 0)
-    for (int i = tid; i < D; i += kWarps * 32) sh.mu_k[i] = a.mu_k[(size_t)u * D + i];
-  named_sync(1, kWarps * 32);
-  // four threads a column (a warp has eight: all of them take every turn, for the shuffles)
-  for (int c = tid >> 2; c < 8 * NT; c += kWarps * 8) {
-    float e = 0.f;
-    if (n_e > 0) {
-#pragma unroll 4
-      for (int i = (tid & 3) * 2; i < D; i += 8) {
-        const float2 q = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(sQ + c * q_pitch(D) + i * 2));
-        e = fmaf(q.x, sh.mu_k[i], fmaf(q.y, sh.mu_k[i + 1], e));
-      }
-    }
-    e += __shfl_xor_sync(0xffffffffu, e, 1);
-    e += __shfl_xor_sync(0xffffffffu, e, 2);
-    if ((tid & 3) == 0 && c < cols) {
-      const float x = n_e > 0 ? fmaf(e, scale * kLog2e, log2f(static_cast<float>(n_e))) : kNegInf;
-      a.ml[(size_t)a.moments * a.rows + row_of(c)] = make_float2(x, x != kNegInf ? 1.f : 0.f);
-    }
-  }
-  if (n_e <= 0) return;
-  named_sync(1, kWarps * 32);
-  const float nf = static_cast<float>(n_e), tau = a.tau;
-  for (int mt = warp; mt < D / 16; mt += kWarps) {
-    const int ra = mt * 16 + g, rb = ra + 8;
-    float f[NT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) f[nt][0] = f[nt][1] = f[nt][2] = f[nt][3] = 0.f;
+  const int ra = piece * 64 + warp * 16 + g, rb = ra + 8;
+  float2 cf[KS][4] = {};
+  float va = 0.f, vb = 0.f;
+  if (n_e > 0) {
+    va = a.mu_v[(size_t)u * D + ra], vb = a.mu_v[(size_t)u * D + rb];
+    if (piece == 0)
+      for (int i = tid; i < D; i += kWarps * 32) sh.mu_k[i] = a.mu_k[(size_t)u * D + i];
     if (a.order == 1) {
-      float2 cf[KS][4];
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
@@ -362,40 +341,62 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
                       : a.Cs != nullptr ? *reinterpret_cast<const float2*>(a.Cs + off / 2)
                                         : *reinterpret_cast<const float2*>(a.C + off);
         }
-#pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (a.Cs != nullptr) {
-            hi[i] = __float_as_uint(cf[kk][i].x);
-            lo[i] = __float_as_uint(cf[kk][i].y);
-          } else {
-            const float x = fabsf(cf[kk][i].x * nf) < tau ? 0.f : cf[kk][i].x;
-            const float y = fabsf(cf[kk][i].y * nf) < tau ? 0.f : cf[kk][i].y;
-            hi[i] = pack_bf16x2(x, y);
-            lo[i] = pack_bf16x2(bf16_residual(x), bf16_residual(y));  // (0 of a 16-bit C)
-          }
+    }
+  }
+  named_sync(1, kWarps * 32);
+  if (piece == 0) {
+    // four threads a column (a warp has eight: all of them take every turn, for the shuffles)
+    for (int c = tid >> 2; c < 8 * NT; c += kWarps * 8) {
+      float e = 0.f;
+      if (n_e > 0) {
+#pragma unroll 4
+        for (int i = (tid & 3) * 2; i < D; i += 8) {
+          const float2 q = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(sQ + c * q_pitch(D) + i * 2));
+          e = fmaf(q.x, sh.mu_k[i], fmaf(q.y, sh.mu_k[i + 1], e));
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const uint8_t* p = sQ + (nt * 8 + g) * q_pitch(D) + kk * 32 + t * 4;
-          const uint32_t b0 = *reinterpret_cast<const uint32_t*>(p), b1 = *reinterpret_cast<const uint32_t*>(p + 16);
-          mma_m16n8k16(f[nt], hi[0], hi[1], hi[2], hi[3], b0, b1);
-          mma_m16n8k16(f[nt], lo[0], lo[1], lo[2], lo[3], b0, b1);
-        }
+      }
+      e += __shfl_xor_sync(0xffffffffu, e, 1);
+      e += __shfl_xor_sync(0xffffffffu, e, 2);
+      if ((tid & 3) == 0 && c < cols) {
+        const float x = n_e > 0 ? fmaf(e, scale * kLog2e, log2f(static_cast<float>(n_e))) : kNegInf;
+        a.ml[(size_t)a.moments * a.rows + row_of(c)] = make_float2(x, x != kNegInf ? 1.f : 0.f);
       }
     }
-    const float va = a.mu_v[(size_t)u * D + ra], vb = a.mu_v[(size_t)u * D + rb];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = nt * 8 + 2 * t + (i & 1);
-        if (c < cols)
-          a.o[((size_t)a.moments * a.rows + row_of(c)) * D + (i >> 1 ? rb : ra)] = fmaf(scale, f[nt][i], i >> 1 ? vb : va);
-      }
   }
+  if (n_e <= 0) return;
+  const float nf = static_cast<float>(n_e), tau = a.tau;
+  float f[NT][4] = {};
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (a.Cs != nullptr) {
+        hi[i] = __float_as_uint(cf[kk][i].x);
+        lo[i] = __float_as_uint(cf[kk][i].y);
+      } else {
+        const float x = fabsf(cf[kk][i].x * nf) < tau ? 0.f : cf[kk][i].x;
+        const float y = fabsf(cf[kk][i].y * nf) < tau ? 0.f : cf[kk][i].y;
+        hi[i] = pack_bf16x2(x, y);
+        lo[i] = pack_bf16x2(bf16_residual(x), bf16_residual(y));  // (0 of a 16-bit C)
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint8_t* p = sQ + (nt * 8 + g) * q_pitch(D) + kk * 32 + t * 4;
+      const uint32_t b0 = *reinterpret_cast<const uint32_t*>(p), b1 = *reinterpret_cast<const uint32_t*>(p + 16);
+      mma_m16n8k16(f[nt], hi[0], hi[1], hi[2], hi[3], b0, b1);
+      mma_m16n8k16(f[nt], lo[0], lo[1], lo[2], lo[3], b0, b1);
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = nt * 8 + 2 * t + (i & 1);
+      if (c < cols)
+        a.o[((size_t)a.moments * a.rows + row_of(c)) * D + (i >> 1 ? rb : ra)] = fmaf(scale, f[nt][i], i >> 1 ? vb : va);
+    }
 }
 
 // Query rows of unit (b, kv) from row `first` on into shared memory, `wide` of them, zeros where there is none.
@@ -411,8 +412,8 @@ __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int 
   }
 }
 
-// Blocks: the shared rows' runs (unit, split) and the moment terms (unit), where
-// they are this launch's, and the tails (a run of one, or several short ones).
+// Blocks: the shared rows' runs (unit, column block, split) and the moment terms
+// (unit, column block), where they are this launch's, and the tails (a run of one, or several short ones).
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, 2)
     prefix_parts_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap tmK,
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   mbar_fence_init();
   // what this block's work is
   const int units = a.batch * a.n_kv, shared_blocks = units * a.blocks * a.splits;
-  const int moment_blocks = a.moments >= 0 ? units : 0;
+  const int moment_blocks = a.moments >= 0 ? units * a.blocks * (D / 64) : 0;
   int x = blockIdx.x, kind = 0;
   if (x >= shared_blocks) x -= shared_blocks, kind = 1;
   if (kind == 1 && x >= moment_blocks) x -= moment_blocks, kind = 2;
@@ -448,13 +449,14 @@ __global__ void __launch_bounds__(kThreads, 2)
     return max(0, min(len, t1 * kRows) - t0 * kRows);
   };
   if (kind < 2) {
-    const int u = kind == 0 ? x / a.splits : x, split = kind == 0 ? x - u * a.splits : 0;
-    const int b = u / a.n_kv, kv = u - b * a.n_kv;
+    const int each = kind == 0 ? a.splits : D / 64;  // blocks of an item: its runs, or the pieces of its moment term
+    const int item = x / each, split = x - item * each;
+    const int u = item / a.blocks, b = u / a.n_kv, kv = u - b * a.n_kv, first = (item - u * a.blocks) * 8 * NT;
     const int counted = a.count != nullptr ? a.count[b] : a.N, have = kind == 0 ? a.len[u] : a.n[u];
-    if (!loads) stage_q<D>(a, b, kv, 0, 8 * NT, sm);
-    const int count = min(max(counted, 0), a.N), cols = count * a.group;
+    if (!loads) stage_q<D>(a, b, kv, first, 8 * NT, sm);
+    const int count = min(max(counted, 0), a.N), cols = min(8 * NT, count * a.group - first);
     const int len = min(max(have, 0), a.cap);
-    if (kind == 0 && split == 0 && tid == 0) {
+    if (kind == 0 && split == 0 && first == 0 && tid == 0) {
       if (kv == 0 && count != counted) record_error(a.ws, MKV_ERR_INVALID_ARG, b);
       if (have != len) record_error(a.ws, MKV_ERR_CAPACITY, u);
     }
@@ -464,12 +466,13 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (loads) {
         if (lane == 0 && kind == 0) load_run<D, NS>(a, &tmK, &tmV, u * a.cap + row, n, ring, sh, seq);
       } else {
-        named_sync(1, kWarps * 32);
-        auto row_of = [&](int c) { return out_row(a, b, kv, c); };
-        if (kind == 0)
+        auto row_of = [&](int c) { return out_row(a, b, kv, first + c); };
+        if (kind == 0) {
+          named_sync(1, kWarps * 32);
           attend_run<D, NT, NS>(a, n, cols, split, ring, sm, sh, seq, row_of);
-        else
-          moment_run<D, NT>(a, u, have, cols, sm, sh, row_of);
+        } else {
+          moment_run<D, NT>(a, u, have, split, cols, sm, sh, row_of);
+        }
       }
     }
   } else {
@@ -483,22 +486,41 @@ __global__ void __launch_bounds__(kThreads, 2)
       len_all = live_all ? min(max(have, 0), a.cap_t) : 0;
       if (live_all && have != len_all && split == 0 && loads) record_error(a.ws, MKV_ERR_CAPACITY, u);
     }
+    // a tail's query rows: 16 bytes a thread, the next tail's on their way while one is worked on
+    auto query = [&](int i) {
+      const int u = u0 + i, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
+      const int c = tid / (D / 8), k = tid % (D / 8);
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (i < mine && c < a.group)
+        w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch +
+                                            (pair - b * a.N) * a.q_seq + (kv * a.group + c) * D + k * 8);
+      return w;
+    };
+    uint4 next = make_uint4(0u, 0u, 0u, 0u);
+    if (!loads) next = query(0);
     for (int i = 0; i < mine; ++i) {
       const int u = u0 + i, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
       int row;
       const int n = run_of(__shfl_sync(0xffffffffu, len_all, i), a.splits_t, split, row);
-      if (!__shfl_sync(0xffffffffu, live_all, i)) continue;
+      const bool live = __shfl_sync(0xffffffffu, live_all, i) != 0;
       if (loads) {
-        if (lane == 0) load_run<D, NS>(a, &tmKt, &tmVt, u * a.cap_t + row, n, ring, sh, seq);
+        if (lane == 0 && live) load_run<D, NS>(a, &tmKt, &tmVt, u * a.cap_t + row, n, ring, sh, seq);
         __syncwarp();
-      } else {
-        const int first = (pair - b * a.N) * a.group;
-        named_sync(1, kWarps * 32);  // (every warp is past the tail before)
-        stage_q<D>(a, b, kv, first, 8, sm);
-        if (tid < 2) sh.moved[tid] = 0;
-        named_sync(1, kWarps * 32);
-        attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, seq, [&](int c) { return out_row(a, b, kv, first + c); });
+        continue;
       }
+      const uint4 w = next;
+      next = query(i + 1);
+      if (!live) continue;
+      const int first = (pair - b * a.N) * a.group;
+      if (n == 0) {  // (nothing but the new token yet)
+        if (tid < a.group) a.ml[(size_t)(a.tail + split) * a.rows + out_row(a, b, kv, first + tid)] = make_float2(kNegInf, 0.f);
+        continue;
+      }
+      named_sync(1, kWarps * 32);  // (every warp is past the tail before)
+      if (tid < D) *reinterpret_cast<uint4*>(sm + tid / (D / 8) * q_pitch(D) + tid % (D / 8) * 16) = w;
+      if (tid < 2) sh.moved[tid] = 0;
+      named_sync(1, kWarps * 32);
+      attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, seq, [&](int c) { return out_row(a, b, kv, first + c); });
     }
   }
   __syncthreads();
@@ -509,71 +531,96 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
 }
 
-// A thread has 4 dims of a query row: the parts, then the new token, joined; the
-// first row of a unit appends the token to the tail.
-template <int D>
+struct State {
+  float m, l, o[4];
+};
+__device__ __forceinline__ void join(State& s, float m, float l, const float4& v) {
+  const float mn = fmaxf(s.m, m), ref = mn == kNegInf ? 0.f : mn;
+  const float f0 = s.l != 0.f ? fast_exp2(s.m - ref) : 0.f, f = fast_exp2(m - ref);
+  s.m = mn;
+  s.l = s.l * f0 + l * f;
+  s.o[0] = fmaf(v.x, f, s.o[0] * f0);
+  s.o[1] = fmaf(v.y, f, s.o[1] * f0);
+  s.o[2] = fmaf(v.z, f, s.o[2] * f0);
+  s.o[3] = fmaf(v.w, f, s.o[3] * f0);
+}
+
+// P threads share 4 dims of a query row, every P-th part each; the first joins
+// theirs and the new token, and a unit's first row appends that token to its tail.
+template <int D, int P>
 __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_constant__ PrefixArgs a) {
-  constexpr int kLanes = D / 4;
-  grid_dependency_wait();
-  grid_launch_dependents();
-  const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / kLanes) + threadIdx.x / kLanes;
-  const int d0 = (threadIdx.x % kLanes) * 4;
-  if (row >= a.rows) return;
-  const uint32_t mask = kLanes == 32 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16);
+  constexpr int kLanes = D / 4, kPer = kJoinThreads / kLanes / P;  // rows of a block
+  __shared__ State others[P > 1 ? P - 1 : 1][P > 1 ? kPer * kLanes : 1];
+  const int at_row = threadIdx.x / kLanes % kPer, slice = threadIdx.x / kLanes / kPer, lane = threadIdx.x % kLanes;
+  const int64_t row = (int64_t)blockIdx.x * kPer + at_row;
+  const int d0 = lane * 4;
+  const bool in = row < a.rows;
   const int h = static_cast<int>(row % a.group), ut = static_cast<int>(row / a.group);  // head, tail unit
   const int kv = ut % a.n_kv, pair = ut / a.n_kv, b = pair / a.N, seq = pair - b * a.N;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  // four parts' loads at a time in flight, whether they hold anything or not
+  State s{kNegInf, 0.f, {}};
+  const bool token = a.k_new != nullptr && slice == 0 && in;
+  uint2 kw{}, vw{}, qw{};
+  int len = 0, seen = 0;
+  if (token) {
+    const int64_t at = b * a.kv_batch + seq * a.kv_seq + kv * D + d0;
+    kw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.k_new) + at);
+    vw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.v_new) + at);
+    qw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + seq * a.q_seq +
+                                         (kv * a.group + h) * D + d0);
+    if (h == 0) len = a.len_t[ut], seen = a.seen_t[ut];
+  }
+  const bool live = in && seq < live_seqs(a, b);
+  if (live) {
+    for (int p0 = slice; p0 < a.parts; p0 += 4 * P) {
+      float2 ml[4];
+      float4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const size_t at = (size_t)min(p0 + i * P, a.parts - 1) * a.rows + row;
+        ml[i] = a.ml[at];
+        v[i] = *reinterpret_cast<const float4*>(a.o + at * D + d0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p0 + i * P < a.parts && ml[i].y != 0.f) join(s, ml[i].x, ml[i].y, v[i]);
+    }
+  }
+  if constexpr (P > 1) {
+    if (slice > 0) others[slice - 1][at_row * kLanes + lane] = s;
+    __syncthreads();
+    if (slice > 0) return;
+#pragma unroll
+    for (int i = 0; i < P - 1; ++i) {
+      const State& x = others[i][at_row * kLanes + lane];
+      if (x.l != 0.f) join(s, x.m, x.l, make_float4(x.o[0], x.o[1], x.o[2], x.o[3]));
+    }
+  }
+  if (!in) return;
   uint2* dst = reinterpret_cast<uint2*>(a.out + row * D + d0);
-  if (seq >= live_seqs(a, b)) {
+  if (!live) {
     *dst = make_uint2(0u, 0u);
     if (d0 == 0 && a.lse != nullptr) a.lse[row] = kNegInf;
     return;
   }
-  float M = kNegInf, L = 0.f, acc[4] = {};
-  auto join = [&](float m, float l, const float4& v) {
-    const float mn = fmaxf(M, m), ref = mn == kNegInf ? 0.f : mn;
-    const float f0 = L != 0.f ? fast_exp2(M - ref) : 0.f, f = fast_exp2(m - ref);
-    M = mn;
-    L = L * f0 + l * f;
-    acc[0] = fmaf(v.x, f, acc[0] * f0);
-    acc[1] = fmaf(v.y, f, acc[1] * f0);
-    acc[2] = fmaf(v.z, f, acc[2] * f0);
-    acc[3] = fmaf(v.w, f, acc[3] * f0);
-  };
-  // four parts' loads at a time in flight (what an empty part's O holds is not used)
-  for (int p0 = 0; p0 < a.parts; p0 += 4) {
-    float2 ml[4];
-    float4 v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const size_t at = (size_t)min(p0 + i, a.parts - 1) * a.rows + row;
-      ml[i] = a.ml[at];
-      v[i] = *reinterpret_cast<const float4*>(a.o + at * D + d0);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (p0 + i < a.parts && ml[i].y != 0.f) join(ml[i].x, ml[i].y, v[i]);
-  }
-  if (a.k_new != nullptr) {
-    const int64_t at = b * a.kv_batch + seq * a.kv_seq + kv * D + d0;
-    const uint2 kw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.k_new) + at);
-    const uint2 vw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.v_new) + at);
-    const uint2 qw = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch +
-                                                     seq * a.q_seq + (kv * a.group + h) * D + d0);
+  if (token) {
+    const uint32_t mask = kLanes == 32 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16);  // the row's lanes
     auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
     auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
-    float s = lo(qw.x) * lo(kw.x) + hi(qw.x) * hi(kw.x) + lo(qw.y) * lo(kw.y) + hi(qw.y) * hi(kw.y);
+    float x = lo(qw.x) * lo(kw.x) + hi(qw.x) * hi(kw.x) + lo(qw.y) * lo(kw.y) + hi(qw.y) * hi(kw.y);
 #pragma unroll
-    for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor_sync(mask, s, off);
-    join(s * rsqrtf(static_cast<float>(D)) * kLog2e, 1.f, make_float4(lo(vw.x), hi(vw.x), lo(vw.y), hi(vw.y)));
+    for (int off = kLanes / 2; off > 0; off >>= 1) x += __shfl_xor_sync(mask, x, off);
+    join(s, x * rsqrtf(static_cast<float>(D)) * kLog2e, 1.f, make_float4(lo(vw.x), hi(vw.x), lo(vw.y), hi(vw.y)));
     if (h == 0) {
-      const int len = min(max(a.len_t[ut], 0), a.cap_t);
-      __syncwarp(mask);
+      len = min(max(len, 0), a.cap_t);
+      __syncwarp(mask);  // (all have read the length)
       if (len < a.cap_t) {
         const size_t slot = (size_t)ut * a.cap_t + len;
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.Kt) + slot * D + d0) = kw;
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.Vt) + slot * D + d0) = vw;
         if (d0 == 0) {
-          const int seen = a.seen_t[ut];
           a.pos_t[slot] = seen;
           a.seen_t[ut] = seen + 1;
           a.len_t[ut] = len + 1;
@@ -583,27 +630,29 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_
       }
     }
   }
-  const float inv = L != 0.f ? 1.f / L : 0.f;
-  *dst = L != 0.f ? make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv))
-                  : make_uint2(0u, 0u);
-  if (d0 == 0 && a.lse != nullptr) a.lse[row] = L != 0.f ? (M + log2f(L)) * kLn2 : kNegInf;
+  const float inv = s.l != 0.f ? 1.f / s.l : 0.f;
+  *dst = s.l != 0.f ? make_uint2(pack_bf16x2(s.o[0] * inv, s.o[1] * inv), pack_bf16x2(s.o[2] * inv, s.o[3] * inv))
+                    : make_uint2(0u, 0u);
+  if (d0 == 0 && a.lse != nullptr) a.lse[row] = s.l != 0.f ? (s.m + log2f(s.l)) * kLn2 : kNegInf;
 }
 
-// The 8-column tiles of a block (1 or 2; 0: the shared rows run on tcgen05, whose
+// The 8-column tiles of a block (1, 2 or 4; 0: the shared rows run on tcgen05, whose
 // state is part 0), the parts of a query row and the splits.
 int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
-  const long units = (long)g.batch * g.n_kv_heads, rows = (long)a.N * g.group;
-  const int nt = rows <= 8 ? 1 : rows <= kTreeRows ? 2 : 0;
-  const long tiles = nt > 0 ? ((long)a.cap + kRows - 1) / kRows : 0, tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
+  const long units = (long)g.batch * g.n_kv_heads, rows = (long)a.N * g.group, places = 2 * num_sms;
+  long tiles = ((long)a.cap + kRows - 1) / kRows;
+  const long tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
+  int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  long blocks = (rows + 8 * nt - 1) / (8 * nt);
+  if (nt == 4 && units * blocks * tiles > kVisits * places) nt = 0, blocks = 0, tiles = 0;
   const long moments = nt > 0 && a.n != nullptr ? 1 : 0;
   // runs of equal length, as many as there are places
-  const long places = 2 * num_sms;
-  long per = std::max<long>(kMinTiles, (units * tiles + units * a.N * tiles_t + places - 1) / places);
+  long per = std::max<long>(kMinTiles, (units * blocks * tiles + units * a.N * tiles_t + places - 1) / places);
   const auto splits = [&](long t) { return std::min<long>(kMaxSplits, (t + per - 1) / per); };
   const auto tails = [&] { return std::clamp<long>(per / tiles_t, 1, kMaxTails); };
   // (a few blocks too many would be a second wave)
-  const auto blocks = [&] { return units * (splits(tiles) + moments) + (units * a.N + tails() - 1) / tails() * splits(tiles_t); };
-  for (const long first = per; blocks() > places; ++per)
+  const auto all = [&] { return units * blocks * (splits(tiles) + moments * (g.head_dim / 64)) + (units * a.N + tails() - 1) / tails() * splits(tiles_t); };
+  for (const long first = per; all() > places; ++per)
     if (per == 2 * first) {
       per = first;
       break;
@@ -611,7 +660,7 @@ int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   a.splits = nt > 0 ? static_cast<int>(splits(tiles)) : 1;
   a.splits_t = static_cast<int>(splits(tiles_t));
   a.tails = static_cast<int>(tails());
-  a.blocks = nt > 0 ? 1 : 0;
+  a.blocks = static_cast<int>(blocks);
   a.moments = moments > 0 ? a.splits : -1;
   a.tail = a.splits + static_cast<int>(moments);
   a.parts = a.tail + a.splits_t;
@@ -632,7 +681,7 @@ cudaError_t launch_parts(const PrefixArgs& a, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const long units = (long)a.batch * a.n_kv;
-  const long blocks = units * a.blocks * (a.splits + (a.moments >= 0 ? 1 : 0)) +
+  const long blocks = units * a.blocks * (a.splits + (a.moments >= 0 ? D / 64 : 0)) +
                       (units * a.N + a.tails - 1) / a.tails * a.splits_t;
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
   return launch_pdl(prefix_parts_kernel<D, NT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), smem, stream, a,
@@ -673,21 +722,29 @@ cudaError_t launch_shared(const PrefixArgs& a, const mkv_geom& g, int num_sms, v
 
 template <int D>
 cudaError_t launch(const PrefixArgs& a, const mkv_geom& g, int nt, int num_sms, void* parts, cudaStream_t stream) {
-  cudaError_t e = nt == 2 ? launch_parts<D, 2>(a, stream) : launch_parts<D, 1>(a, stream);
+  cudaError_t e = nt == 4 ? launch_parts<D, 4>(a, stream) : nt == 2 ? launch_parts<D, 2>(a, stream) : launch_parts<D, 1>(a, stream);
   if (e == cudaSuccess && nt == 0) e = launch_shared(a, g, num_sms, parts, stream);
   if (e != cudaSuccess) return e;
-  constexpr int kPer = kJoinThreads / (D / 4);
-  return launch_pdl(prefix_join_kernel<D>, dim3((a.rows + kPer - 1) / kPer), dim3(kJoinThreads), 0, stream, a);
+  // threads of a row: one round of loads each, where the GPU holds them all at once
+  const auto run = [&](auto kernel, int P) {
+    const int per = kJoinThreads / (D / 4) / P;
+    return launch_pdl(kernel, dim3((a.rows + per - 1) / per), dim3(kJoinThreads), 0, stream, a);
+  };
+  const long all = (long)a.rows * (D / 4), most = 1024l * num_sms;
+  if (a.parts > 16 && all * 8 <= most) return run(prefix_join_kernel<D, 8>, 8);
+  if (a.parts > 8 && all * 4 <= most) return run(prefix_join_kernel<D, 4>, 4);
+  if (a.parts > 4 && all * 2 <= most) return run(prefix_join_kernel<D, 2>, 2);
+  return run(prefix_join_kernel<D, 1>, 1);
 }
 
 }  // namespace
 
 // Bytes of the parts: of every query row one of the shared rows, the moment
-// term's and one of its tail, and as many more as there are places (up to 16 rows of a
-// unit, or 8 of a tail); more than any smaller call needs.
+// term's and one of its tail, and as many more as there are places (of up to 32 rows
+// each, or 8 of a tail); more than any smaller call needs.
 size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms) {
   const long rows = (long)g.batch * g.n_kv_heads * n_seqs * g.group;
-  const long part_rows = 3 * rows + 2l * num_sms * (kTreeRows + 8);
+  const long part_rows = 3 * rows + 2l * num_sms * (kMaxCols + 8);
   const size_t tree = prefix_tree_bytes(g, n_seqs, capacity, num_sms);
   return kHeaderBytes + 256 + tree + align_up(part_rows * sizeof(float2), 256) + (size_t)part_rows * g.head_dim * 4;
 }
