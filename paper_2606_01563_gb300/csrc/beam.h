@@ -56,6 +56,8 @@ struct PrefixArgs {
   int32_t tail;      // the tails' first part
   int32_t splits_t;  // parts of a tail
   int32_t tails;     // tails of a block
+  int32_t g_shift;   // log2 of the group
+  int32_t shared_last;  // the shared rows' blocks come last
   int32_t parts;
 };
 size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms);

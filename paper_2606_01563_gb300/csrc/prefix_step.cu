@@ -45,7 +45,7 @@ constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
 constexpr int kMaxTails = 8;   // tails of a block
 constexpr long kVisits = 100000;
-constexpr float kSlack = 8.f;  // log2 headroom of a reference (weights at most 2^8)
+constexpr float kSlack = 32.f;  // log2 headroom of a reference above the score that set it (weights at most 1)
 constexpr float kNegInf = -INFINITY;
 constexpr int kJoinThreads = 256;
 
@@ -62,9 +62,8 @@ __host__ __device__ constexpr int parts_smem(int D, int NT) { return stages(D) *
 static_assert(2 * (parts_smem(128, 4) + 3072) <= 228 * 1024, "two blocks to an SM");
 
 // A query row of a unit: sequence r / G, head r % G.
-__device__ __forceinline__ int64_t out_row(const PrefixArgs& a, int b, int kv, int r) {
-  const int seq = r / a.group;
-  return ((int64_t)(b * a.N + seq) * a.n_kv + kv) * a.group + (r - seq * a.group);
+__device__ __forceinline__ int out_row(const PrefixArgs& a, int b, int kv, int r) {
+  return (((b * a.N + (r >> a.g_shift)) * a.n_kv + kv) << a.g_shift) + (r & (a.group - 1));
 }
 __device__ __forceinline__ int live_seqs(const PrefixArgs& a, int b) {
   return a.count != nullptr ? min(max(a.count[b], 0), a.N) : a.N;
@@ -114,6 +113,13 @@ __device__ __forceinline__ void load_run(const PrefixArgs& a, const CUtensorMap*
   }
 }
 
+// s += two bf16 values, each in one instruction without widening it first.
+__device__ __forceinline__ void add_rounded(float (&s)[2], uint32_t w) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}"
+      : "+f"(s[0]), "+f"(s[1])
+      : "r"(w));
+}
+
 // Columns nt (and nt + 1, with four registers) of rows of q or of the weights as B
 // operands: 8 columns x 16 values of their rows.
 __device__ __forceinline__ void ldsm_b2(uint32_t& r0, uint32_t& r1, const uint8_t* p) {
@@ -129,10 +135,13 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int tiles = (n + kRows - 1) / kRows, r0 = warp * 16;
   const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e;
-  float m[NT][2], l[NT][2], lr[NT][2], o[NT][MW][4];
+  // A column's reference, before scaling: kSlack above the score that set it.
+  const float slack = kSlack / qscale;
+  auto reference = [&](float x) { return x == kNegInf ? 0.f : x * qscale; };
+  float most[NT][2], l[NT][2], lr[NT][2], o[NT][MW][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    m[nt][0] = m[nt][1] = kNegInf;
+    most[nt][0] = most[nt][1] = kNegInf;
     l[nt][0] = l[nt][1] = lr[nt][0] = lr[nt][1] = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MW; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
@@ -194,24 +203,22 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
       }
     }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[nt][i] *= qscale;
-      moves |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
-    }
+    for (int nt = 0; nt < NT; ++nt)
+      moves |= fmaxf(s[nt][0], s[nt][2]) > most[nt][0] || fmaxf(s[nt][1], s[nt][3]) > most[nt][1];
     // the weights, and what they add to the sums (taken once the references are known to hold)
     float dl[NT][2], dr[NT][2];
     auto weigh = [&]() {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float ma = m[nt][0] == kNegInf ? 0.f : m[nt][0], mb = m[nt][1] == kNegInf ? 0.f : m[nt][1];
-        const float x0 = fast_exp2(s[nt][0] - ma), x1 = fast_exp2(s[nt][1] - mb);
-        const float x2 = fast_exp2(s[nt][2] - ma), x3 = fast_exp2(s[nt][3] - mb);
+        const float ma = reference(most[nt][0]), mb = reference(most[nt][1]);
+        const float x0 = fast_exp2(fmaf(s[nt][0], qscale, -ma)), x1 = fast_exp2(fmaf(s[nt][1], qscale, -mb));
+        const float x2 = fast_exp2(fmaf(s[nt][2], qscale, -ma)), x3 = fast_exp2(fmaf(s[nt][3], qscale, -mb));
         const uint32_t h0 = pack_bf16x2(x0, x1), h1 = pack_bf16x2(x2, x3);
         dl[nt][0] = x0 + x2;
         dl[nt][1] = x1 + x3;
-        dr[nt][0] = __uint_as_float(h0 << 16) + __uint_as_float(h1 << 16);
-        dr[nt][1] = __uint_as_float(h0 & 0xffff0000u) + __uint_as_float(h1 & 0xffff0000u);
+        dr[nt][0] = dr[nt][1] = 0.f;
+        add_rounded(dr[nt], h0);
+        add_rounded(dr[nt], h1);
         uint8_t* p = sP + (nt * 8 + g) * kPPitch + (r0 + 2 * t) * 2;  // [column][key]
         *reinterpret_cast<uint32_t*>(p) = movmatrix_t(h0);
         *reinterpret_cast<uint32_t*>(p + 16) = movmatrix_t(h1);
@@ -240,9 +247,10 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int c = nt * 8 + 2 * t + j;
-          const float mn = fmaxf(fmaxf(m[nt][j], fmaxf(sh.top[0][c], sh.top[1][c])), fmaxf(sh.top[2][c], sh.top[3][c]));
-          const float f = mn == kNegInf ? 1.f : fast_exp2(m[nt][j] - mn);
-          m[nt][j] = mn;
+          const float mn = fmaxf(fmaxf(sh.top[0][c], sh.top[1][c]), fmaxf(sh.top[2][c], sh.top[3][c])) + slack;
+          if (!(mn > most[nt][j])) continue;  // (this column's stays)
+          const float f = fast_exp2((most[nt][j] - mn) * qscale);
+          most[nt][j] = mn;
           l[nt][j] *= f, lr[nt][j] *= f;
 #pragma unroll
           for (int mt = 0; mt < MW; ++mt) o[nt][mt][j] *= f, o[nt][mt][j + 2] *= f;
@@ -303,7 +311,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) L += sh.l[w][c][0], LR += sh.l[w][c][1];
       const size_t at = (size_t)part * a.rows + row_of(c);
-      if (warp == 0 && g == 0) a.ml[at] = make_float2(m[nt][j], L);
+      if (warp == 0 && g == 0) a.ml[at] = make_float2(reference(most[nt][j]), L);
       if (L == 0.f) continue;
       const float even = LR != 0.f ? L / LR : 1.f;
       float* dst = a.o + at * D + warp * (D / 4) + g;
@@ -403,11 +411,11 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
 template <int D>
 __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int first, int wide, uint8_t* sm) {
   for (int i = threadIdx.x; i < wide * (D / 8); i += kWarps * 32) {
-    const int c = i / (D / 8), k = i % (D / 8), r = first + c, seq = r / a.group;
+    const int c = i / (D / 8), k = i % (D / 8), r = first + c, seq = r >> a.g_shift;
     uint4 w = make_uint4(0u, 0u, 0u, 0u);
     if (seq < a.N)
       w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + seq * a.q_seq +
-                                          (kv * a.group + r - seq * a.group) * D + k * 8);
+                                          ((kv << a.g_shift) + (r & (a.group - 1))) * D + k * 8);
     *reinterpret_cast<uint4*>(sm + c * q_pitch(D) + k * 16) = w;
   }
 }
@@ -432,12 +440,17 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   if (tid == 0) sh.fail = sh.moved[0] = sh.moved[1] = 0;
   mbar_fence_init();
-  // what this block's work is
+  // what this block's work is: in one wave the short ones' loads go first, in several the long runs
   const int units = a.batch * a.n_kv, shared_blocks = units * a.blocks * a.splits;
   const int moment_blocks = a.moments >= 0 ? units * a.blocks * (D / 64) : 0;
   int x = blockIdx.x, kind = 0;
+  if (a.shared_last) x = x < static_cast<int>(gridDim.x) - shared_blocks ? x + shared_blocks : x - (gridDim.x - shared_blocks);
   if (x >= shared_blocks) x -= shared_blocks, kind = 1;
   if (kind == 1 && x >= moment_blocks) x -= moment_blocks, kind = 2;
+  const int each = kind == 0 ? a.splits : kind == 1 ? D / 64 : a.splits_t;  // blocks of an item: its runs, or the moment term's pieces
+  const int item = x / each, split = x - item * each;
+  const int u = kind == 2 ? item * a.tails : a.blocks > 1 ? item / a.blocks : item;
+  const int b = kind == 2 ? 0 : u / a.n_kv, kv = u - b * a.n_kv, first = kind == 2 ? 0 : (item - u * a.blocks) * 8 * NT;
   __syncthreads();
   grid_dependency_wait();
   grid_launch_dependents();
@@ -449,9 +462,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     return max(0, min(len, t1 * kRows) - t0 * kRows);
   };
   if (kind < 2) {
-    const int each = kind == 0 ? a.splits : D / 64;  // blocks of an item: its runs, or the pieces of its moment term
-    const int item = x / each, split = x - item * each;
-    const int u = item / a.blocks, b = u / a.n_kv, kv = u - b * a.n_kv, first = (item - u * a.blocks) * 8 * NT;
     const int counted = a.count != nullptr ? a.count[b] : a.N, have = kind == 0 ? a.len[u] : a.n[u];
     if (!loads) stage_q<D>(a, b, kv, first, 8 * NT, sm);
     const int count = min(max(counted, 0), a.N), cols = min(8 * NT, count * a.group - first);
@@ -476,8 +486,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     }
   } else {
-    const int item = x / a.splits_t, split = x - item * a.splits_t;
-    const int u0 = item * a.tails, mine = min(a.tails, units * a.N - u0);
+    const int u0 = u, mine = min(a.tails, units * a.N - u0);
     // the tails' lengths, a lane each (0 of a sequence that is not in use)
     int len_all = 0, live_all = 0;
     if (lane < mine) {
@@ -555,7 +564,7 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const __grid_
   const int64_t row = (int64_t)blockIdx.x * kPer + at_row;
   const int d0 = lane * 4;
   const bool in = row < a.rows;
-  const int h = static_cast<int>(row % a.group), ut = static_cast<int>(row / a.group);  // head, tail unit
+  const int h = static_cast<int>(row) & (a.group - 1), ut = static_cast<int>(row >> a.g_shift);  // head, tail unit
   const int kv = ut % a.n_kv, pair = ut / a.n_kv, b = pair / a.N, seq = pair - b * a.N;
   grid_dependency_wait();
   grid_launch_dependents();
@@ -646,25 +655,33 @@ int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   long blocks = (rows + 8 * nt - 1) / (8 * nt);
   if (nt == 4 && units * blocks * tiles > kVisits * places) nt = 0, blocks = 0, tiles = 0;
   const long moments = nt > 0 && a.n != nullptr ? 1 : 0;
-  // runs of equal length, as many as there are places
-  long per = std::max<long>(kMinTiles, (units * blocks * tiles + units * a.N * tiles_t + places - 1) / places);
+  // Runs of equal length, as many as there are places, and no more than that
+  // where a little longer ones or several tails a block avoid it (a second wave).
+  const long least = std::max<long>(kMinTiles, (units * blocks * tiles + units * a.N * tiles_t + places - 1) / places);
+  long per = least, in_block = 1;
   const auto splits = [&](long t) { return std::min<long>(kMaxSplits, (t + per - 1) / per); };
-  const auto tails = [&] { return std::clamp<long>(per / tiles_t, 1, kMaxTails); };
-  // (a few blocks too many would be a second wave)
-  const auto all = [&] { return units * blocks * (splits(tiles) + moments * (g.head_dim / 64)) + (units * a.N + tails() - 1) / tails() * splits(tiles_t); };
-  for (const long first = per; all() > places; ++per)
-    if (per == 2 * first) {
-      per = first;
-      break;
-    }
+  const auto all = [&] {
+    return units * blocks * (splits(tiles) + moments * (g.head_dim / 64)) + (units * a.N + in_block - 1) / in_block * splits(tiles_t);
+  };
+  const auto fits = [&] {
+    for (in_block = 1; in_block <= std::clamp<long>(per / tiles_t, 1, kMaxTails); in_block *= 2)
+      if (all() <= places) return true;
+    return false;
+  };
+  bool one_wave = false;
+  for (; per <= 2 * least && !(one_wave = fits()); ++per) {
+  }
+  if (!one_wave) per = least, in_block = std::clamp<long>(per / tiles_t, 1, kMaxTails);
+  a.shared_last = one_wave ? 1 : 0;
   a.splits = nt > 0 ? static_cast<int>(splits(tiles)) : 1;
   a.splits_t = static_cast<int>(splits(tiles_t));
-  a.tails = static_cast<int>(tails());
+  a.tails = static_cast<int>(in_block);
   a.blocks = static_cast<int>(blocks);
   a.moments = moments > 0 ? a.splits : -1;
   a.tail = a.splits + static_cast<int>(moments);
   a.parts = a.tail + a.splits_t;
   a.rows = static_cast<int>(units * rows);
+  a.g_shift = g.group == 8 ? 3 : g.group == 4 ? 2 : g.group == 2 ? 1 : 0;
   return nt;
 }
 
