@@ -55,7 +55,7 @@ struct PrefixArgs {
   int32_t moments;   // the moment term's part, or -1
   int32_t tail;      // the tails' first part
   int32_t splits_t;  // parts of a tail
-  int32_t tails;     // tails of a block
+  int32_t tails;     // items (a tail, or a split of one) of a warp
   int32_t g_shift;   // log2 of the group
   int32_t shared_last;  // the shared rows' blocks come last
   int32_t parts;

@@ -27,6 +27,7 @@
 // at that barrier.  O is scaled by the ratio of the unrounded weights' sum to the
 // rounded ones', so that roundings that are common cancel.
 #include <algorithm>
+#include <cmath>
 
 #include "beam.h"
 #include "common.cuh"
@@ -43,8 +44,8 @@ constexpr int kThreads = (kWarps + 1) * 32;  // and one that loads
 constexpr int kRows = 64;                   // rows of a tile
 constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
-constexpr int kMaxTails = 8;   // tails of a block
-constexpr long kVisits = 100000;
+constexpr int kMaxTails = 8;   // tails of a warp
+constexpr long kVisits = 12;
 constexpr float kSlack = 32.f;  // log2 headroom of a reference above the score that set it (weights at most 1)
 constexpr float kNegInf = -INFINITY;
 constexpr int kJoinThreads = 256;
@@ -72,6 +73,7 @@ __device__ __forceinline__ int live_seqs(const PrefixArgs& a, int b) {
 constexpr int kMaxCols = 32;  // query rows of a block at most
 struct PartsShared {
   uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t own[kWarps][kMaxStages];  // tails: a ring a warp
   float l[kWarps][kMaxCols][2];  // of a warp and column: the weights' sum and the rounded ones'
   float top[kWarps][kMaxCols];   // a moving reference: the warps' largest scores
   float mu_k[128];
@@ -80,14 +82,16 @@ struct PartsShared {
 };
 
 __device__ __forceinline__ bool failed(const PartsShared& sh) { return *reinterpret_cast<const volatile int*>(&sh.fail) != 0; }
-// A wait on a tile; one that runs out fails the block, whose later waits then
+// A warp's wait on a tile (every lane's, and the lanes stay together: what follows
+// is the warp's as one).  One that runs out fails the block, whose later waits then
 // pass at once (barriers are met as ever; what is computed from here on is not used).
-template <int NS>
-__device__ __forceinline__ void wait_tile(PartsShared& sh, uint32_t seq, uint32_t polls) {
-  uint64_t* bar = &sh.full[seq % NS];
-  const uint32_t parity = (seq / NS) & 1;
-  if (polls > 0 && mbar_try_wait(bar, parity)) return;
-  if (!failed(sh) && !mbar_wait(bar, parity, polls)) *reinterpret_cast<volatile int*>(&sh.fail) = 1;
+__device__ __forceinline__ void wait_tile(uint64_t* bar, uint32_t parity, PartsShared& sh, uint32_t polls) {
+  for (uint32_t i = 0; i < polls; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+    if ((i & 63) == 63 && __any_sync(0xffffffffu, failed(sh))) return;
+  }
+  *reinterpret_cast<volatile int*>(&sh.fail) = 1;
+  __syncwarp();
 }
 
 // The loading warp's part of a run of n rows: one thread, tiles seq, seq + 1, ... of the block.
@@ -119,6 +123,9 @@ __device__ __forceinline__ void add_rounded(float (&s)[2], uint32_t w) {
       : "+f"(s[0]), "+f"(s[1])
       : "r"(w));
 }
+
+// Shared memory read or written by threads, next written by a bulk copy.
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Columns nt (and nt + 1, with four registers) of rows of q or of the weights as B
 // operands: 8 columns x 16 values of their rows.
@@ -156,7 +163,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
   const int kr = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
   const int vr = (lane & 7) + (lane >> 4) * 8, vc = warp * (D / 4) + ((lane >> 3) & 1) * 8;
   for (int it = 0; it < tiles; ++it, ++seq) {
-    wait_tile<NS>(sh, seq, a.polls);
+    wait_tile(&sh.full[seq % NS], (seq / NS) & 1, sh, a.polls);
     const int rows = min(kRows, n - it * kRows);
     const uint8_t* tK = ring + (size_t)(seq % NS) * 2 * kTile;
     uint8_t* tV = ring + (size_t)(seq % NS) * 2 * kTile + kTile;
@@ -226,10 +233,16 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
     };
     if (__any_sync(0xffffffffu, moves)) {
       if (lane == 0) *reinterpret_cast<volatile int*>(&sh.moved[it & 1]) = it + 1;
+      __syncwarp();
     } else {
       weigh();
     }
     named_sync(1, kWarps * 32);
+    // Past the barrier all four warps have read the tile before.  (Released by each warp
+    // after its own reads, with a barrier arrival that nothing but its order ties to them, a tile's last
+    // rows were now and then those of the copy that took its place: 3 of 100
+    // first runs of a process.)
+    if (it > 0 && tid == 0) mbar_arrive(&sh.empty[(seq - 1) % NS]);
     if (*reinterpret_cast<volatile int*>(&sh.moved[it & 1]) == it + 1) {
       // some column's reference moves: to the largest score of the four warps'
 #pragma unroll
@@ -247,9 +260,10 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int c = nt * 8 + 2 * t + j;
-          const float mn = fmaxf(fmaxf(sh.top[0][c], sh.top[1][c]), fmaxf(sh.top[2][c], sh.top[3][c])) + slack;
-          if (!(mn > most[nt][j])) continue;  // (this column's stays)
-          const float f = fast_exp2((most[nt][j] - mn) * qscale);
+          const float mx = fmaxf(fmaxf(sh.top[0][c], sh.top[1][c]), fmaxf(sh.top[2][c], sh.top[3][c]));
+          // (selects: the lanes stay together)
+          const float mn = mx > most[nt][j] ? mx + slack : most[nt][j];
+          const float f = mx > most[nt][j] ? fast_exp2((most[nt][j] - mn) * qscale) : 1.f;
           most[nt][j] = mn;
           l[nt][j] *= f, lr[nt][j] *= f;
 #pragma unroll
@@ -282,8 +296,6 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
         }
       }
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.empty[seq % NS]);
   }
   // the columns' sums over the warps, and the state
 #pragma unroll
@@ -407,6 +419,165 @@ __device__ __forceinline__ void moment_run(const PrefixArgs& a, int u, int n_e, 
     }
 }
 
+// Tails, one to a warp: its items are first, first + 4, ... below `end` (tail
+// unit, split), `mine` of them at most 32.  A warp has a ring of its own, of 16-row
+// tiles that it asks for itself, ahead over its items; the keys and then the value dims are the 16-row side,
+// the weights stay in registers, and no warp waits for another.
+template <int D>
+__device__ __forceinline__ void tail_warp(const PrefixArgs& a, const CUtensorMap* tmK, const CUtensorMap* tmV, int first,
+                                          int end, uint8_t* ring, PartsShared& sh) {
+  constexpr int KS = D / 16, MT = D / 16, NS = stages(D), kKeys = 16, kTile = kKeys * D * 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* full = sh.own[warp];
+  ring += warp * NS * 2 * kTile;
+  const int mine = end > first ? (end - first + kWarps - 1) / kWarps : 0;
+  // an item each lane: its rows, none of a sequence that is not in use
+  int n_all = -1, row_all = 0;
+  if (lane < mine) {
+    const int item = first + kWarps * lane, u = item / a.splits_t, split = item - u * a.splits_t, b = u / a.n_kv / a.N;
+    const int have = a.len_t[u];
+    if (u / a.n_kv - b * a.N < (a.count != nullptr ? a.count[b] : a.N)) {
+      const int len = min(max(have, 0), a.cap_t);
+      if (have != len && split == 0) record_error(a.ws, MKV_ERR_CAPACITY, u);
+      const int tiles = (len + kKeys - 1) / kKeys, per = (tiles + a.splits_t - 1) / a.splits_t;
+      const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
+      n_all = max(0, min(len, t1 * kKeys) - t0 * kKeys);
+      row_all = u * a.cap_t + t0 * kKeys;
+    }
+  }
+  uint32_t asked = 0, seq = 0;  // tiles asked for and used
+  int ask_item = 0, ask_row = 0;
+  const uint64_t pol = l2_evict_first();
+  auto ask = [&]() {  // the next tile of the warp's items, if there is one
+    int n = 0;
+    while (ask_item < mine && ask_row >= (n = __shfl_sync(0xffffffffu, n_all, ask_item))) ++ask_item, ask_row = 0;
+    if (ask_item == mine) return;
+    const int row = __shfl_sync(0xffffffffu, row_all, ask_item) + ask_row;
+    if (lane == 0) {
+      if (ask_row == 0 && n > kKeys) {  // the next tiles into L2 now (further ahead they would crowd it)
+        const size_t off = (size_t)(row + kKeys) * D * 2;
+        const uint32_t bytes = static_cast<uint32_t>(min(n, 6 * kKeys) - kKeys) * D * 2;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(a.Kt) + off), "r"(bytes) : "memory");
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(a.Vt) + off), "r"(bytes) : "memory");
+      }
+      uint8_t* dst = ring + (asked % NS) * 2 * kTile;
+      uint64_t* bar = &full[asked % NS];
+      mbar_arrive_expect_tx(bar, 2u * kTile);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        tma_load_2d_hint(dst + x * kKeys * 128, tmK, x * 64, row, bar, pol);
+        tma_load_2d_hint(dst + kTile + x * kKeys * 128, tmV, x * 64, row, bar, pol);
+      }
+    }
+    ++asked;
+    ask_row += kKeys;
+  };
+  auto query = [&](int i, uint32_t (&q)[KS][2]) {  // item i's query rows as the B operand
+    const int u = (first + kWarps * i) / a.splits_t, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch + (pair - b * a.N) * a.q_seq +
+                             ((kv << a.g_shift) + g) * D + 2 * t;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      q[kk][0] = i < mine && g < a.group ? *reinterpret_cast<const uint32_t*>(p + kk * 16) : 0u;
+      q[kk][1] = i < mine && g < a.group ? *reinterpret_cast<const uint32_t*>(p + kk * 16 + 8) : 0u;
+    }
+  };
+  for (int i = 0; i < NS; ++i) ask();
+  const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e, slack = kSlack / qscale;
+  uint32_t next[KS][2];
+  query(0, next);
+  for (int i = 0; i < mine; ++i) {
+    uint32_t q[KS][2];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) q[kk][0] = next[kk][0], q[kk][1] = next[kk][1];
+    if (i + 1 < mine) query(i + 1, next);
+    const int n = __shfl_sync(0xffffffffu, n_all, i);
+    if (n < 0) continue;  // (not in use: nothing is joined)
+    float most[2] = {kNegInf, kNegInf}, l[2] = {}, lr[2] = {}, o[MT][4] = {};
+    for (int r0 = 0; r0 < n; r0 += kKeys, ++seq) {
+      wait_tile(&full[seq % NS], (seq / NS) & 1, sh, a.polls);
+      const uint8_t* tK = ring + (seq % NS) * 2 * kTile;
+      uint8_t* tV = ring + (seq % NS) * 2 * kTile + kTile;
+      const int rows = min(kKeys, n - r0);
+      if (rows < kKeys) {  // V rows past the end are zeroed: their weights are 0, but they may hold anything
+        for (int x = lane; x < (kKeys - rows) * (D / 8); x += 32) {
+          const int r = rows + x / (D / 8), c = (x % (D / 8)) * 8;
+          *reinterpret_cast<uint4*>(tV + (c >> 6) * kKeys * 128 + r * 128 + (c & 63) * 2) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+      }
+      const int kr = (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
+      float c[2][4] = {};
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        uint32_t k4[4];
+        ldsm_x4(k4, tK + swz_off(kr, kk * 16 + kc, kKeys));
+        mma_m16n8k16(c[kk & 1], k4[0], k4[1], k4[2], k4[3], q[kk][0], q[kk][1]);
+      }
+      // lane (g, t): keys g (0, 1) and g + 8 (2, 3), columns 2t (0, 2) and 2t + 1 (1, 3)
+      float s[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[x] = (x < 2 ? g : g + 8) < rows ? c[0][x] + c[1][x] : kNegInf;
+      const float m0 = fmaxf(s[0], s[2]), m1 = fmaxf(s[1], s[3]);
+      if (__any_sync(0xffffffffu, m0 > most[0] || m1 > most[1])) {
+        float mx[2] = {m0, m1};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], off));
+          const float mn = mx[j] > most[j] ? mx[j] + slack : most[j];
+          const float f = mx[j] > most[j] ? fast_exp2((most[j] - mn) * qscale) : 1.f;
+          most[j] = mn;
+          l[j] *= f, lr[j] *= f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) o[mt][j] *= f, o[mt][j + 2] *= f;
+        }
+      }
+      const float ra = most[0] == kNegInf ? 0.f : most[0] * qscale, rb = most[1] == kNegInf ? 0.f : most[1] * qscale;
+      const float x0 = fast_exp2(fmaf(s[0], qscale, -ra)), x1 = fast_exp2(fmaf(s[1], qscale, -rb));
+      const float x2 = fast_exp2(fmaf(s[2], qscale, -ra)), x3 = fast_exp2(fmaf(s[3], qscale, -rb));
+      const uint32_t h0 = pack_bf16x2(x0, x1), h1 = pack_bf16x2(x2, x3);
+      l[0] += x0 + x2;
+      l[1] += x1 + x3;
+      add_rounded(lr, h0);
+      add_rounded(lr, h1);
+      const uint32_t p0 = movmatrix_t(h0), p1 = movmatrix_t(h1);
+      const int vr = (lane & 7) + (lane >> 4) * 8, vc = ((lane >> 3) & 1) * 8;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        uint32_t v4[4];
+        ldsm_x4_t(v4, tV + swz_off(vr, mt * 16 + vc, kKeys));
+        mma_m16n8k16(o[mt], v4[0], v4[1], v4[2], v4[3], p0, p1);
+      }
+      fence_proxy_async();  // every lane has read the tile (and written its zeros) before a copy takes its place
+      __syncwarp();
+      ask();
+    }
+    const int u = (first + kWarps * i) / a.splits_t, split = first + kWarps * i - u * a.splits_t;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) {
+        l[j] += __shfl_xor_sync(0xffffffffu, l[j], off);
+        lr[j] += __shfl_xor_sync(0xffffffffu, lr[j], off);
+      }
+      if (2 * t + j >= a.group) continue;
+      const size_t at = (size_t)(a.tail + split) * a.rows + ((size_t)u << a.g_shift) + 2 * t + j;
+      if (g == 0) a.ml[at] = make_float2(most[j] == kNegInf ? 0.f : most[j] * qscale, l[j]);
+      const float even = lr[j] != 0.f ? l[j] / lr[j] : 1.f;
+      if (l[j] != 0.f)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          a.o[at * D + mt * 16 + g] = o[mt][j] * even;
+          a.o[at * D + mt * 16 + g + 8] = o[mt][j + 2] * even;
+        }
+    }
+  }
+  // after a wait that gave up: the copies in flight land before the block ends
+  if (failed(sh) && lane == 0)
+    for (uint32_t j = asked > NS ? asked - NS : 0; j < asked; ++j) (void)mbar_wait(&full[j % NS], (j / NS) & 1);
+}
+
 // Query rows of unit (b, kv) from row `first` on into shared memory, `wide` of them, zeros where there is none.
 template <int D>
 __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int first, int wide, uint8_t* sm) {
@@ -421,7 +592,7 @@ __device__ __forceinline__ void stage_q(const PrefixArgs& a, int b, int kv, int 
 }
 
 // Blocks: the shared rows' runs (unit, column block, split) and the moment terms
-// (unit, column block), where they are this launch's, and the tails (a run of one, or several short ones).
+// (unit, column block, piece), where they are this launch's, and the tails.
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, 2)
     prefix_parts_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ CUtensorMap tmK,
@@ -436,7 +607,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   const bool loads = tid >= kWarps * 32;
   if (tid < NS) {
     mbar_init(&sh.full[tid], 1);
-    mbar_init(&sh.empty[tid], kWarps);
+    mbar_init(&sh.empty[tid], 1);
+    for (int w = 0; w < kWarps; ++w) mbar_init(&sh.own[w][tid], 1);
   }
   if (tid == 0) sh.fail = sh.moved[0] = sh.moved[1] = 0;
   mbar_fence_init();
@@ -447,9 +619,9 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (a.shared_last) x = x < static_cast<int>(gridDim.x) - shared_blocks ? x + shared_blocks : x - (gridDim.x - shared_blocks);
   if (x >= shared_blocks) x -= shared_blocks, kind = 1;
   if (kind == 1 && x >= moment_blocks) x -= moment_blocks, kind = 2;
-  const int each = kind == 0 ? a.splits : kind == 1 ? D / 64 : a.splits_t;  // blocks of an item: its runs, or the moment term's pieces
+  const int each = kind == 0 ? a.splits : kind == 1 ? D / 64 : 1;  // blocks of an item: its runs, or the moment term's pieces
   const int item = x / each, split = x - item * each;
-  const int u = kind == 2 ? item * a.tails : a.blocks > 1 ? item / a.blocks : item;
+  const int u = kind == 2 ? 0 : a.blocks > 1 ? item / a.blocks : item;
   const int b = kind == 2 ? 0 : u / a.n_kv, kv = u - b * a.n_kv, first = kind == 2 ? 0 : (item - u * a.blocks) * 8 * NT;
   __syncthreads();
   grid_dependency_wait();
@@ -475,6 +647,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (kind == 0) n = run_of(len, a.splits, split, row);
       if (loads) {
         if (lane == 0 && kind == 0) load_run<D, NS>(a, &tmK, &tmV, u * a.cap + row, n, ring, sh, seq);
+        __syncwarp();
       } else {
         auto row_of = [&](int c) { return out_row(a, b, kv, first + c); };
         if (kind == 0) {
@@ -485,52 +658,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
       }
     }
-  } else {
-    const int u0 = u, mine = min(a.tails, units * a.N - u0);
-    // the tails' lengths, a lane each (0 of a sequence that is not in use)
-    int len_all = 0, live_all = 0;
-    if (lane < mine) {
-      const int u = u0 + lane, b = u / a.n_kv / a.N, have = a.len_t[u];
-      live_all = u / a.n_kv - b * a.N < (a.count != nullptr ? a.count[b] : a.N);
-      len_all = live_all ? min(max(have, 0), a.cap_t) : 0;
-      if (live_all && have != len_all && split == 0 && loads) record_error(a.ws, MKV_ERR_CAPACITY, u);
-    }
-    // a tail's query rows: 16 bytes a thread, the next tail's on their way while one is worked on
-    auto query = [&](int i) {
-      const int u = u0 + i, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
-      const int c = tid / (D / 8), k = tid % (D / 8);
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      if (i < mine && c < a.group)
-        w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.q_batch +
-                                            (pair - b * a.N) * a.q_seq + (kv * a.group + c) * D + k * 8);
-      return w;
-    };
-    uint4 next = make_uint4(0u, 0u, 0u, 0u);
-    if (!loads) next = query(0);
-    for (int i = 0; i < mine; ++i) {
-      const int u = u0 + i, pair = u / a.n_kv, kv = u - pair * a.n_kv, b = pair / a.N;
-      int row;
-      const int n = run_of(__shfl_sync(0xffffffffu, len_all, i), a.splits_t, split, row);
-      const bool live = __shfl_sync(0xffffffffu, live_all, i) != 0;
-      if (loads) {
-        if (lane == 0 && live) load_run<D, NS>(a, &tmKt, &tmVt, u * a.cap_t + row, n, ring, sh, seq);
-        __syncwarp();
-        continue;
-      }
-      const uint4 w = next;
-      next = query(i + 1);
-      if (!live) continue;
-      const int first = (pair - b * a.N) * a.group;
-      if (n == 0) {  // (nothing but the new token yet)
-        if (tid < a.group) a.ml[(size_t)(a.tail + split) * a.rows + out_row(a, b, kv, first + tid)] = make_float2(kNegInf, 0.f);
-        continue;
-      }
-      named_sync(1, kWarps * 32);  // (every warp is past the tail before)
-      if (tid < D) *reinterpret_cast<uint4*>(sm + tid / (D / 8) * q_pitch(D) + tid % (D / 8) * 16) = w;
-      if (tid < 2) sh.moved[tid] = 0;
-      named_sync(1, kWarps * 32);
-      attend_run<D, 1, NS>(a, n, a.group, a.tail + split, ring, sm, sh, seq, [&](int c) { return out_row(a, b, kv, first + c); });
-    }
+  } else if (!loads) {
+    const int from = x * kWarps * a.tails, all = units * a.N * a.splits_t;
+    tail_warp<D>(a, &tmKt, &tmVt, from + (tid >> 5), min(all, from + kWarps * a.tails), ring, sh);
   }
   __syncthreads();
   if (failed(sh) && loads && lane == 0) {
@@ -653,29 +783,36 @@ int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   const long tiles_t = ((long)a.cap_t + kRows - 1) / kRows;
   int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   long blocks = (rows + 8 * nt - 1) / (8 * nt);
-  if (nt == 4 && units * blocks * tiles > kVisits * places) nt = 0, blocks = 0, tiles = 0;
+  if (blocks > 1 && units * blocks * tiles * g.head_dim > kVisits * 128 * places) nt = 0, blocks = 0, tiles = 0;
   const long moments = nt > 0 && a.n != nullptr ? 1 : 0;
-  // Runs of equal length, as many as there are places, and no more than that
-  // where a little longer ones or several tails a block avoid it (a second wave).
-  const long least = std::max<long>(kMinTiles, (units * blocks * tiles + units * a.N * tiles_t + places - 1) / places);
-  long per = least, in_block = 1;
-  const auto splits = [&](long t) { return std::min<long>(kMaxSplits, (t + per - 1) / per); };
-  const auto all = [&] {
-    return units * blocks * (splits(tiles) + moments * (g.head_dim / 64)) + (units * a.N + in_block - 1) / in_block * splits(tiles_t);
-  };
-  const auto fits = [&] {
-    for (in_block = 1; in_block <= std::clamp<long>(per / tiles_t, 1, kMaxTails); in_block *= 2)
-      if (all() <= places) return true;
-    return false;
-  };
-  bool one_wave = false;
-  for (; per <= 2 * least && !(one_wave = fits()); ++per) {
+  // Tails are a warp's; long ones are split, so that their items are more than the places (13 x 8
+  // tails of up to 300 rows: 208 blocks on 152 SMs took 25 us, two or three times as many 15).
+  const long items = units * a.N;
+  const long splits_t = std::clamp<long>((5 * kWarps * places / 2 + items - 1) / items, 1, std::min<long>(kMaxSplits, (tiles_t + 1) / 2));
+  const long item_tiles = (tiles_t + splits_t - 1) / splits_t;
+  // Splits of the shared rows and tails of a warp: the least of an estimate (in
+  // us, from clock stamps of blocks): the longest block, or all blocks over the
+  // places and half of the longest for the last wave's end, and the join's traffic.
+  const float tile = (nt == 4 ? 1.1f : 0.85f) * g.head_dim / 128;
+  float best = INFINITY;
+  long best_splits = 1, in_warp = 1;
+  for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
+    // (and no more parts than the workspace was sized for)
+    if (s > 1 && (s * kMinTiles > tiles + kMinTiles - 1 || units * blocks * (s - 1) > places)) break;
+    for (int w = 1; w <= kMaxTails; w *= 2) {
+      const float run = nt > 0 ? 3.f + tile * ((tiles + s - 1) / s) : 0.f, tail = 2.f + w * (0.8f + 2.f * item_tiles);
+      const long runs = units * blocks * s, terms = units * blocks * moments * (g.head_dim / 64);
+      const long tails = (items * splits_t + kWarps * w - 1) / (kWarps * w);
+      const float longest = std::max(run, tail), all = (runs * run + terms * 3.f + tails * tail) / places;
+      const float us = (runs + terms + tails <= places ? longest : std::max(longest, all + 0.5f * longest)) +
+                       units * rows * (s + moments + splits_t) * g.head_dim * 1e-6f;
+      if (us < best) best = us, best_splits = s, in_warp = w, a.shared_last = runs + terms + tails <= places;
+    }
+    if (nt == 0) break;
   }
-  if (!one_wave) per = least, in_block = std::clamp<long>(per / tiles_t, 1, kMaxTails);
-  a.shared_last = one_wave ? 1 : 0;
-  a.splits = nt > 0 ? static_cast<int>(splits(tiles)) : 1;
-  a.splits_t = static_cast<int>(splits(tiles_t));
-  a.tails = static_cast<int>(in_block);
+  a.splits = static_cast<int>(best_splits);
+  a.splits_t = static_cast<int>(splits_t);
+  a.tails = static_cast<int>(in_warp);
   a.blocks = static_cast<int>(blocks);
   a.moments = moments > 0 ? a.splits : -1;
   a.tail = a.splits + static_cast<int>(moments);
@@ -691,15 +828,15 @@ cudaError_t launch_parts(const PrefixArgs& a, cudaStream_t stream) {
   const uint64_t rows = (uint64_t)a.batch * a.n_kv * a.cap, rows_t = (uint64_t)a.batch * a.N * a.n_kv * a.cap_t;
   if (!encode_tmap_bf16(&tm[0], a.K, D, rows, (uint64_t)D * 2, 64, kRows) ||
       !encode_tmap_bf16(&tm[1], a.V, D, rows, (uint64_t)D * 2, 64, kRows) ||
-      !encode_tmap_bf16(&tm[2], a.Kt, D, rows_t, (uint64_t)D * 2, 64, kRows) ||
-      !encode_tmap_bf16(&tm[3], a.Vt, D, rows_t, (uint64_t)D * 2, 64, kRows))
+      !encode_tmap_bf16(&tm[2], a.Kt, D, rows_t, (uint64_t)D * 2, 64, 16) ||
+      !encode_tmap_bf16(&tm[3], a.Vt, D, rows_t, (uint64_t)D * 2, 64, 16))
     return cudaErrorInvalidValue;
   constexpr int smem = parts_smem(D, NT);
   cudaError_t e = cudaFuncSetAttribute(prefix_parts_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const long units = (long)a.batch * a.n_kv;
   const long blocks = units * a.blocks * (a.splits + (a.moments >= 0 ? D / 64 : 0)) +
-                      (units * a.N + a.tails - 1) / a.tails * a.splits_t;
+                      (units * a.N * a.splits_t + kWarps * a.tails - 1) / (kWarps * a.tails);
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
   return launch_pdl(prefix_parts_kernel<D, NT>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), smem, stream, a,
                     tm[0], tm[1], tm[2], tm[3]);
@@ -757,11 +894,11 @@ cudaError_t launch(const PrefixArgs& a, const mkv_geom& g, int nt, int num_sms, 
 }  // namespace
 
 // Bytes of the parts: of every query row one of the shared rows, the moment
-// term's and one of its tail, and as many more as there are places (of up to 32 rows
-// each, or 8 of a tail); more than any smaller call needs.
+// term's and one of its tail, as many more as there are places (of up to 32 rows
+// each), and a warp of every place for a tail's (8 rows each); more than any smaller call needs.
 size_t prefix_workspace_bytes(const mkv_geom& g, int32_t n_seqs, int32_t capacity, int num_sms) {
   const long rows = (long)g.batch * g.n_kv_heads * n_seqs * g.group;
-  const long part_rows = 3 * rows + 2l * num_sms * (kMaxCols + 8);
+  const long part_rows = 3 * rows + 2l * num_sms * (kMaxCols + 5 * kWarps / 2 * 8);
   const size_t tree = prefix_tree_bytes(g, n_seqs, capacity, num_sms);
   return kHeaderBytes + 256 + tree + align_up(part_rows * sizeof(float2), 256) + (size_t)part_rows * g.head_dim * 4;
 }
