@@ -116,7 +116,7 @@ MKV_API size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int3
  * The n_out best continuations of every batch item, best first.  A live beam
  * that has not ended continues with token t at score[beam] + logit[t] -
  * log sum exp(logits of the beam); one that has ended continues only with
- * end_token, at its own score (its logits are not read).  Equal ones: the lower beam, then the lower token.
+ * end_token, at its own score (its logits do not matter).  Equal ones: the lower beam, then the lower token.
  *   parent     int32 [batch, n_out]  the beam that is continued
  *   token      int32 [batch, n_out]  by which token
  *   score_out  fp32  [batch, n_out]

@@ -14,17 +14,17 @@
 // lists by score.
 //
 // The best of a run.  A logit and its token make one 64-bit key, so no two are
-// equal.  Of the groups of a few threads each, the n_out-th largest of the groups'
-// best keys is a bound with at least n_out keys at or above it, and only keys of n_out groups
+// equal.  The n_out-th largest of the threads' best keys of a chunk is a bound
+// with at least n_out keys at or above it, and only keys of n_out threads
 // at most reach it: they fit a buffer whatever the logits are.  Once a list
 // is full its last key is the bound for what follows, which nearly nothing
 // passes.
 //
-// Rounding.  Terms are fp32 about a reference that is a whole number at or
+// Rounding.  Terms and sums are fp32 about a reference that is a whole number at or
 // above the largest logit (a term of weight has a small exponent, and sums about different references
-// join by factors that depend on whole numbers alone), sums of a thread fp32,
-// the joined sum, its log and the scores fp64: which of two continuations is
-// better is decided to about 1e-7, and the scores that come back are rounded once.
+// join by factors that depend on whole numbers alone), the log of the joined sum
+// and the scores fp64: which of two continuations is better is decided to a few
+// 1e-7, and the scores that come back are rounded once.
 //
 // Bounded by HBM over many beams: each logit is read once.
 #include <algorithm>
@@ -38,12 +38,14 @@ namespace mkv {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;  // of a run's block
+constexpr int kJoinThreads = 512;
 constexpr int kVec = 16;                   // elements of a thread and chunk
 constexpr int kChunk = kThreads * kVec;    // elements of a chunk
 constexpr int kMaxOut = MKV_BEAM_MAX_OUT;  // 64
-constexpr int kBuffer = 2048 + 2 * kMaxOut;
+constexpr int kBuffer = kMaxOut * kVec + 2 * kMaxOut;
 constexpr int kMaxLists = 128;  // of a batch item
+constexpr int64_t kBlocks = 8;
 constexpr float kNegInf = -INFINITY;
 
 // Order-preserving key of a logit and the token that has it: larger is better,
@@ -57,14 +59,10 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 __device__ __forceinline__ uint32_t key_token(uint64_t k) { return ~static_cast<uint32_t>(k); }
 
-__device__ __forceinline__ uint64_t shfl_max(uint64_t k, int o) {
-  const uint64_t other = __shfl_xor_sync(0xffffffffu, k, o);
-  return other > k ? other : k;
-}
-
 struct RowShared {
   uint64_t keys[kBuffer];
-  uint64_t groups[256];
+  uint64_t best[kMaxOut];
+  uint64_t tops[kThreads];
   uint64_t bound;  // the least key that is still wanted
   int fill;
   float ref[kWarps];
@@ -75,25 +73,20 @@ struct RowShared {
 __device__ __forceinline__ void keep_best(RowShared& sh, int out) {
   __syncthreads();
   const int n = sh.fill;
-  uint64_t mine[(kBuffer + kThreads - 1) / kThreads];
-  int rank[(kBuffer + kThreads - 1) / kThreads];
+  // the ranks' keys by way of a second place (a rank below `out` is one thread's)
 #pragma unroll 1
-  for (int j = 0; j * kThreads < n; ++j) {
-    const int i = j * kThreads + threadIdx.x;
-    uint64_t k = i < n ? sh.keys[i] : 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t k = sh.keys[i];
     int r = 0;
-    if (i < n)
-#pragma unroll 4
-      for (int m = 0; m < n; ++m) r += sh.keys[m] > k;
-    mine[j] = k, rank[j] = i < n ? r : kBuffer;
+#pragma unroll 8
+    for (int m = 0; m < n; ++m) r += sh.keys[m] > k;
+    if (r < out) {
+      sh.best[r] = k;
+      if (r == out - 1) sh.bound = k + 1;
+    }
   }
   __syncthreads();
-#pragma unroll 1
-  for (int j = 0; j * kThreads < n; ++j)
-    if (rank[j] < out) {
-      sh.keys[rank[j]] = mine[j];
-      if (rank[j] == out - 1) sh.bound = mine[j] + 1;
-    }
+  if (threadIdx.x < min(n, out)) sh.keys[threadIdx.x] = sh.best[threadIdx.x];
   if (threadIdx.x == 0) sh.fill = min(n, out);
   __syncthreads();
 }
@@ -107,37 +100,82 @@ __device__ __forceinline__ int element_of(int i) {
   return ((i / V) * kThreads + threadIdx.x) * V + i % V;
 }
 
-// A thread's elements of the chunk that starts at element `first` of the row; from `end` on they are
-// -infinity and not read.
+// A thread's elements of the chunk that starts at element `first` of the row, as
+// they lie in memory (a chunk ahead); from `end` on they are -infinity and not read.
 template <bool F32, bool Vec>
-__device__ __forceinline__ void load_chunk(const void* row, int first, int end, float (&x)[kVec]) {
-  constexpr int V = !Vec ? 1 : F32 ? 4 : 8;
+struct Chunk {
+  uint32_t w[F32 ? kVec : kVec / 2];
+  __device__ __forceinline__ void load(const void* row, int first, int end) {
+    constexpr int V = F32 ? 4 : 8;
+    constexpr uint32_t kNone = F32 ? 0xff800000u : 0xff80u;  // -infinity
+    if constexpr (Vec) {
 #pragma unroll
-  for (int j = 0; j < kVec / V; ++j) {
-    const int v = first + element_of<F32, Vec>(j * V);
-    if (Vec && v + V <= end) {
-      const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(row) + (size_t)v * (F32 ? 4 : 2)));
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+      for (int j = 0; j < kVec / V; ++j) {
+        const int v = first + element_of<F32, Vec>(j * V);
+        if (v + V <= end) {
+          const uint4 x = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(row) + (size_t)v * (F32 ? 4 : 2)));
+          w[4 * j] = x.x, w[4 * j + 1] = x.y, w[4 * j + 2] = x.z, w[4 * j + 3] = x.w;
+        } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (F32) {
-          x[j * V + (Vec ? i : 0)] = __uint_as_float(u[i]);
-        } else if constexpr (Vec) {
-          x[j * V + 2 * i] = __uint_as_float(u[i] << 16);
-          x[j * V + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (F32) {
+              w[4 * j + i] = v + i < end ? static_cast<const uint32_t*>(row)[v + i] : kNone;
+            } else {
+              const int e = v + 2 * i;
+              const uint32_t lo = e < end ? static_cast<const uint16_t*>(row)[e] : kNone;
+              w[4 * j + i] = lo | (e + 1 < end ? static_cast<const uint16_t*>(row)[e + 1] : kNone) << 16;
+            }
+          }
         }
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (F32)
-          x[j * V + i] = v + i < end ? __ldcs(static_cast<const float*>(row) + v + i) : kNegInf;
-        else
-          x[j * V + i] = v + i < end ? __uint_as_float(static_cast<uint32_t>(__ldcs(static_cast<const uint16_t*>(row) + v + i)) << 16)
-                                     : kNegInf;
+      for (int i = 0; i < kVec; ++i) {
+        const int v = first + element_of<F32, Vec>(i);
+        if constexpr (F32) {
+          w[i] = v < end ? __ldcs(static_cast<const uint32_t*>(row) + v) : kNone;
+        } else {
+          const uint32_t x = v < end ? __ldcs(static_cast<const uint16_t*>(row) + v) : kNone;
+          w[i / 2] = i % 2 == 0 ? x : w[i / 2] | x << 16;
+        }
       }
     }
   }
+  __device__ __forceinline__ void floats(float (&x)[kVec]) const {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      if constexpr (F32)
+        x[i] = __uint_as_float(w[i]);
+      else
+        x[i] = __uint_as_float(i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xffff0000u);
+    }
+  }
+};
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+static_assert(kVec == 16, "four fours");
+// Two floats in one 64-bit register, and two operations per instruction.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t x, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 template <bool F32, bool Vec>
@@ -146,6 +184,11 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
   grid_dependency_wait();
   grid_launch_dependents();
   const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits, tid = threadIdx.x, lane = tid & 31;
+  const int item = row / a.beams, lo = split * a.per, end = min(lo + a.per, a.vocab);
+  const uint8_t* base = static_cast<const uint8_t*>(a.logits) +
+                        (item * a.s_batch + (row - item * a.beams) * a.s_beam) * (F32 ? 4 : 2);
+  Chunk<F32, Vec> next;  // on its way while the beam's state is read
+  next.load(base, lo, end);
   const float score = a.score[row];
   float4* stat = a.stats + (size_t)row * a.splits + split;
   if (split == 0 && tid == 0 && !(score < INFINITY)) record_error(a.ws, MKV_ERR_INVALID_ARG, row);
@@ -153,32 +196,36 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
     if (tid == 0) *stat = make_float4(kNegInf, 0.f, __int_as_float(0), 0.f);
     return;
   }
-  const int item = row / a.beams;
-  const uint8_t* base = static_cast<const uint8_t*>(a.logits) +
-                        (item * a.s_batch + (row - item * a.beams) * a.s_beam) * (F32 ? 4 : 2);
-  const int lo = split * a.per, end = min(lo + a.per, a.vocab);
   if (tid == 0) sh.fill = 0, sh.bound = 1;
   float ref = kNegInf, sum = 0.f;
-  bool odd = false;
-  const int span = a.out <= 32 ? 4 : 2, groups = kThreads / span;  // threads of a group
   __syncthreads();
   for (int first = lo; first < end; first += kChunk) {
     float x[kVec];
-    load_chunk<F32, Vec>(base, first, end, x);
-    float top = kNegInf;
+    next.floats(x);
+    if (first + kChunk < end) next.load(base, first + kChunk, end);
+    float tops[kVec / 4];  // of four elements each
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      top = fmaxf(top, x[i]);
-      odd |= !(x[i] < INFINITY);
+    for (int i = 0; i < kVec / 4; ++i) tops[i] = fmaxf(max3(x[4 * i], x[4 * i + 1], x[4 * i + 2]), x[4 * i + 3]);
+    const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
+    if (top > ref) {
+      const float r = ceilf(top);
+      sum = ref == kNegInf ? 0.f : sum * expf(ref - r);
+      ref = r;
     }
-    if (top > kNegInf && !odd) {
-      if (top > ref) {
-        const float r = ceilf(top);
-        sum = ref == kNegInf ? 0.f : sum * expf(ref - r);
-        ref = r;
-      }
+    {
+      // (about a reference of 0 where there is nothing yet; a NaN or +infinity makes the sum one)
+      const float r = ref == kNegInf ? 0.f : ref;
+      const uint64_t nref = pack2(-r, -r), scale = pack2(kLog2e, kLog2e);
+      uint64_t sums = 0;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += fast_exp2((x[i] - ref) * kLog2e);
+      for (int i = 0; i < kVec; i += 2) {
+        float t0, t1;
+        unpack2(mul2(add2(pack2(x[i], x[i + 1]), nref), scale), t0, t1);
+        sums = add2(sums, pack2(fast_exp2(t0), fast_exp2(t1)));
+      }
+      float s0, s1;
+      unpack2(sums, s0, s1);
+      sum += s0 + s1;
     }
     // what is still wanted of the chunk
     uint64_t bound = sh.bound;
@@ -194,32 +241,34 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
         const uint64_t k = make_key(x[i], first + element_of<F32, Vec>(i));
         best = k > best ? k : best;
       }
-      for (int o = 1; o < span; o <<= 1) best = shfl_max(best, o);
-      if (tid % span == 0) sh.groups[tid / span] = best;
+      sh.tops[tid] = best;
       __syncthreads();
-      if (tid < groups) {
-        const uint64_t mine = sh.groups[tid];
-        int r = 0;
-#pragma unroll 8
-        for (int g = 0; g < groups; ++g) r += sh.groups[g] > mine;
-        if (r == a.out - 1 && mine > sh.bound) sh.bound = mine;
-      }
+      int r = 0;
+#pragma unroll 16
+      for (int t = 0; t < kThreads; ++t) r += sh.tops[t] > best;
+      if (r == a.out - 1 && best > sh.bound) sh.bound = best;
       __syncthreads();
       bound = sh.bound;
     }
     if (any) {
+      const float wanted_from = bound == 1 ? kNegInf : key_logit(bound);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const uint64_t k = make_key(x[i], first + element_of<F32, Vec>(i));
-        if (k >= bound) sh.keys[atomicAdd(&sh.fill, 1)] = k;
+      for (int j = 0; j < kVec / 4; ++j) {
+        if (!(tops[j] >= wanted_from)) continue;  // (most are not)
+#pragma unroll
+        for (int i = 4 * j; i < 4 * j + 4; ++i) {
+          const uint64_t k = make_key(x[i], first + element_of<F32, Vec>(i));
+          if (k >= bound) sh.keys[atomicAdd(&sh.fill, 1)] = k;
+        }
       }
     }
     __syncthreads();
     // (a full list's last key is the bound from here on)
-    if (sh.fill > 4 * a.out || (sh.fill >= a.out && bound == 1)) keep_best(sh, a.out);
+    if (sh.fill > 2 * a.out) keep_best(sh, a.out);
   }
   // the sums of the warps, then of the block
   float r = warp_max(ref);
+  bool odd = !(sum < INFINITY);
   sum = warp_sum(ref == kNegInf ? 0.f : sum * expf(ref - r));
   if (lane == 0) sh.ref[tid >> 5] = r, sh.sum[tid >> 5] = sum;
   odd = __syncthreads_or(odd);
@@ -238,18 +287,29 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
   }
 }
 
-// A continuation: larger is better, of equal scores the lower place.
+// A continuation: larger is better, of equal scores the lower place.  (Scores
+// are compared as order-preserving integers: the fp64 units are few, and ranks are many comparisons.)
 struct Cand {
-  double v;
+  uint64_t key;
   uint32_t at;  // beam * vocab + token
   uint32_t pad;
 };
-__device__ __forceinline__ bool better(const Cand& a, const Cand& b) { return a.v > b.v || (a.v == b.v && a.at < b.at); }
+__device__ __forceinline__ uint64_t score_key(double v) {
+  const int64_t u = __double_as_longlong(v + 0.0);  // (-0 is 0)
+  return static_cast<uint64_t>(u) ^ (u < 0 ? ~0ull : 1ull << 63);
+}
+__device__ __forceinline__ float key_score(uint64_t k) {
+  return static_cast<float>(__longlong_as_double(static_cast<int64_t>(k >> 63 ? k ^ 1ull << 63 : ~k)));
+}
+// (without branches: ranks are many comparisons)
+__device__ __forceinline__ int better(const Cand& a, const Cand& b) {
+  return static_cast<int>(a.key > b.key) | (static_cast<int>(a.key == b.key) & static_cast<int>(a.at < b.at));
+}
 
 // A block per batch item.  Its lists (a run of one beam's tokens each, or an ended beam's
 // one continuation) are in order, so a bound with n_out continuations at or above it is
 // the n_out-th best of the lists' first ones, or any list's n_out-th one.
-__global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_constant__ SelectArgs a) {
   extern __shared__ __align__(16) uint8_t raw[];
   Cand* cand = reinterpret_cast<Cand*>(raw);  // [lists * out]
   __shared__ Cand heads[kMaxLists];
@@ -261,33 +321,54 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_consta
   grid_dependency_wait();
   grid_launch_dependents();
   const int item = blockIdx.x, tid = threadIdx.x, lists = a.beams * a.splits;
-  if (tid == 0) fill = 0, bound = Cand{-INFINITY, 0xffffffffu, 0};
-  for (int b = tid; b < a.beams; b += kThreads) {
-    const int row = item * a.beams + b;
-    scores[b] = a.score[row];
-    over[b] = a.done != nullptr && a.done[row] != 0;
-    const float4* st = a.stats + (size_t)row * a.splits;
-    float m = kNegInf, odd = 0.f;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, st[s].x), odd += st[s].w;
-    double sum = 0;
-    for (int s = 0; s < a.splits; ++s)
-      if (st[s].x > kNegInf) sum += static_cast<double>(st[s].y * expf(st[s].x - m));
-    const bool ok = !over[b] && odd == 0.f && sum > 0;
-    refs[b] = m;
-    offset[b] = ok ? static_cast<double>(scores[b]) - log(sum) : 0;
-    for (int s = 0; s < a.splits; ++s) count[b * a.splits + s] = ok ? __float_as_int(st[s].z) : 0;
-    // an ended beam's one continuation is its first list's
-    if (over[b] && scores[b] > kNegInf && scores[b] < INFINITY && a.end >= 0) count[b * a.splits] = 1;
+  if (tid == 0) fill = 0, bound = Cand{0, 0xffffffffu, 0};
+  // a warp a beam, a lane a split (at most 128 of them, where there is one beam)
+  for (int b = tid >> 5; b < a.beams; b += kJoinThreads / 32) {
+    const int row = item * a.beams + b, lane = tid & 31;
+    const float score = a.score[row];
+    const bool ended = a.done != nullptr && a.done[row] != 0;
+    float4 st[kMaxLists / 32];
+    float m = kNegInf, sum = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < kMaxLists / 32; ++i) {
+      const int s = i * 32 + lane;
+      st[i] = s < a.splits ? a.stats[(size_t)row * a.splits + s] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+      m = fmaxf(m, st[i].x);
+      odd |= st[i].w != 0.f;
+    }
+    m = warp_max(m);
+    odd = __any_sync(0xffffffffu, odd);
+#pragma unroll
+    for (int i = 0; i < kMaxLists / 32; ++i)
+      if (st[i].x > kNegInf) sum += st[i].y * expf(st[i].x - m);
+    sum = warp_sum(sum);
+    const bool ok = !ended && !odd && sum > 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxLists / 32; ++i) {
+      const int s = i * 32 + lane;
+      // an ended beam's one continuation is its first list's
+      if (s < a.splits)
+        count[b * a.splits + s] = ended ? (s == 0 && score > kNegInf && score < INFINITY && a.end >= 0 ? 1 : 0)
+                                  : ok  ? __float_as_int(st[i].z)
+                                        : 0;
+    }
+    if (lane == 0) {
+      scores[b] = score;
+      over[b] = ended;
+      refs[b] = m;
+      offset[b] = ok ? static_cast<double>(score) - log(static_cast<double>(sum)) : 0;
+    }
   }
   __syncthreads();
   auto get = [&](int list, int i) {
     const int b = list / a.splits;
-    if (over[b]) return Cand{static_cast<double>(scores[b]), static_cast<uint32_t>(b) * a.vocab + a.end, 0};
+    if (over[b]) return Cand{score_key(static_cast<double>(scores[b])), static_cast<uint32_t>(b) * a.vocab + a.end, 0};
     const uint64_t k = a.keys[((size_t)item * lists + list) * a.out + i];
     // (a logit less its reference first: exact, where both are far from 0)
-    return Cand{(static_cast<double>(key_logit(k)) - refs[b]) + offset[b], static_cast<uint32_t>(b) * a.vocab + key_token(k), 0};
+    return Cand{score_key((static_cast<double>(key_logit(k)) - refs[b]) + offset[b]), static_cast<uint32_t>(b) * a.vocab + key_token(k), 0};
   };
-  const Cand none{-INFINITY, 0xffffffffu, 0};
+  const Cand none{0, 0xffffffffu, 0};  // (no finite score has key 0)
   if (tid < lists) {
     heads[tid] = count[tid] > 0 ? get(tid, 0) : none;
     deep[tid] = count[tid] == a.out ? get(tid, a.out - 1) : none;
@@ -296,13 +377,14 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_consta
   if (tid < lists) {
     const Cand h = heads[tid], d = deep[tid];
     int r = 0, rd = 0;
+#pragma unroll 8
     for (int l = 0; l < lists; ++l) {
       r += better(heads[l], h);
       rd += better(deep[l], d);
     }
     // (both may hold: the better one is the bound)
-    if (r == a.out - 1 && h.v > -INFINITY) heads[tid].pad = 1;
-    if (rd == 0 && d.v > -INFINITY) deep[tid].pad = 1;
+    if (r == a.out - 1 && h.key != 0) heads[tid].pad = 1;
+    if (rd == 0 && d.key != 0) deep[tid].pad = 1;
   }
   __syncthreads();
   if (tid < lists) {
@@ -312,7 +394,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_consta
   if (tid < lists && deep[tid].pad && better(deep[tid], bound)) bound = deep[tid];
   __syncthreads();
   const Cand least = bound;
-  for (int i = tid; i < lists * a.out; i += kThreads) {
+  for (int i = tid; i < lists * a.out; i += kJoinThreads) {
     const int list = i / a.out, k = i - list * a.out;
     if (k >= count[list]) continue;
     const Cand c = get(list, k);
@@ -320,20 +402,20 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_consta
   }
   __syncthreads();
   const int n = fill;
-  for (int i = tid; i < n; i += kThreads) {
+  for (int i = tid; i < n; i += kJoinThreads) {
     const Cand c = cand[i];
     int r = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int j = 0; j < n; ++j) r += better(cand[j], c);
     if (r >= a.out) continue;
     const size_t o = (size_t)item * a.out + r;
     const int b = static_cast<int>(c.at / a.vocab), t = static_cast<int>(c.at - static_cast<uint32_t>(b) * a.vocab);
     a.parent[o] = b;
     a.token[o] = t;
-    a.score_out[o] = static_cast<float>(c.v);
+    a.score_out[o] = key_score(c.key);
     if (a.done_out != nullptr) a.done_out[o] = over[b] || t == a.end;
   }
-  for (int r = n + tid; r < a.out; r += kThreads) {
+  for (int r = n + tid; r < a.out; r += kJoinThreads) {
     const size_t o = (size_t)item * a.out + r;
     a.parent[o] = -1;
     a.token[o] = -1;
@@ -345,11 +427,11 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(const __grid_consta
 }  // namespace
 
 size_t select_plan(SelectArgs& a, int batch, int num_sms, void* ws) {
-  // Blocks of 512 threads, four to an SM, as many as there are places, but no
-  // split below a chunk, and lists of a batch item that the second launch can hold.
+  // As many blocks as there are places for eight on an SM, but no split below a
+  // chunk, and lists of a batch item that the second launch can hold.
   const int64_t rows = (int64_t)batch * a.beams;
   const int64_t most = std::min<int64_t>(kMaxLists / a.beams, ((int64_t)a.vocab + kChunk - 1) / kChunk);
-  a.splits = static_cast<int>(std::clamp<int64_t>(4ll * num_sms / rows, 1, most));
+  a.splits = static_cast<int>(std::clamp<int64_t>(kBlocks * num_sms / rows, 1, most));
   a.per = static_cast<int>((((int64_t)a.vocab + a.splits - 1) / a.splits + 7) / 8 * 8);
   const size_t stats = align_up((size_t)rows * a.splits * sizeof(float4), 256);
   if (ws != nullptr) {
@@ -374,7 +456,7 @@ cudaError_t launch_beam_select(const SelectArgs& a, int batch, bool f32, cudaStr
   e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            kMaxLists * kMaxOut * static_cast<int>(sizeof(Cand)));
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_join_kernel, dim3(batch), block, smem, stream, a);
+  return launch_pdl(beam_join_kernel, dim3(batch), dim3(kJoinThreads), smem, stream, a);
 }
 
 }  // namespace mkv

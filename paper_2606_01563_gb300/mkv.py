@@ -185,8 +185,7 @@ def lib():
         L.mkv_prefix_workspace_size.restype = ctypes.c_size_t
         L.mkv_prefix_workspace_size.argtypes = [mkv_geom, c_i32, c_i32, c_i32]
         L.mkv_prefix_step.restype = c_i32
-        L.mkv_prefix_step.argtypes = [mkv_geom, c_vp, c_vp, c_vp, c_vp, ctypes.POINTER(mkv_cache),
-                                      ctypes.POINTER(mkv_moments), ctypes.POINTER(mkv_cache),
+        L.mkv_prefix_step.argtypes = [mkv_geom, c_vp, c_vp, c_vp, c_vp, c_vp, ctypes.POINTER(mkv_moments), c_vp,
                                       ctypes.POINTER(mkv_decode_params), c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
         L.mkv_beam_select_workspace_size.restype = ctypes.c_size_t
         L.mkv_beam_select_workspace_size.argtypes = [c_i32, c_i32, c_i32, c_i32]
@@ -214,6 +213,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+# (of torch too; the public one checks first whether CUDA was initialised, which a CUDA tensor's being there says)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
@@ -581,11 +584,19 @@ _I64x12, _I64x17 = ([ctypes.c_int64 * (m * n) for n in range(5)] for m in (12, 1
 
 
 def _here(*tensors):
-    """Refuses tensors that are not on the current device: the kernels run there, on its stream."""
-    at = torch.cuda.current_device()
+    """Refuses tensors that are not on the current device, whose index it returns: the kernels run there, on its stream."""
+    at = _device()
     for t in tensors:
         if t is not None and t.get_device() != at:
             raise ValueError(f"tensors on the current device (cuda:{at}), not on {t.device}")
+    return at
+
+
+def _stream_of(stream, device):
+    """The handle of `stream`, or of the current one of `device`."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
 def _positions(pos, p):
@@ -598,26 +609,28 @@ def _positions(pos, p):
     return b, t, ps[0], ps[1] if b > 1 else 0
 
 
-def _rows(t, b, tokens, d):
-    """The heads of a bf16 [b, tokens, heads, d] tensor with adjacent dims, and its strides in elements."""
-    shape, s = t.shape, t.stride()
-    if t.dtype is not _BF16 or len(shape) != 4 or shape[0] != b or shape[1] != tokens or shape[3] != d or s[3] != 1:
-        raise ValueError("tensors: bf16 [b, tokens, heads, d] with adjacent dims")
-    h = shape[2]
-    # (a stride over an extent of one is never used)
-    return h, s[0] if b > 1 else 0, s[1] if tokens > 1 else 0, s[2] if h > 1 else 0
+def _row_strides(t, shape):
+    """The strides in elements of a bf16 tensor of this shape [b, tokens, heads, d] with adjacent dims."""
+    s = t.stride()
+    if t.dtype is not _BF16 or t.shape != shape or s[3] != 1:
+        raise ValueError("tensors: bf16 [b, tokens, heads, d] of one shape, with adjacent dims")
+    if 1 in shape:  # (a stride over an extent of one is never used)
+        return [x if e > 1 else 0 for x, e in zip(s[:3], shape)]
+    return s[:3]
 
 
 def _norm_weight(w, heads, d):
     """(address, elements from head to head, fp32 or not) of a norm's weights [d] or [heads, d], or None."""
     if w is None:
         return 0, 0, 0
-    if w.dtype not in (_BF16, torch.float32) or w.shape not in ((d,), (heads, d)) or w.stride(-1) != 1:
+    shape, s, f32 = w.shape, w.stride(), w.dtype is torch.float32
+    if (not f32 and w.dtype is not _BF16) or s[-1] != 1 or (shape != (d,) and shape != (heads, d)):
         raise ValueError("weights: bf16 or float32, [d] or [heads, d] with adjacent dims")
-    step = w.stride(0) if w.dim() == 2 else 0
-    if w.dim() == 2 and step == 0 and heads > 1:
+    if len(s) == 1:
+        return w.data_ptr(), 0, f32
+    if heads > 1 and s[0] == 0:
         raise ValueError("weights: [heads, d] not expanded over heads ([d] is one row for all)")
-    return w.data_ptr(), step or (d if w.dim() == 2 else 0), int(w.dtype is torch.float32)
+    return w.data_ptr(), s[0] if heads > 1 else d, f32
 
 
 def mkv_norm_rope(pos, p: mkv_rope_params, tensors, eps, stream=None):
@@ -626,63 +639,62 @@ def mkv_norm_rope(pos, p: mkv_rope_params, tensors, eps, stream=None):
     b, t, pa, pb = _positions(pos, p)
     if not 0 < len(tensors) < 5:
         raise ValueError("tensors: one to four (in, out, weight)")
-    d = tensors[0][0].shape[-1]
-    flat = []
+    flat, all_, d = [], [pos], tensors[0][0].shape[-1]
     for x, y, w in tensors:
-        hx, *xs = _rows(x, b, t, d)
-        hy, *ys = _rows(y, b, t, d)
-        if hx != hy:
-            raise ValueError("tensors: in and out of the same shape")
-        at, step, f32 = _norm_weight(w, hx, d)
-        _here(pos, x, y, w)
-        flat += (x.data_ptr(), y.data_ptr(), hx, *xs, *ys, at, step, f32)
+        shape = x.shape
+        h = shape[2] if len(shape) == 4 else 0
+        if shape != (b, t, h, d):
+            raise ValueError("tensors: bf16 [b, tokens, heads, d], of the positions' b and tokens")
+        flat += (x.data_ptr(), y.data_ptr(), h, *_row_strides(x, shape), *_row_strides(y, shape), *_norm_weight(w, h, d))
+        all_ += (x, y, w)
     code = lib().mkv_norm_rope(b, t, d, pos.data_ptr(), pa, pb, p, eps, len(tensors), _I64x12[len(tensors)](*flat),
-                               _stream(stream))
+                               _stream_of(stream, _here(*all_)))
     if code:
         _check(code, "mkv_norm_rope")
 
 
-def _grad_tensors(tensors, b, t, d):
-    """The C structures of mkv_norm_rope_grad's tensors, checked."""
+def _grad_tensors(tensors):
+    """b, tokens, the head dim and the C structures of mkv_norm_rope_grad's tensors, checked."""
     if not 0 < len(tensors) < 5:
         raise ValueError("tensors: one to four (x, dy, dx, weight, dweight)")
-    flat = []
+    flat, first = [], None
     for x, dy, dx, w, dw in tensors:
-        hx, *xs = _rows(x, b, t, d)
-        hy, *ys = _rows(dy, b, t, d)
-        hd, *ds = _rows(dx, b, t, d)
-        if hx != hy or hx != hd:
-            raise ValueError("tensors: x, dy and dx of the same shape")
-        at, step, f32 = _norm_weight(w, hx, d)
+        shape = x.shape
+        if len(shape) != 4:
+            raise ValueError("tensors: bf16 [b, tokens, heads, d]")
+        b, t, h, d = shape
+        first = first or (b, t, d)
+        if first != (b, t, d):
+            raise ValueError("tensors: of the same batch, tokens and head dim")
         if dw is not None and (w is None or dw.dtype is not torch.float32 or dw.shape != w.shape or not dw.is_contiguous()):
             raise ValueError("dweight: contiguous float32 of the weights' shape")
-        flat += (x.data_ptr(), dy.data_ptr(), dx.data_ptr(), hx, *xs, *ys, *ds, at, step, f32,
-                 0 if dw is None else dw.data_ptr())
-    return _I64x17[len(tensors)](*flat)
+        flat += (x.data_ptr(), dy.data_ptr(), dx.data_ptr(), h, *_row_strides(x, shape), *_row_strides(dy, shape),
+                 *_row_strides(dx, shape), *_norm_weight(w, h, d), 0 if dw is None else dw.data_ptr())
+    return first, _I64x17[len(tensors)](*flat)
 
 
 def mkv_norm_rope_grad_workspace_size(tensors):
     """Bytes for mkv_norm_rope_grad of these tensors."""
-    b, t, _, d = tensors[0][0].shape
-    return lib().mkv_norm_rope_grad_workspace_size(b, t, d, len(tensors), _grad_tensors(tensors, b, t, d))
+    (b, t, d), array = _grad_tensors(tensors)
+    return lib().mkv_norm_rope_grad_workspace_size(b, t, d, len(tensors), array)
 
 
 def mkv_norm_rope_grad(pos, p: mkv_rope_params, tensors, eps, ws, stream=None):
     """The gradient of mkv_norm_rope: (x, dy, dx, weight, dweight) of every tensor, x, dy and dx bf16 [b, tokens, heads,
     d] with adjacent dims (dx may be x or dy), dweight float32 of the weights' shape, overwritten, or None."""
     b, t, pa, pb = _positions(pos, p)
-    d = tensors[0][0].shape[-1] if tensors else 0
-    flat = _grad_tensors(tensors, b, t, d)
-    for tensor in tensors:
-        _here(pos, ws, *tensor)
-    code = lib().mkv_norm_rope_grad(b, t, d, pos.data_ptr(), pa, pb, p, eps, len(tensors), flat, ws.data_ptr(),
-                                    ws.numel(), _stream(stream))
+    of, array = _grad_tensors(tensors)
+    if of[:2] != (b, t):
+        raise ValueError("tensors: of the positions' b and tokens")
+    at = _here(pos, ws, *[x for tensor in tensors for x in tensor])
+    code = lib().mkv_norm_rope_grad(b, t, of[2], pos.data_ptr(), pa, pb, p, eps, len(tensors), array, ws.data_ptr(),
+                                    ws.numel(), _stream_of(stream, at))
     if code:
         _check(code, "mkv_norm_rope_grad")
 
 
 # --------------------------------------------- several continuations of a prompt
-_I64x6 = ctypes.c_int64 * 6
+_I64x6, _I64x8 = ctypes.c_int64 * 6, ctypes.c_int64 * 8
 
 
 def mkv_prefix_workspace_size(g, n_seqs, capacity, tail_capacity):
@@ -724,11 +736,16 @@ def mkv_prefix_step(g, seqs: Seqs, q, k_new, v_new, prefix: Cache, mom: Moments 
     kp, kt = prefix.K.shape, tail.K.shape
     if (kp[0], kp[1], kp[3]) != (b, h, d) or (kt[0], kt[1], kt[3]) != (b * n, h, d):
         raise ValueError("prefix: [b, h_kv, ...]; tail: [b * N, h_kv, ...]")
-    _here(q, k_new, v_new, out, lse, ws, prefix.K, tail.K)
+    at = _here(q, k_new, v_new, out, lse, ws, prefix.K, tail.K)
     s = _I64x6(n, 0 if seqs.count is None else seqs.count.data_ptr(), *qs, *ks)
-    code = lib().mkv_prefix_step(g, s, q.data_ptr(), _ptr(k_new), _ptr(v_new), prefix.c(),
-                                 None if mom is None else mom.c(), tail.c(), p, out.data_ptr(), _ptr(lse),
-                                 ws.data_ptr(), ws.numel(), _stream(stream))
+    # (the caches' y rows are not used)
+    shared = _I64x8(prefix.K.data_ptr(), prefix.V.data_ptr(), prefix.pos.data_ptr(), prefix.len.data_ptr(),
+                    prefix.seen.data_ptr(), kp[2], 0, 0)
+    own = _I64x8(tail.K.data_ptr(), tail.V.data_ptr(), tail.pos.data_ptr(), tail.len.data_ptr(), tail.seen.data_ptr(),
+                 kt[2], 0, 0)
+    code = lib().mkv_prefix_step(g, s, q.data_ptr(), _ptr(k_new), _ptr(v_new), shared,
+                                 None if mom is None else mom.c(), own, p, out.data_ptr(), _ptr(lse), ws.data_ptr(),
+                                 ws.numel(), _stream_of(stream, at))
     if code:
         _check(code, "mkv_prefix_step")
 
@@ -756,12 +773,12 @@ def mkv_beam_select(logits, score, parent, token, score_out, ws, done=None, done
         _int32(done, rows, "done")
     if done_out is not None:
         _int32(done_out, out, "done_out")
-    _here(logits, score, done, parent, token, score_out, done_out, ws)
+    at = _here(logits, score, done, parent, token, score_out, done_out, ws)
     # (strides over an extent of one are never used)
     s = _I64x7(logits.data_ptr(), int(lt is torch.float32), ls[0] if b > 1 else 0, ls[1] if beams > 1 else 0,
                score.data_ptr(), 0 if done is None else done.data_ptr(), end_token)
     code = lib().mkv_beam_select(b, beams, vocab, s, out[1], parent.data_ptr(), token.data_ptr(), score_out.data_ptr(),
-                                 _ptr(done_out), ws.data_ptr(), ws.numel(), _stream(stream))
+                                 _ptr(done_out), ws.data_ptr(), ws.numel(), _stream_of(stream, at))
     if code:
         _check(code, "mkv_beam_select")
 
@@ -800,9 +817,9 @@ def mkv_beam_reorder(g, layers: BeamLayers, parent, ws, stream=None):
     b, n = parent.shape
     _int32(parent, (g.batch, n), "parent")
     _need(layers.shape == (b * n, g.n_kv_heads, g.head_dim), "layers: states [b * N, h_kv] of this geometry")
-    _here(parent, ws)
+    at = _here(parent, ws)
     code = lib().mkv_beam_reorder(g, n, len(layers.array), layers.array, parent.data_ptr(), ws.data_ptr(), ws.numel(),
-                                  _stream(stream))
+                                  _stream_of(stream, at))
     if code:
         _check(code, "mkv_beam_reorder")
 

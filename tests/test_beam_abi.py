@@ -147,7 +147,8 @@ def test_prefix_refusals(L):
              prefix=C(FAKE, FAKE, FAKE, FAKE, FAKE, 64), tail=C(FAKE, FAKE, FAKE, FAKE, FAKE, 9), null=False,
              mom=mkv.mkv_moments(FAKE, FAKE, FAKE, FAKE), p=mkv.mkv_decode_params(1, 1, 1e-6), ws=FAKE, wsb=1 << 40):
         s = mkv.mkv_seqs(n, count, *strides)
-        return L.mkv_prefix_step(g, None if null else ctypes.byref(s), q, k, v, prefix, mom, tail, p, out, lse, ws, wsb, None)
+        return L.mkv_prefix_step(g, None if null else ctypes.byref(s), q, k, v, ctypes.byref(prefix), mom, ctypes.byref(tail), p, out,
+                                 lse, ws, wsb, None)
     assert call(g=mkv.geom(2, 3, 4, 96)) == UNSUPPORTED and call(g=mkv.geom(2, 3, 3, 128)) == SHAPE
     for n in (0, 257, -1):
         assert call(n=n) == SHAPE and mkv.mkv_prefix_workspace_size(mkv.geom(1, 1, 1, 64), n, 10, 10) == 0
