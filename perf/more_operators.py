@@ -196,6 +196,7 @@ def _prefix_call(s):
     c = s["case"]
     b, n, h, g, d = c["batch"], c["seqs"], c["heads"], c["group"], c["dim"]
     geom = mkv.geom(b, h, g, d)
+    s["Kt"], s["Vt"] = s["Kt"].contiguous(), s["Vt"].contiguous()  # (of one prompt's sequences they are a transposed view)
     prefix = mkv.Cache(s["K"], s["V"], s["pos"], s["len"], s["seen"])
     tail = mkv.Cache(s["Kt"], s["Vt"], s["post"], s["state"][0], s["state"][1])
     mom, c16, split = None, None, None
