@@ -713,6 +713,20 @@ def _strides(t, shape, what):
     return s[1] if n else 0, s[0] if b else 0
 
 
+def _slabs(c: Cache, shape, what):
+    """The C structure of a cache whose tensors are the dense slabs [units, h_kv, capacity, d] it stands for (without
+    the y rows)."""
+    k, v, pos, length, seen = c.K, c.V, c.pos, c.len, c.seen
+    of, i32 = k.shape, torch.int32
+    if (of[0], of[1], of[3]) != shape or v.shape != of or pos.shape != of[:3] or length.shape != of[:2] or seen.shape != of[:2]:
+        raise ValueError(f"{what}: K and V [{shape[0]}, {shape[1]}, capacity, {shape[2]}], pos, len and seen of their units")
+    if (k.dtype is not _BF16 or v.dtype is not _BF16 or pos.dtype is not i32 or length.dtype is not i32
+            or seen.dtype is not i32 or not (k.is_contiguous() and v.is_contiguous() and pos.is_contiguous()
+                                             and length.is_contiguous() and seen.is_contiguous())):
+        raise ValueError(f"{what}: contiguous bf16 K and V, int32 pos, len and seen")
+    return _I64x8(k.data_ptr(), v.data_ptr(), pos.data_ptr(), length.data_ptr(), seen.data_ptr(), of[2], 0, 0)
+
+
 def mkv_prefix_step(g, seqs: Seqs, q, k_new, v_new, prefix: Cache, mom: Moments | None, tail: Cache,
                     p: mkv_decode_params, out, lse, ws, stream=None):
     """One decoding step of N sequences per prompt: q bf16 [b, N, g*h_kv, d], k_new and v_new bf16 [b, N, h_kv, d] or
@@ -733,16 +747,12 @@ def mkv_prefix_step(g, seqs: Seqs, q, k_new, v_new, prefix: Cache, mom: Moments 
         raise ValueError(f"out: contiguous bf16 {list(of)}")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != of[:3] or not lse.is_contiguous()):
         raise ValueError("lse: contiguous float32 [b, N, g*h_kv]")
-    kp, kt = prefix.K.shape, tail.K.shape
-    if (kp[0], kp[1], kp[3]) != (b, h, d) or (kt[0], kt[1], kt[3]) != (b * n, h, d):
-        raise ValueError("prefix: [b, h_kv, ...]; tail: [b * N, h_kv, ...]")
-    at = _here(q, k_new, v_new, out, lse, ws, prefix.K, tail.K)
+    shared, own = _slabs(prefix, (b, h, d), "prefix"), _slabs(tail, (b * n, h, d), "tail")
+    if mom is not None and not (mom.n.is_contiguous() and mom.mu_k.is_contiguous() and mom.mu_v.is_contiguous()
+                                and mom.C.is_contiguous() and mom.C.shape == (b, h, d, d)):
+        raise ValueError("mom: contiguous moments of the prefix's units")
+    at = _here(q, k_new, v_new, out, lse, ws, prefix.K, prefix.V, prefix.len, tail.K, tail.V, tail.len, seqs.count)
     s = _I64x6(n, 0 if seqs.count is None else seqs.count.data_ptr(), *qs, *ks)
-    # (the caches' y rows are not used)
-    shared = _I64x8(prefix.K.data_ptr(), prefix.V.data_ptr(), prefix.pos.data_ptr(), prefix.len.data_ptr(),
-                    prefix.seen.data_ptr(), kp[2], 0, 0)
-    own = _I64x8(tail.K.data_ptr(), tail.V.data_ptr(), tail.pos.data_ptr(), tail.len.data_ptr(), tail.seen.data_ptr(),
-                 kt[2], 0, 0)
     code = lib().mkv_prefix_step(g, s, q.data_ptr(), _ptr(k_new), _ptr(v_new), shared,
                                  None if mom is None else mom.c(), own, p, out.data_ptr(), _ptr(lse), ws.data_ptr(),
                                  ws.numel(), _stream_of(stream, at))

@@ -185,9 +185,15 @@ def test_prefix_binding_refusals():
                   good["q"][:, :1].expand(-1, 3, -1, -1), torch.zeros(2, 3, 4, 128, **b16)[..., ::2], torch.zeros(2, 3, 8, 64, **b16)[:, :, ::2]),
                k_new=(None, good["k_new"].half(), torch.zeros(2, 3, 4, 64, **b16)[:, :, :2]),
                v_new=(None, torch.zeros(2, 4, 2, 64, **b16)), out=(good["out"].float(), torch.zeros(2, 6, 4, 64, **b16)[:, ::2]),
-               lse=(torch.zeros(2, 3, 2), torch.zeros(2, 3, 4, dtype=torch.float64)), prefix=(tail,), tail=(prefix,))
+               lse=(torch.zeros(2, 3, 2), torch.zeros(2, 3, 4, dtype=torch.float64)), prefix=(tail,), tail=(prefix,),
+               mom=(mkv.alloc_moments(mkv.geom(2, 3, 2, 64), device="cpu"),))
+    # a cache whose tensors are not dense slabs: a transposed view has its units in another order
+    for name, x in (("K", torch.zeros(2, 6, 4, 64, **b16).transpose(0, 1)), ("V", torch.zeros(6, 2, 64, 4, **b16).transpose(2, 3)),
+                    ("len", torch.zeros(2, 6, dtype=torch.int32).t()), ("pos", torch.zeros(6, 2, 8, dtype=torch.int32)[..., ::2]),
+                    ("K", tail.K.float()), ("seen", tail.seen.long()), ("V", torch.zeros(6, 2, 5, 64, **b16))):
+        bad["tail"] += (mkv.Cache(**{**tail.__dict__, name: x}),)
     for name, values in bad.items():
         for x in values:
             with pytest.raises(ValueError):
-                mkv.mkv_prefix_step(g, **{**good, name: x}, mom=None, p=mkv.mkv_decode_params(0, 1, 1e-6),
+                mkv.mkv_prefix_step(g, **{"mom": None, **good, name: x}, p=mkv.mkv_decode_params(0, 1, 1e-6),
                                     ws=torch.zeros(1 << 20, dtype=torch.uint8))
