@@ -106,6 +106,7 @@ struct ReorderArgs {
   int32_t N;
   int32_t n_kv;
   int32_t D;
+  int32_t split;  // blocks of the bulk copies of an item, layer and head (filled by the launcher)
   uint32_t polls;
   void* ws;
 };

@@ -9,8 +9,9 @@
 // Loads and stores are bulk copies; one warp issues them, a range
 // loading while the one before is stored.
 //
-// Lengths change last: a second launch moves the positions, means and counts,
-// after every block of the first has read the lengths.
+// Positions and means, which need not start at 16 bytes, are blocks of their own
+// that go through shared memory word by word.  Lengths and counts change last: a
+// second launch, after every block of the first has read the lengths.
 //
 // Bounded by HBM: the bytes of the parents read and of the changed slots written.
 #include <algorithm>
@@ -28,7 +29,6 @@ constexpr int kThreads = 128;
 constexpr int kRing = 96 * 1024;  // of a block: two fit an SM
 constexpr int kStages = 2;
 constexpr int kSmallThreads = 256;
-constexpr int kSmallWords = 8192;
 
 __device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes)
@@ -91,6 +91,29 @@ __device__ __forceinline__ bool read_slots(const ReorderArgs& a, const ReorderLa
   return s.reads > 0;
 }
 
+// `stride` words of an array per unit, of which slot j holds have(j), at most
+// `most`: from the slots that are read into shared memory, then to the others.
+template <typename Have>
+__device__ __forceinline__ void move_words(const ReorderArgs& a, const Slots& s, int item, int kv, int32_t* base,
+                                           size_t stride, int most, int32_t* words, Have have) {
+  if (base == nullptr) return;
+  const int per = kRing / 4 / s.reads;  // words of a slot at a time (at least 96)
+  auto unit = [&](int j) { return (size_t)((item * a.N + j) * a.n_kv + kv); };
+  for (int w0 = 0; w0 < most; w0 += per) {
+    const int n = min(per, most - w0);
+    __syncthreads();
+    for (int j = 0; j < a.N; ++j)
+      if (s.place[j] >= 0)
+        for (int w = threadIdx.x; w < min(n, have(j) - w0); w += kThreads) words[s.place[j] * per + w] = base[unit(j) * stride + w0 + w];
+    __syncthreads();
+    for (int j = 0; j < a.N; ++j) {
+      const int p = s.parent[j];
+      if (p >= 0)
+        for (int w = threadIdx.x; w < min(n, have(p) - w0); w += kThreads) base[unit(j) * stride + w0 + w] = words[s.place[p] * per + w];
+    }
+  }
+}
+
 __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant__ ReorderArgs a) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ Slots s;
@@ -101,7 +124,18 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
   mbar_fence_init();
   grid_dependency_wait();
   grid_launch_dependents();
-  if (!read_slots<kThreads>(a, l, item, kv, blockIdx.x == 0, s) || tid >= 32) return;
+  if (!read_slots<kThreads>(a, l, item, kv, blockIdx.x == 0, s)) return;
+  if (blockIdx.x >= a.split) {
+    int32_t* words = reinterpret_cast<int32_t*>(ring);
+    if (blockIdx.x == a.split) {
+      move_words(a, s, item, kv, l.pos, l.cap, s.longest, words, [&](int j) { return s.length[j]; });
+    } else {
+      move_words(a, s, item, kv, l.mu_k, a.D, a.D, words, [&](int) { return a.D; });
+      move_words(a, s, item, kv, l.mu_v, a.D, a.D, words, [&](int) { return a.D; });
+    }
+    return;
+  }
+  if (tid >= 32) return;
   // one warp from here on
   const uint32_t range = kRing / kStages / s.reads / 128 * 128;  // bytes of a slot (at least 128: 256 slots)
   const uint32_t row = a.D * 2;
@@ -159,11 +193,11 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
       if (n > 0) bulk_g2s(ring + (size_t)stage * (kRing / kStages) + (size_t)s.place[j] * range, at(r, j), n, &full[stage]);
     }
   };
-  uint32_t i = blockIdx.x, phase[kStages] = {};
+  uint32_t i = blockIdx.x, phase[kStages] = {};  // (of a.split blocks)
   int stage = 0;
   if (i < total) load(i, 0);
-  for (; i < total; i += gridDim.x) {
-    const uint32_t next = i + gridDim.x;
+  for (; i < total; i += a.split) {
+    const uint32_t next = i + a.split;
     if (next < total) {
       // (the next stage's stores have read shared memory)
       asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -194,39 +228,27 @@ __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant
   __syncwarp();
 }
 
-// Positions, means and counts: a block per item, layer and head.
+// Lengths and counts: a block per item, layer and head, a thread a slot.
 __global__ void __launch_bounds__(kSmallThreads) reorder_small_kernel(const __grid_constant__ ReorderArgs a) {
-  __shared__ Slots s;
-  __shared__ int32_t words[kSmallWords];
-  const int tid = threadIdx.x, item = blockIdx.y / a.n_kv, kv = blockIdx.y - item * a.n_kv;
+  __shared__ int bad;
+  const int j = threadIdx.x, item = blockIdx.y / a.n_kv, kv = blockIdx.y - item * a.n_kv;
   const ReorderLayer& l = a.layer[blockIdx.z];
+  if (j == 0) bad = 0;
   grid_dependency_wait();
-  if (!read_slots<kSmallThreads>(a, l, item, kv, false, s)) return;
-  const int per = kSmallWords / s.reads;  // words of a slot at a time (at least 32)
-  auto unit = [&](int j) { return (size_t)((item * a.N + j) * a.n_kv + kv); };
-  // `stride` words of an array per unit, of which slot j holds have(j), at most `most`
-  auto move = [&](int32_t* base, size_t stride, int most, auto have) {
-    if (base == nullptr) return;
-    for (int w0 = 0; w0 < most; w0 += per) {
-      const int n = min(per, most - w0);
-      __syncthreads();
-      for (int x = tid; x < a.N * n; x += kSmallThreads) {
-        const int j = x / n, w = x - j * n;
-        if (s.place[j] >= 0 && w0 + w < have(j)) words[s.place[j] * per + w] = base[unit(j) * stride + w0 + w];
-      }
-      __syncthreads();
-      for (int x = tid; x < a.N * n; x += kSmallThreads) {
-        const int j = x / n, w = x - j * n, p = s.parent[j];
-        if (p >= 0 && w0 + w < have(p)) base[unit(j) * stride + w0 + w] = words[s.place[p] * per + w];
-      }
-    }
-  };
-  move(l.pos, l.cap, s.longest, [&](int j) { return s.length[j]; });
-  move(l.mu_k, a.D, a.D, [&](int) { return a.D; });
-  move(l.mu_v, a.D, a.D, [&](int) { return a.D; });
-  int32_t* one[4] = {l.n, l.seen, l.len, l.y_len};
+  __syncthreads();
+  const int p = j < a.N ? a.parent[(size_t)item * a.N + j] : -1;
+  if (p < -1 || p >= a.N) bad = 1;
+  int32_t* const array[4] = {l.n, l.seen, l.len, l.y_len};
+  const bool moves = p >= 0 && p < a.N && p != j;
+  const size_t from = (size_t)((item * a.N + p) * a.n_kv + kv), to = (size_t)((item * a.N + j) * a.n_kv + kv);
+  int32_t x[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) move(one[k], 1, 1, [](int) { return 1; });
+  for (int k = 0; k < 4; ++k) x[k] = moves && array[k] != nullptr ? array[k][from] : 0;
+  __syncthreads();
+  if (bad || !moves) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (array[k] != nullptr) array[k][to] = x[k];
 }
 
 }  // namespace
@@ -242,7 +264,10 @@ cudaError_t launch_beam_reorder(const ReorderArgs& args, int layers, int batch, 
   for (int i = 0; i < layers; ++i) cap = std::max(cap, a.layer[i].cap);
   const int64_t ranges = std::max<int64_t>(1, (int64_t)cap * a.D * 4 * a.N / (kRing / kStages));
   const int split = static_cast<int>(std::clamp<int64_t>((4ll * num_sms + units - 1) / units, 1, std::min<int64_t>(ranges, 256)));
-  const dim3 grid(split, batch * a.n_kv, layers);
+  bool means = false;
+  for (int i = 0; i < layers; ++i) means |= a.layer[i].mu_k != nullptr;
+  a.split = split;
+  const dim3 grid(split + (means ? 2 : 1), batch * a.n_kv, layers);
   e = launch_pdl(reorder_kernel, grid, dim3(kThreads), kRing, stream, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(reorder_small_kernel, dim3(1, batch * a.n_kv, layers), dim3(kSmallThreads), 0, stream, a);
