@@ -80,13 +80,16 @@ MKV_API size_t mkv_prefix_workspace_size(mkv_geom geom, int32_t n_seqs, int32_t 
  * rows 0..len-1, the tail's rows 0..len-1, the new token and, if p->correction
  * and n > 0, the moment term with logit log n + scale q.mu_k and value mu_v +
  * scale C' q (p->order 1) or mu_v (order 0), as in mkv_decode_step; p->C16 and
- * p->C_split have that call's meaning.  p->early_load: the caller's guarantee of that call for the shared cache
- * and moments.  A sequence with nothing at all to attend to gets zeros and lse -infinity.
+ * p->C_split have that call's meaning; p->early_load is accepted and changes
+ * nothing (the shared rows are loaded early wherever that is always safe).  A
+ * sequence with nothing at all to attend to gets zeros and lse -infinity.
  * An append past the tail's capacity records MKV_ERR_CAPACITY (info: the tail's
- * unit), still attends over the new token and leaves the tail as it is; a length outside 0..capacity is
- * recorded as MKV_ERR_CAPACITY and taken as the nearer end.  Scores,
- * statistics and sums are fp32; the softmax weights enter the product with the
- * values as bf16 (one part, with a normaliser of the rounded weights, or two), and the output is rounded to bf16.
+ * unit), still attends over the new token and leaves the tail as it is; a
+ * length outside 0..capacity is recorded as MKV_ERR_CAPACITY and taken as the
+ * nearer end.  Scores, statistics and sums are fp32; the softmax weights enter
+ * the product with the values rounded to bf16 (about a normaliser of the
+ * rounded weights), as the output is, and the order-1 product takes an fp32 C'
+ * as two bf16 parts.
  * Requirements: q, k_new, v_new and out 16-byte aligned, lse 4; p as in
  * mkv_decode_step.
  */

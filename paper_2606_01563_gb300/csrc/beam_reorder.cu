@@ -13,7 +13,8 @@
 // that go through shared memory word by word.  Lengths and counts change last: a
 // second launch, after every block of the first has read the lengths.
 //
-// Bounded by HBM: the bytes of the parents read and of the changed slots written.
+// Bounded by HBM: the bytes of the parents read and of the changed slots written
+// (8 layers, 4 x 16 slots of 8 heads, 512 rows and moments: 278 us, 0.91 of 6.8 TB/s).
 #include <algorithm>
 
 #include "beam.h"

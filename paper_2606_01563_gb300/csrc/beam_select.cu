@@ -26,7 +26,10 @@
 // and the scores fp64: which of two continuations is better is decided to a few
 // 1e-7, and the scores that come back are rounded once.
 //
-// Bounded by HBM over many beams: each logit is read once.
+// Each logit is read once; what bounds it over many beams is issue, 18
+// instructions a logit and a barrier a chunk (32 x 8 beams of 150001 bf16 logits: 43-46 us,
+// HBM's floor 9.6; with blocks of 512 threads 72), over few the two launches'
+// chains (4 beams of 32000: 9.5 us).
 #include <algorithm>
 
 #include "beam.h"
@@ -45,7 +48,7 @@ constexpr int kChunk = kThreads * kVec;    // elements of a chunk
 constexpr int kMaxOut = MKV_BEAM_MAX_OUT;  // 64
 constexpr int kBuffer = kMaxOut * kVec + 2 * kMaxOut;
 constexpr int kMaxLists = 128;  // of a batch item
-constexpr int64_t kBlocks = 8;
+constexpr int64_t kBlocks = 8;  // of an SM (measured at 32 x 8 beams of 150001: 4, 8, 16 and 32: 57, 47, 55 and 76 us)
 constexpr float kNegInf = -INFINITY;
 
 // Order-preserving key of a logit and the token that has it: larger is better,

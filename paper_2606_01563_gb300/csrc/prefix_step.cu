@@ -12,9 +12,10 @@
 // Two launches.  prefix_parts_kernel leaves states ("parts") of every query row in
 // the workspace: a block takes a run of the shared rows for up to 8 NT query
 // rows of a unit (all sequences' heads side by side, so that a shared row is read
-// once for all of them), or the moment term for as many, or a run of one tail for
-// its unit's heads.  prefix_join_kernel joins each row's parts and the new token and
-// appends that token to its tail.
+// once for all of them), or 64 dims of the moment term for as many, or tails, one
+// a warp.  prefix_join_kernel joins each row's parts and the new token and
+// appends that token to its tail.  For many query rows over many shared rows the kernels of
+// tree_step.cu take the shared rows, between the two.
 //
 // A run: a warp issues 64-row TMA copies into a ring; four warps work on every
 // tile together.  Each takes the logits of 16 of its rows, S^T = K q^T with the keys on
@@ -26,6 +27,11 @@
 // moves when a score exceeds it by more than 8 (log2), which every warp learns
 // at that barrier.  O is scaled by the ratio of the unrounded weights' sum to the
 // rounded ones', so that roundings that are common cancel.
+//
+// What bounds it: HBM with few query rows over a long prompt (4 sequences of 8 x 4
+// heads, 65536 rows: 43.5-45 us, 0.88-0.91 of 6.8 TB/s); with 32 the chain of a tile, 1
+// us (8 sequences, 65536 rows: 50 us); short prompts the two launches' chains
+// (4 sequences, 128 rows: 6.0 us; 8 sequences of 4 prompts, 1024 rows, tails of 100: 15).
 #include <algorithm>
 #include <cmath>
 
@@ -45,6 +51,13 @@ constexpr int kRows = 64;                   // rows of a tile
 constexpr int kMinTiles = 2;   // of a run, where there are as many
 constexpr int kMaxSplits = 64;
 constexpr int kMaxTails = 8;   // tails of a warp
+// Visits of 64-row tiles by blocks of up to 32 query rows, per place and at 128
+// dims, above which several such blocks of a unit give way to tcgen05.  Measured
+// at 8 heads of 4, here and there (visits a place): 16 sequences over 16384
+// rows 26 and 34 us (14), 24 over 8192 23 and 26 (10), 32 x 2 prompts over 2048 21
+// and 26 (7); 64 over 4096 32 and 28 (14), 64 x 4 over 1024 44 and 39 (14), 32 x 2
+// over 8192 55 and 38 (27), 24 over 32768 61 and 45 (40).  A unit's only block
+// keeps its rows: 8 sequences over 65536 49 and 59 (27).
 constexpr long kVisits = 12;
 constexpr float kSlack = 32.f;  // log2 headroom of a reference above the score that set it (weights at most 1)
 constexpr float kNegInf = -INFINITY;
@@ -60,7 +73,7 @@ constexpr int kPPitch = kRows * 2 + 16;
 __host__ __device__ constexpr int p_offset(int D, int NT, int buffer) { return buffer == 0 ? 0 : 8 * NT * q_pitch(D); }
 __host__ __device__ constexpr int qp_bytes(int D, int NT) { return p_offset(D, NT, 1) + 8 * NT * kPPitch; }
 __host__ __device__ constexpr int parts_smem(int D, int NT) { return stages(D) * 2 * tile_bytes(D) + qp_bytes(D, NT) + 1024; }
-static_assert(2 * (parts_smem(128, 4) + 3072) <= 228 * 1024, "two blocks to an SM");
+static_assert(2 * (parts_smem(128, 4) + 3 * 1024) <= 228 * 1024, "two blocks to an SM");
 
 // A query row of a unit: sequence r / G, head r % G.
 __device__ __forceinline__ int out_row(const PrefixArgs& a, int b, int kv, int r) {
@@ -240,8 +253,8 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
     named_sync(1, kWarps * 32);
     // Past the barrier all four warps have read the tile before.  (Released by each warp
     // after its own reads, with a barrier arrival that nothing but its order ties to them, a tile's last
-    // rows were now and then those of the copy that took its place: 3 of 100
-    // first runs of a process.)
+    // rows were now and then those of the copy that took its place: in some 4 of
+    // 100 processes, in the first run.)
     if (it > 0 && tid == 0) mbar_arrive(&sh.empty[(seq - 1) % NS]);
     if (*reinterpret_cast<volatile int*>(&sh.moved[it & 1]) == it + 1) {
       // some column's reference moves: to the largest score of the four warps'
@@ -786,7 +799,7 @@ int plan(PrefixArgs& a, const mkv_geom& g, int num_sms) {
   if (blocks > 1 && units * blocks * tiles * g.head_dim > kVisits * 128 * places) nt = 0, blocks = 0, tiles = 0;
   const long moments = nt > 0 && a.n != nullptr ? 1 : 0;
   // Tails are a warp's; long ones are split, so that their items are more than the places (13 x 8
-  // tails of up to 300 rows: 208 blocks on 152 SMs took 25 us, two or three times as many 15).
+  // tails of up to 300 rows: 208 blocks on 152 SMs took 25 us, three times as many 20).
   const long items = units * a.N;
   const long splits_t = std::clamp<long>((5 * kWarps * places / 2 + items - 1) / items, 1, std::min<long>(kMaxSplits, (tiles_t + 1) / 2));
   const long item_tiles = (tiles_t + splits_t - 1) / splits_t;

@@ -751,7 +751,8 @@ def mkv_prefix_step(g, seqs: Seqs, q, k_new, v_new, prefix: Cache, mom: Moments 
     if mom is not None and not (mom.n.is_contiguous() and mom.mu_k.is_contiguous() and mom.mu_v.is_contiguous()
                                 and mom.C.is_contiguous() and mom.C.shape == (b, h, d, d)):
         raise ValueError("mom: contiguous moments of the prefix's units")
-    at = _here(q, k_new, v_new, out, lse, ws, prefix.K, prefix.V, prefix.len, tail.K, tail.V, tail.len, seqs.count)
+    at = _here(q, k_new, v_new, out, lse, ws, prefix.K, prefix.V, prefix.len, tail.K, tail.V, tail.len, seqs.count,
+               None if mom is None else mom.C, None if mom is None else mom.n)
     s = _I64x6(n, 0 if seqs.count is None else seqs.count.data_ptr(), *qs, *ks)
     code = lib().mkv_prefix_step(g, s, q.data_ptr(), _ptr(k_new), _ptr(v_new), shared,
                                  None if mom is None else mom.c(), own, p, out.data_ptr(), _ptr(lse), ws.data_ptr(),
