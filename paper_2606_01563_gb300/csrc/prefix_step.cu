@@ -97,14 +97,18 @@ struct PartsShared {
 __device__ __forceinline__ bool failed(const PartsShared& sh) { return *reinterpret_cast<const volatile int*>(&sh.fail) != 0; }
 // A warp's wait on a tile (every lane's, and the lanes stay together: what follows
 // is the warp's as one).  One that runs out fails the block, whose later waits then
-// pass at once (barriers are met as ever; what is computed from here on is not used).
-__device__ __forceinline__ void wait_tile(uint64_t* bar, uint32_t parity, PartsShared& sh, uint32_t polls) {
+// end at once.  From there on no tile is asked for: a copy into a place
+// whose last one was not waited for would count against that one's phase, and the
+// block could end with copies in flight.  (The warps of a run meet their barriers
+// as ever; what they compute is not used.)
+__device__ __forceinline__ bool wait_tile(uint64_t* bar, uint32_t parity, PartsShared& sh, uint32_t polls) {
   for (uint32_t i = 0; i < polls; ++i) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
-    if ((i & 63) == 63 && __any_sync(0xffffffffu, failed(sh))) return;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 63) == 63 && __any_sync(0xffffffffu, failed(sh))) return false;
   }
   *reinterpret_cast<volatile int*>(&sh.fail) = 1;
   __syncwarp();
+  return false;
 }
 
 // The loading warp's part of a run of n rows: one thread, tiles seq, seq + 1, ... of the block.
@@ -115,7 +119,8 @@ __device__ __forceinline__ void load_run(const PrefixArgs& a, const CUtensorMap*
   const uint64_t pol = l2_evict_first();
   for (int i = 0; i * kRows < n; ++i) {
     const uint32_t st = seq % NS;
-    if (seq >= NS && (failed(sh) || !mbar_wait(&sh.empty[st], ((seq / NS) - 1) & 1, a.polls))) {
+    // (a place may have been released by warps whose own wait had given up)
+    if (seq >= NS && (!mbar_wait(&sh.empty[st], ((seq / NS) - 1) & 1, a.polls) || failed(sh))) {
       *reinterpret_cast<volatile int*>(&sh.fail) = 1;
       return;
     }
@@ -176,7 +181,7 @@ __device__ __forceinline__ void attend_run(const PrefixArgs& a, int n, int cols,
   const int kr = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kc = (lane >> 4) * 8;
   const int vr = (lane & 7) + (lane >> 4) * 8, vc = warp * (D / 4) + ((lane >> 3) & 1) * 8;
   for (int it = 0; it < tiles; ++it, ++seq) {
-    wait_tile(&sh.full[seq % NS], (seq / NS) & 1, sh, a.polls);
+    (void)wait_tile(&sh.full[seq % NS], (seq / NS) & 1, sh, a.polls);
     const int rows = min(kRows, n - it * kRows);
     const uint8_t* tK = ring + (size_t)(seq % NS) * 2 * kTile;
     uint8_t* tV = ring + (size_t)(seq % NS) * 2 * kTile + kTile;
@@ -499,7 +504,8 @@ __device__ __forceinline__ void tail_warp(const PrefixArgs& a, const CUtensorMap
   const float qscale = rsqrtf(static_cast<float>(D)) * kLog2e, slack = kSlack / qscale;
   uint32_t next[KS][2];
   query(0, next);
-  for (int i = 0; i < mine; ++i) {
+  bool waited = true;
+  for (int i = 0; waited && i < mine; ++i) {
     uint32_t q[KS][2];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) q[kk][0] = next[kk][0], q[kk][1] = next[kk][1];
@@ -508,7 +514,8 @@ __device__ __forceinline__ void tail_warp(const PrefixArgs& a, const CUtensorMap
     if (n < 0) continue;  // (not in use: nothing is joined)
     float most[2] = {kNegInf, kNegInf}, l[2] = {}, lr[2] = {}, o[MT][4] = {};
     for (int r0 = 0; r0 < n; r0 += kKeys, ++seq) {
-      wait_tile(&full[seq % NS], (seq / NS) & 1, sh, a.polls);
+      waited = wait_tile(&full[seq % NS], (seq / NS) & 1, sh, a.polls);
+      if (!waited) break;  // (a state of part of a tail is not used)
       const uint8_t* tK = ring + (seq % NS) * 2 * kTile;
       uint8_t* tV = ring + (seq % NS) * 2 * kTile + kTile;
       const int rows = min(kKeys, n - r0);

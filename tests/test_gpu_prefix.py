@@ -282,3 +282,90 @@ def test_tensors_of_another_device_are_refused():
     c.out = c.out.cpu()
     with pytest.raises(ValueError):
         c.run()
+
+
+# Many query rows over many shared rows, which the kernels of drafted trees take: the same columns as CASES.
+MANY = [
+    (2, 64, 8, 4, 128, 2000, 100, "f32", 1),   # one row block of 256, lengths from 0 on
+    (1, 256, 4, 8, 64, 2000, 3, "bf16", 1),    # the most rows
+    (3, 33, 8, 1, 128, 4900, 40, "split", 1),  # 33 rows
+    (1, 40, 8, 2, 128, 10000, 300, "f32", 0), (60, 9, 8, 4, 128, 500, 70, "f32", 1),
+    (2, 100, 6, 8, 64, 1600, 1, "split", 1), (1, 65, 8, 8, 128, 2000, 0, "none", 1),
+    (140, 5, 8, 8, 128, 200, 2, "f32", 1),     # more units than a list of their runs is made for
+]
+
+
+@pytest.mark.parametrize("b,N,h,g,d,rows,tail,moments,order", MANY)
+@pytest.mark.parametrize("ragged", [True, False])
+def test_step_of_many_rows(b, N, h, g, d, rows, tail, moments, order, ragged):
+    Case(b, N, h, g, d, rows, tail, moments, order, ragged, seed=rows, fused=N % 2 == 0).step_and_check()
+
+
+def test_many_rows_with_nothing_shared():
+    for moments, new in (("none", False), ("f32", True)):
+        c = Case(2, 64, 8, 4, 128, 2000, 9, moments=moments, new=new, seed=30)
+        c.prefix.len.zero_()
+        c.prefix.K.fill_(float("nan"))
+        c.prefix.V.fill_(float("nan"))
+        c.tail.len[::3] = 0
+        if c.mom is not None:
+            c.mom.n[:, ::2] = 0
+        c.step_and_check()
+
+
+def test_many_rows_with_large_scores():
+    Case(1, 64, 8, 8, 128, 2500, 80, seed=31, loud=30.0).step_and_check()
+
+
+def test_many_rows_sizes_out_of_range_are_recorded():
+    for who in ("prefix", "tail", "count"):
+        c = Case(2, 64, 8, 4, 128, 2000, 20, ragged=False, seed=32, new=False)
+        x = c.tail if who == "tail" else c.prefix
+        for y in (x.K, x.V):
+            y[1, 1] = torch.randn(y[1, 1].shape, generator=c.gen, device="cuda")
+        if who != "count":
+            x.len[1, 1], x.len[0, 0] = x.capacity, 0
+        ref = c.reference()
+        if who == "count":
+            c.count[1] = 65
+        else:
+            x.len[1, 1], x.len[0, 0] = 2 ** 31 - 1, -2 ** 31
+        c.run()
+        c.check(ref, error=INVALID if who == "count" else CAPACITY)
+
+
+def test_many_rows_captured_and_between_calls_of_few():
+    """One workspace: a graph of the step of many rows, replayed in turn with eager steps of few."""
+    big = Case(2, 64, 8, 4, 128, 2000, 30, seed=33, room=8)
+    few = Case(2, 3, 8, 4, 128, 300, 30, seed=34, room=8)
+    few.ws = big.ws
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        big.run(stream=side)
+    for _ in range(3):
+        ref, ref_few = big.reference(), few.reference()
+        graph.replay()
+        few.run()
+        big.check(ref)
+        few.check(ref_few)
+
+
+def test_many_rows_give_the_same_bits_again():
+    c = Case(2, 64, 8, 4, 128, 2000, 100, seed=35, new=False)
+    c.run()
+    out, lse = c.out.clone(), c.lse.clone()
+    for _ in range(20):
+        c.run()
+        assert torch.equal(c.out.view(torch.int16), out.view(torch.int16)) and torch.equal(c.lse, lse)
+
+
+def test_many_rows_waits_that_run_out_are_recorded():
+    c = Case(2, 64, 8, 4, 128, 2000, 100, seed=36)
+    old = mkv.mkv_debug_set_poll_limit(0)
+    try:
+        c.run()
+        assert mkv.mkv_get_device_error(c.ws)[0] == TIMEOUT
+    finally:
+        mkv.mkv_debug_set_poll_limit(old)
+    Case(2, 64, 8, 4, 128, 2000, 100, seed=36).step_and_check()
