@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
     const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
     if (top > ref) {
       const float r = ceilf(top);
-      sum = ref == kNegInf ? 0.f : sum * expf(ref - r);
+      if (ref != kNegInf) sum *= expf(ref - r);  // (else it is 0, or NaN for good)
       ref = r;
     }
     {

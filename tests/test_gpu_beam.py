@@ -107,6 +107,17 @@ def test_select_values_that_are_not_finite_are_recorded():
         _check(logits, score, None, 2, 6, error=INVALID)
 
 
+def test_select_a_nan_among_forbidden_tokens_before_the_first_logit():
+    """A run's first 2048 tokens are forbidden but for a NaN, which what comes after must not hide."""
+    for nan in (float("nan"), -float("nan")):
+        logits, score, _ = _inputs(100, 8, 5001, F32, 17)
+        logits[1, 3, :2048] = -float("inf")
+        logits[1, 3, 5] = nan
+        *_, ws = _select(logits, score, None, 2, 6)
+        assert mkv.mkv_get_device_error(ws) == (INVALID, 11)
+        _check(logits, score, None, 2, 6, error=INVALID)
+
+
 def test_select_odd_addresses_strides_and_offsets_past_32_bits():
     gen = torch.Generator(device="cuda")
     gen.manual_seed(3)
