@@ -140,8 +140,12 @@ mkv_status mkv_beam_reorder(mkv_geom geom, int32_t n_seqs, int32_t n_layers, con
   if (!geom_ok(geom)) return geom_status(geom);
   if (n_seqs < 1 || n_seqs > MKV_BEAM_MAX_SEQS || (long)geom.batch * geom.n_kv_heads > 65535) return MKV_ERR_SHAPE;
   if (n_layers < 0 || !layers || !parent || !aligned(parent, 4)) return MKV_ERR_INVALID_ARG;
-  for (int i = 0; i < n_layers; ++i)
+  for (int i = 0; i < n_layers; ++i) {
     if (!cache_ok(&layers[i].cache) || (layers[i].mom.n && !moments_ok(&layers[i].mom))) return MKV_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)  // (a state listed twice would be moved twice, at once)
+      if (layers[k].cache.K == layers[i].cache.K || (layers[i].mom.n && layers[k].mom.n == layers[i].mom.n))
+        return MKV_ERR_INVALID_ARG;
+  }
   if (!workspace || workspace_bytes < kHeaderBytes || !aligned(workspace, 256)) return MKV_ERR_WORKSPACE;
   ReorderArgs a{};
   a.parent = parent;

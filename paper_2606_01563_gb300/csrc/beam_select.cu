@@ -43,7 +43,7 @@ namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;  // of a run's block
 constexpr int kJoinThreads = 512;
-constexpr int kVec = 16;                   // elements of a thread and chunk
+constexpr int kVec = 16;                   // elements of a thread and chunk (32 and six blocks an SM: 51 us for 42.6)
 constexpr int kChunk = kThreads * kVec;    // elements of a chunk
 constexpr int kMaxOut = MKV_BEAM_MAX_OUT;  // 64
 constexpr int kBuffer = kMaxOut * kVec + 2 * kMaxOut;

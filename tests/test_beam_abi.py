@@ -67,6 +67,16 @@ def test_reorder_refusals(L):
     assert call(layers=0) == OK  # nothing to launch
 
 
+def test_reorder_refuses_a_state_twice(L):
+    def layer(at, mom=None):
+        return mkv.mkv_beam_layer(mkv.mkv_cache(at, at, FAKE, FAKE, FAKE, 64),
+                                  mkv.mkv_moments() if mom is None else mkv.mkv_moments(mom, FAKE, FAKE, FAKE))
+    far = FAKE + (1 << 20)
+    for pair in ((layer(FAKE), layer(FAKE)), (layer(FAKE, FAKE), layer(far, FAKE))):
+        arr = (mkv.mkv_beam_layer * 2)(*pair)
+        assert L.mkv_beam_reorder(mkv.geom(2, 3, 1, 128), 4, 2, arr, FAKE, FAKE, 256, None) == INVALID
+
+
 def test_select_binding_refusals():
     b, k, v = 2, 3, 50
     good = dict(logits=torch.zeros(b, k, v), score=torch.zeros(b, k), parent=torch.zeros(b, 4, dtype=torch.int32),
