@@ -234,10 +234,13 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
     uint64_t bound = sh.bound;
     const float least = key_logit(bound);
     const bool any = bound == 1 ? top > kNegInf : top >= least;
+    // (read before the barrier: behind it other warps may already be adding keys,
+    // and all threads must take the same side, which has barriers of its own)
+    const int fill = sh.fill;
     const int wanted = __syncthreads_count(any);
     if (wanted == 0) continue;
-    if (sh.fill + wanted * kVec > kBuffer) {
-      if (sh.fill > a.out) keep_best(sh, a.out);
+    if (fill + wanted * kVec > kBuffer) {
+      if (fill > a.out) keep_best(sh, a.out);
       uint64_t best = 0;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {

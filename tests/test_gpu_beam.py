@@ -79,6 +79,43 @@ def test_select_orders_that_fill_lists(v, out, order):
     _check(x.to(BF16), torch.full((1, 2), -1.5, device="cuda"), None, 7, out)
 
 
+@pytest.mark.parametrize("dtype,sizes", [(BF16, range(521, 577, 5)), (F32, range(257, 289, 3))])
+def test_select_vocabularies_of_one_chunk_in_part_of_a_block(dtype, sizes):
+    """One vector of 16 bytes in each of 65 to 72 threads: what they add decides whether it had fitted."""
+    for v in sizes:
+        logits, score, _ = _inputs(1, 2, v, dtype, v, padded=-v % 8)
+        _check(logits, score, None, 2, 64)
+
+
+@pytest.mark.parametrize("threads", range(64, 74))
+def test_select_masks_that_leave_some_threads_a_token(threads):
+    """A chunk in which as many threads have one permitted token, of several chunks."""
+    v = 3 * 2048 + 1000
+    logits, score, _ = _inputs(1, 2, v, BF16, threads, padded=8 - v % 8)
+    at = torch.arange(threads, device="cuda") * 8
+    mask = torch.full((v,), -float("inf"), device="cuda")
+    for chunk in range(3):
+        mask[chunk * 2048 + at + chunk] = 0
+    _check(logits + mask.to(BF16), score, None, -1, 64)
+
+
+@pytest.mark.parametrize("out", [48, 56, 64])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_many_blocks_with_long_lists(out, dtype):
+    """48 batch items with the same logits and scores: the same bits of each, on every call.  Against one item's call
+    the scores are within twice the bound (that call cuts its runs elsewhere, so its sums round differently)."""
+    logits, score, _ = _inputs(1, 8, 20000, dtype, out)
+    p, t, s = _check(logits, score, None, 2, out)
+    first = None
+    for _ in range(20):
+        got = _select(logits.expand(48, -1, -1), score.expand(48, -1).contiguous(), None, 2, out)
+        assert (got[0] == p).all() and (got[1] == t).all()
+        assert ((got[2] - s).abs() <= 2 * (5e-7 + 2.0 ** -24 * s.abs())).all()
+        first = got[2][:1] if first is None else first
+        assert (got[2] == first).all()
+        assert mkv.mkv_get_device_error(got[4])[0] == 0
+
+
 def test_select_first_step_and_masks():
     """Beams that are not alive, tokens that are forbidden, and items with fewer continuations than slots."""
     logits, score, _ = _inputs(4, 4, 300, F32, 11)
