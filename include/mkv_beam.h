@@ -129,8 +129,9 @@ MKV_API size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int3
  * token -1, score -infinity and done 0.  A live beam with a logit that is NaN
  * or +infinity, or a score that is, takes no part and is recorded as
  * MKV_ERR_INVALID_ARG (info: batch item * beams + beam).
- * Sums of exponentials, their logs and the scores are joined in fp64; a term's error of about 1e-7
- * decides between continuations that are nearer to each other than that.
+ * Exponentials, and sums of 16 of them, are fp32; their sums are kept in pairs of fp32 values, logs and
+ * scores in fp64.  An error of a few 1e-7, whatever the vocabulary, decides between continuations of
+ * different beams that are nearer to each other than that.
  * score_out may be score, and done_out may be done, where n_out = beams; else
  * outputs do not overlap inputs.
  * Requirements: batch 1..65535, beams 1..64, n_out 1..64, vocab 1..2^24; logits aligned to their

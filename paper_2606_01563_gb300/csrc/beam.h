@@ -77,7 +77,7 @@ struct SelectArgs {
   int32_t* done_out;  // or null
   void* ws;
   // carved from the workspace by select_plan
-  float4* stats;   // [b * beams][splits]: reference, sum, candidates (int), unused
+  float4* stats;   // [b * beams][splits]: reference, sum and what its rounding lost, candidates (int; -1: a value that is not finite)
   uint64_t* keys;  // [b * beams][splits][out], best first
   int32_t splits;
   int32_t per;  // elements of a split

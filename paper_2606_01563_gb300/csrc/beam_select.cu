@@ -20,11 +20,12 @@
 // is full its last key is the bound for what follows, which nearly nothing
 // passes.
 //
-// Rounding.  Terms and sums are fp32 about a reference that is a whole number at or
+// Rounding.  Terms, and the sum of 16 of them, are fp32 about a reference that is a whole number at or
 // above the largest logit (a term of weight has a small exponent, and sums about different references
-// join by factors that depend on whole numbers alone), the log of the joined sum
-// and the scores fp64: which of two continuations is better is decided to a few
-// 1e-7, and the scores that come back are rounded once.
+// join by factors that depend on whole numbers alone).  From there on sums are pairs of fp32
+// values: a thread may add 4096 such sums, whose roundings in one value came to 2e-5.
+// The log of the joined sum and the scores are fp64: which of two continuations is
+// better is decided to a few 1e-7 whatever the vocabulary, and the scores that come back are rounded once.
 //
 // Each logit is read once; what bounds it over many beams is issue, 18
 // instructions a logit and a barrier a chunk (32 x 8 beams of 150001 bf16 logits: 43-46 us,
@@ -62,6 +63,33 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 __device__ __forceinline__ uint32_t key_token(uint64_t k) { return ~static_cast<uint32_t>(k); }
 
+// A sum that is kept to more than 32 bits: hi, with what its roundings lost in lo.
+// (fp64 units are few: a warp's addition holds them for 16 cycles.)
+struct Sum {
+  float hi, lo;
+};
+__device__ __forceinline__ Sum add(const Sum& a, const Sum& b) {
+  const float s = a.hi + b.hi, t = s - a.hi;
+  return Sum{s, ((a.hi - (s - t)) + (b.hi - t)) + (a.lo + b.lo)};
+}
+// a += x, four operations: exact where a is the larger.  Where x is, the sum at least
+// doubles, so that what such steps lose is at most 2^-23 of the result, however many there are.
+__device__ __forceinline__ void add_to(Sum& a, float x) {
+  const float y = x + a.lo, s = a.hi + y;
+  a.lo = y - (s - a.hi);
+  a.hi = s;
+}
+__device__ __forceinline__ Sum scaled(const Sum& a, float f) {
+  const float hi = a.hi * f;
+  return Sum{hi, fmaf(a.hi, f, -hi) + a.lo * f};
+}
+// The sum of a warp's first `lanes` lanes (those after them hold 0), in each of them.
+__device__ __forceinline__ Sum lanes_sum(Sum s, int lanes) {
+  for (int o = 1; o < lanes; o <<= 1)
+    s = add(s, Sum{__shfl_xor_sync(0xffffffffu, s.hi, o), __shfl_xor_sync(0xffffffffu, s.lo, o)});
+  return s;
+}
+
 struct RowShared {
   uint64_t keys[kBuffer];
   uint64_t best[kMaxOut];
@@ -69,7 +97,7 @@ struct RowShared {
   uint64_t bound;  // the least key that is still wanted
   int fill;
   float ref[kWarps];
-  float sum[kWarps];
+  Sum sum[kWarps];
 };
 
 // The buffer's best `out` keys (all, if there are fewer) in order, at its start.
@@ -196,11 +224,12 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
   float4* stat = a.stats + (size_t)row * a.splits + split;
   if (split == 0 && tid == 0 && !(score < INFINITY)) record_error(a.ws, MKV_ERR_INVALID_ARG, row);
   if (!(score > kNegInf && score < INFINITY) || (a.done != nullptr && a.done[row] != 0)) {
-    if (tid == 0) *stat = make_float4(kNegInf, 0.f, __int_as_float(0), 0.f);
+    if (tid == 0) *stat = make_float4(kNegInf, 0.f, 0.f, __int_as_float(0));
     return;
   }
   if (tid == 0) sh.fill = 0, sh.bound = 1;
-  float ref = kNegInf, sum = 0.f;
+  float ref = kNegInf;
+  Sum sum{0.f, 0.f};
   __syncthreads();
   for (int first = lo; first < end; first += kChunk) {
     float x[kVec];
@@ -212,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
     const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
     if (top > ref) {
       const float r = ceilf(top);
-      if (ref != kNegInf) sum *= expf(ref - r);  // (else it is 0, or NaN for good)
+      if (ref != kNegInf) sum = scaled(sum, expf(ref - r));  // (else it is 0, or NaN for good)
       ref = r;
     }
     {
@@ -228,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
       }
       float s0, s1;
       unpack2(sums, s0, s1);
-      sum += s0 + s1;
+      add_to(sum, s0 + s1);
     }
     // what is still wanted of the chunk
     uint64_t bound = sh.bound;
@@ -274,8 +303,8 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
   }
   // the sums of the warps, then of the block
   float r = warp_max(ref);
-  bool odd = !(sum < INFINITY);
-  sum = warp_sum(ref == kNegInf ? 0.f : sum * expf(ref - r));
+  bool odd = !(sum.hi < INFINITY);
+  sum = lanes_sum(ref == kNegInf ? Sum{0.f, 0.f} : scaled(sum, expf(ref - r)), 32);
   if (lane == 0) sh.ref[tid >> 5] = r, sh.sum[tid >> 5] = sum;
   odd = __syncthreads_or(odd);
   keep_best(sh, a.out);
@@ -283,11 +312,10 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const __grid_consta
   if (tid < n) a.keys[((size_t)row * a.splits + split) * a.out + tid] = sh.keys[tid];
   if (tid < 32) {
     r = tid < kWarps ? sh.ref[tid] : kNegInf;
-    sum = tid < kWarps ? sh.sum[tid] : 0.f;
     const float m = warp_max(r);
-    sum = warp_sum(r == kNegInf ? 0.f : sum * expf(r - m));
+    sum = lanes_sum(r == kNegInf ? Sum{0.f, 0.f} : scaled(sh.sum[tid], expf(r - m)), kWarps);  // (lanes past the warps have no reference)
     if (tid == 0) {
-      *stat = make_float4(m, sum, __int_as_float(n), odd ? 1.f : 0.f);
+      *stat = make_float4(m, sum.hi, sum.lo, __int_as_float(odd ? -1 : n));
       if (odd) record_error(a.ws, MKV_ERR_INVALID_ARG, row);
     }
   }
@@ -324,6 +352,7 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
   __shared__ double offset[MKV_BEAM_MAX_BEAMS];  // its score less the log of its sum about that
   __shared__ int count[kMaxLists], over[MKV_BEAM_MAX_BEAMS], fill;
   __shared__ float scores[MKV_BEAM_MAX_BEAMS];
+  __shared__ Sum sums[MKV_BEAM_MAX_BEAMS];
   grid_dependency_wait();
   grid_launch_dependents();
   const int item = blockIdx.x, tid = threadIdx.x, lists = a.beams * a.splits;
@@ -334,38 +363,42 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
     const float score = a.score[row];
     const bool ended = a.done != nullptr && a.done[row] != 0;
     float4 st[kMaxLists / 32];
-    float m = kNegInf, sum = 0.f;
+    float m = kNegInf;
+    Sum sum{0.f, 0.f};
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < kMaxLists / 32; ++i) {
       const int s = i * 32 + lane;
       st[i] = s < a.splits ? a.stats[(size_t)row * a.splits + s] : make_float4(kNegInf, 0.f, 0.f, 0.f);
       m = fmaxf(m, st[i].x);
-      odd |= st[i].w != 0.f;
+      odd |= __float_as_int(st[i].w) < 0;
     }
     m = warp_max(m);
     odd = __any_sync(0xffffffffu, odd);
 #pragma unroll
     for (int i = 0; i < kMaxLists / 32; ++i)
-      if (st[i].x > kNegInf) sum += st[i].y * expf(st[i].x - m);
-    sum = warp_sum(sum);
-    const bool ok = !ended && !odd && sum > 0.f;
+      if (st[i].x > kNegInf) sum = add(sum, scaled(Sum{st[i].y, st[i].z}, expf(st[i].x - m)));
+    sum = lanes_sum(sum, min(a.splits, 32));
+    const bool ok = !ended && !odd && sum.hi > 0.f;
 #pragma unroll
     for (int i = 0; i < kMaxLists / 32; ++i) {
       const int s = i * 32 + lane;
       // an ended beam's one continuation is its first list's
       if (s < a.splits)
         count[b * a.splits + s] = ended ? (s == 0 && score > kNegInf && score < INFINITY && a.end >= 0 ? 1 : 0)
-                                  : ok  ? __float_as_int(st[i].z)
+                                  : ok  ? __float_as_int(st[i].w)
                                         : 0;
     }
     if (lane == 0) {
       scores[b] = score;
       over[b] = ended;
       refs[b] = m;
-      offset[b] = ok ? static_cast<double>(score) - log(static_cast<double>(sum)) : 0;
+      sums[b] = ok ? sum : Sum{1.f, 0.f};
     }
   }
+  __syncthreads();
+  // (all beams' at once: a warp's fp64 instruction takes as long for one lane as for 32)
+  if (tid < a.beams) offset[tid] = static_cast<double>(scores[tid]) - log(static_cast<double>(sums[tid].hi) + sums[tid].lo);
   __syncthreads();
   auto get = [&](int list, int i) {
     const int b = list / a.splits;

@@ -172,6 +172,32 @@ def test_select_odd_addresses_strides_and_offsets_past_32_bits():
     _check(view, -torch.rand(2, 2, generator=gen, device="cuda"), None, 2, 7)
 
 
+@pytest.mark.parametrize("beams", [64, 1])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["equal", "random"])
+def test_select_sums_over_the_largest_vocabulary(kind, dtype, beams):
+    """2^24 tokens: with 64 beams (of the same logits) a thread has 4096 chunks of 16 of them.  Equal logits are the case in
+    which the roundings of one running sum in 32 bits add up.
+
+    A term's exponential is off by 2^-22 at most and its exponent by two roundings (2^-23 of at most 8 where it has
+    weight: 5e-7 at the least weights, less elsewhere), the 16 terms' sum by seven additions (7 2^-24); nothing else is in 32 bits: 1e-6 in all."""
+    v, out = 1 << 24, 6
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(v + beams)
+    row = torch.full((v,), -0.3, device="cuda") if kind == "equal" else torch.randn(v, generator=gen, device="cuda")
+    row = row.to(dtype)
+    score = 16.6 - 50 * torch.arange(beams, device="cuda", dtype=F32)[None]  # (the first beam's are the best, near 0)
+    parent, token, best, _, ws = _select(row.view(1, 1, v).expand(1, beams, -1), score, None, -1, out)
+    x = host(row).astype(np.float64)
+    log = float(x.max()) + np.log(np.exp(x - x.max()).sum())
+    at = np.flatnonzero(x >= np.partition(x, -out)[-out])
+    at = at[np.lexsort((at, -x[at]))][:out]
+    want = host(score)[0, 0].astype(np.float64) + (x[at] - log)
+    assert (host(parent) == 0).all() and (host(token)[0] == at).all()
+    assert (np.abs(host(best)[0] - want) <= 1e-6 + 2.0 ** -24 * np.abs(want)).all(), np.abs(host(best)[0] - want).max()
+    assert mkv.mkv_get_device_error(ws)[0] == 0
+
+
 def test_select_in_place_in_a_graph_on_another_stream():
     b, k, v = 3, 6, 4000
     logits, score, gen = _inputs(b, k, v, BF16, 21)
