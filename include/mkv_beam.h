@@ -156,7 +156,7 @@ typedef struct {
  * number of batch items b; geom's group is not used.
  *   n_seqs  N: slots per batch item, 1..256
  *   parent  int32 [b, N]  0..N-1, several slots may have the same; -1: the slot stays as it is
- *   layers  HOST array of n_layers entries, copied during the call; no cache or moments twice (MKV_ERR_INVALID_ARG)
+ *   layers  HOST array of n_layers entries, copied during the call; no array of a cache or of moments in two of them (MKV_ERR_INVALID_ARG)
  * A batch item with another parent is left as it is and recorded as
  * MKV_ERR_INVALID_ARG (info: the batch item); a length outside 0..capacity is
  * recorded as MKV_ERR_CAPACITY and rows are copied up to the nearer end.

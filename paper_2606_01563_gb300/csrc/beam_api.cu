@@ -26,6 +26,19 @@ bool select_sizes_ok(int32_t batch, int32_t beams, int32_t vocab, int32_t n_out)
          vocab <= (1 << 24) && n_out >= 1 && n_out <= MKV_BEAM_MAX_OUT;
 }
 
+// Whether an array of one layer is an array of the other: it would be moved twice, at once.
+// (Absent ones are null in both; keys and values, and the two means, may also be each other's.)
+bool share_an_array(const mkv_beam_layer& x, const mkv_beam_layer& y) {
+  const mkv_cache &a = x.cache, &b = y.cache;
+  const mkv_moments &m = x.mom, &n = y.mom;
+  const bool rows = (a.K == b.K) | (a.V == b.V) | (a.K == b.V) | (a.V == b.K) | (a.pos == b.pos) | (a.len == b.len) |
+                    (a.seen == b.seen);
+  const bool state = a.y && ((a.y == b.y) | (a.y_len == b.y_len));
+  const bool moments = m.n && n.n && ((m.n == n.n) | (m.mu_k == n.mu_k) | (m.mu_v == n.mu_v) | (m.mu_k == n.mu_v) |
+                                      (m.mu_v == n.mu_k) | (m.C == n.C));
+  return rows | state | moments;
+}
+
 }  // namespace
 
 extern "C" {
@@ -142,9 +155,8 @@ mkv_status mkv_beam_reorder(mkv_geom geom, int32_t n_seqs, int32_t n_layers, con
   if (n_layers < 0 || !layers || !parent || !aligned(parent, 4)) return MKV_ERR_INVALID_ARG;
   for (int i = 0; i < n_layers; ++i) {
     if (!cache_ok(&layers[i].cache) || (layers[i].mom.n && !moments_ok(&layers[i].mom))) return MKV_ERR_INVALID_ARG;
-    for (int k = 0; k < i; ++k)  // (a state listed twice would be moved twice, at once)
-      if (layers[k].cache.K == layers[i].cache.K || (layers[i].mom.n && layers[k].mom.n == layers[i].mom.n))
-        return MKV_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)
+      if (share_an_array(layers[k], layers[i])) return MKV_ERR_INVALID_ARG;
   }
   if (!workspace || workspace_bytes < kHeaderBytes || !aligned(workspace, 256)) return MKV_ERR_WORKSPACE;
   ReorderArgs a{};

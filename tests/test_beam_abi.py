@@ -77,6 +77,27 @@ def test_reorder_refuses_a_state_twice(L):
         assert L.mkv_beam_reorder(mkv.geom(2, 3, 1, 128), 4, 2, arr, FAKE, FAKE, 256, None) == INVALID
 
 
+def test_reorder_refuses_any_array_in_two_layers(L):
+    """Layers whose arrays are all their own, but one: as much a move at once as a whole cache twice."""
+    cache = ("K", "V", "pos", "len", "seen", "y", "y_len")
+    names = cache + ("n", "mu_k", "mu_v", "C")
+
+    def call(take=None, give=None, have=names, layers=3):
+        at = [{x: (1 + i * len(names) + names.index(x)) << 20 if x in have else None for x in names} for i in range(layers)]
+        if take is not None:
+            at[-1][take] = at[0][give or take]
+        arr = (mkv.mkv_beam_layer * layers)(*(mkv.mkv_beam_layer(
+            mkv.mkv_cache(a["K"], a["V"], a["pos"], a["len"], a["seen"], 64, a["y"], a["y_len"]),
+            mkv.mkv_moments(a["n"], a["mu_k"], a["mu_v"], a["C"])) for a in at))
+        return L.mkv_beam_reorder(mkv.geom(2, 3, 1, 128), 4, layers, arr, FAKE, None, 256, None)  # (no workspace: not launched)
+    for have in (names, cache, cache[:5], cache[:5] + names[7:]):
+        assert call(have=have) == WORKSPACE and call(have=have, layers=70) == WORKSPACE
+        for name in have:
+            assert call(name, have=have) == INVALID and call(name, have=have, layers=70) == INVALID, name
+    for take, give in (("K", "V"), ("V", "K"), ("mu_k", "mu_v"), ("mu_v", "mu_k")):
+        assert call(take, give) == INVALID
+
+
 def test_select_binding_refusals():
     b, k, v = 2, 3, 50
     good = dict(logits=torch.zeros(b, k, v), score=torch.zeros(b, k), parent=torch.zeros(b, 4, dtype=torch.int32),
