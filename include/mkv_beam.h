@@ -158,8 +158,8 @@ typedef struct {
  *   parent  int32 [b, N]  0..N-1, several slots may have the same; -1: the slot stays as it is
  *   layers  HOST array of n_layers entries, copied during the call; no array of a cache or of moments in two of them (MKV_ERR_INVALID_ARG)
  * A batch item with another parent is left as it is and recorded as
- * MKV_ERR_INVALID_ARG (info: the batch item); a length outside 0..capacity is
- * recorded as MKV_ERR_CAPACITY and rows are copied up to the nearer end.
+ * MKV_ERR_INVALID_ARG (info: the batch item); a length (len or y_len) outside 0..capacity is
+ * recorded as MKV_ERR_CAPACITY (info: the unit) and rows are copied up to the nearer end.
  * Requirements: b * h_kv <= 65535 (else MKV_ERR_SHAPE); as mkv_cache and mkv_moments.
  * The workspace is 256 bytes, zero-filled before its first use.  Two launches for every 64 layers.
  */

@@ -61,7 +61,8 @@ __device__ __forceinline__ bool read_slots(const ReorderArgs& a, const ReorderLa
     if (p < -1 || p >= a.N) s.bad = 1;
     s.parent[j] = p == j ? -1 : p;
     const int len = l.len[unit], y = l.y_len != nullptr ? l.y_len[unit] : 0;
-    if (first && static_cast<uint32_t>(len) > static_cast<uint32_t>(l.cap)) record_error(a.ws, MKV_ERR_CAPACITY, unit);
+    if (first && max(static_cast<uint32_t>(len), static_cast<uint32_t>(y)) > static_cast<uint32_t>(l.cap))
+      record_error(a.ws, MKV_ERR_CAPACITY, unit);
     s.length[j] = min(max(len, 0), l.cap);
     s.y_len[j] = min(max(y, 0), l.cap);
   }

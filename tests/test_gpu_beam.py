@@ -295,6 +295,16 @@ def test_reorder_refuses_items_with_bad_parents_and_records_lengths():
     assert _reorder_and_check(states, parent, 2, 64, error=CAPACITY) == 8
 
 
+def test_reorder_records_lengths_of_y():
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    parent = torch.tensor([[1, 0, 2, 3]] * 3, dtype=I32, device="cuda")
+    for slot, bad in ((5, 21), (4, -1), (5, 2 ** 31 - 1), (7, -2 ** 31)):  # (slot 7's state stays)
+        states = [_layer(gen, 12, 2, 20, 64, 1, 0) for _ in range(2)]
+        states[1][0].y_len[slot, 1] = bad
+        assert _reorder_and_check(states, parent, 2, 64, error=CAPACITY) == 2 * slot + 1
+
+
 def test_reorder_in_a_graph_after_a_selection():
     """Selection and reordering captured together on another stream; each replay permutes what the last one left."""
     b, k, v, h, cap, d = 2, 4, 500, 2, 40, 128
