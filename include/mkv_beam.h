@@ -126,9 +126,9 @@ MKV_API size_t mkv_beam_select_workspace_size(int32_t batch, int32_t beams, int3
  *   done_out   int32 [batch, n_out]  optional: 1 where the beam had ended or the token is end_token
  * Tokens with a logit of -infinity, and beams whose logits all are, do not take
  * part.  Where there are fewer continuations than n_out, the slots that are left have parent and
- * token -1, score -infinity and done 0.  A live beam with a logit that is NaN
- * or +infinity, or a score that is, takes no part and is recorded as
- * MKV_ERR_INVALID_ARG (info: batch item * beams + beam).
+ * token -1, score -infinity and done 0.  A live beam that has not ended with a logit
+ * that is NaN or +infinity, and any beam with a score that is, take no part and are
+ * recorded as MKV_ERR_INVALID_ARG (info: batch item * beams + beam).
  * Exponentials, and sums of 16 of them, are fp32; their sums are kept in pairs of fp32 values, logs and
  * scores in fp64.  An error of a few 1e-7, whatever the vocabulary, decides between continuations of
  * different beams that are nearer to each other than that.

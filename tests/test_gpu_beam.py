@@ -144,6 +144,18 @@ def test_select_values_that_are_not_finite_are_recorded():
         _check(logits, score, None, 2, 6, error=INVALID)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_select_a_score_that_is_not_finite_of_a_beam_that_has_ended(bad):
+    logits, score, _ = _inputs(2, 3, 900, BF16, 7)
+    logits[1, 1] = float("nan")  # (an ended beam's logits do not matter)
+    done = torch.tensor([[0, 0, 0], [0, 1, 1]], dtype=I32, device="cuda")
+    _check(logits, score, done, 2, 6)
+    score[1, 2] = bad
+    *_, ws = _select(logits, score, done, 2, 6)
+    assert mkv.mkv_get_device_error(ws) == (INVALID, 5)
+    _check(logits, score, done, 2, 6, error=INVALID)
+
+
 def test_select_a_nan_among_forbidden_tokens_before_the_first_logit():
     """A run's first 2048 tokens are forbidden but for a NaN, which what comes after must not hide."""
     for nan in (float("nan"), -float("nan")):
