@@ -204,7 +204,7 @@ typedef struct {
  * Everything is fp32 between x and the one rounding to bf16; sums of squares
  * that pass fp32's range are taken of smaller values, so that any finite x has
  * its norm.  Arguments, layouts and requirements as in mkv_rope, with
- * p->inverse 0 and eps above 0 and finite.
+ * p->inverse 0 and eps a normal number above 0 (2^-126 or more: below fp32's range squares lose their digits).
  */
 MKV_API mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
                                  int64_t pos_batch, const mkv_rope_params* p, float eps, int32_t n_tensors,

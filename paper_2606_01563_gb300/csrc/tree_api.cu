@@ -1,5 +1,6 @@
 // C-ABI entry points declared in include/mkv_tree.h: argument validation,
 // workspace sizing and kernel dispatch.
+#include <cfloat>
 #include <cmath>
 
 #include "common.cuh"
@@ -72,6 +73,8 @@ bool rope_strides_ok(const void* at, int32_t batch, int32_t tokens, int32_t head
     if (s % 8 != 0 || s < 0) return false;
   return !written || ((batch == 1 || s_batch != 0) && (tokens == 1 || s_token != 0) && (heads == 1 || s_head != 0));
 }
+// At or above the least normal number: what sums of squares lose below fp32's range is less than its rounding.
+bool norm_eps_ok(float eps) { return eps >= FLT_MIN && eps <= FLT_MAX; }
 bool norm_weight_ok(const void* weight, int64_t head, int32_t f32, int32_t head_dim, NormWeight* w) {
   *w = NormWeight{weight, head, f32};
   return (f32 == 0 || f32 == 1) && aligned(weight, 16) &&
@@ -233,7 +236,7 @@ mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const 
   NvtxRange nvtx("mkv_norm_rope");
   mkv_status chk = rope_sizes(batch, tokens, head_dim, n_tensors);
   if (chk != MKV_OK) return chk;
-  if (!tensors || !(eps > 0.f) || !std::isfinite(eps)) return MKV_ERR_INVALID_ARG;
+  if (!tensors || !norm_eps_ok(eps)) return MKV_ERR_INVALID_ARG;
   NormRopeArgs a{};
   chk = rope_fill(a, batch, tokens, head_dim, pos, pos_axis, pos_batch, p);
   if (chk != MKV_OK) return chk;
@@ -287,7 +290,7 @@ mkv_status mkv_norm_rope_grad(int32_t batch, int32_t tokens, int32_t head_dim, c
   NvtxRange nvtx("mkv_norm_rope_grad");
   mkv_status chk = rope_sizes(batch, tokens, head_dim, n_tensors);
   if (chk != MKV_OK) return chk;
-  if (!tensors || !(eps > 0.f) || !std::isfinite(eps)) return MKV_ERR_INVALID_ARG;
+  if (!tensors || !norm_eps_ok(eps)) return MKV_ERR_INVALID_ARG;
   NormRopeGradArgs a{};
   chk = rope_fill(a, batch, tokens, head_dim, pos, pos_axis, pos_batch, p);
   if (chk != MKV_OK) return chk;

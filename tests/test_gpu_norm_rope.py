@@ -137,6 +137,27 @@ def test_rows_of_zeros_of_huge_values_and_not_finite(d):
     assert torch.equal(y2[0][~odd], y[0][~odd]) and not torch.isfinite(y2[0][odd]).any(-1).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_least_eps_and_rows_whose_squares_leave_the_range(d):
+    """eps 2^-126, rows from 1e-17 down to bf16's least values: sums of squares from 1e-34 to nothing, which is 2^-24 of eps."""
+    b, t, h, eps = 1, 40, 2, 2.0 ** -126
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(d + 1)
+    pos, p, plain = _rot(np.random.default_rng(d), b, t, d // 4, 1, True)
+    size = 10.0 ** -torch.linspace(17, 40, t, device="cuda", dtype=torch.float64)
+    x = (torch.randn(b, t, h, d, generator=gen, device="cuda").double() * size[:, None, None]).to(BF16)
+    dy = torch.randn(b, t, h, d, generator=gen, device="cuda").to(BF16)
+    w = torch.randn(d, generator=gen, device="cuda")
+    y, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(d, device="cuda")
+    call = [(x, dy, dx, w, dw)]
+    mkv.mkv_norm_rope(pos, p, [(x, y, w)], eps)
+    mkv.mkv_norm_rope_grad(pos, p, call, eps, mkv.alloc_workspace(mkv.mkv_norm_rope_grad_workspace_size(call)))
+    _close(y, *R.forward(host(x), host(w), eps, *plain))
+    ref = R.backward(host(x), host(dy), host(w), eps, *plain)
+    _close(dx, ref[0], ref[1])
+    _close(dw, ref[2], ref[3])
+
+
 def test_no_tokens():
     p, pos = mkv.rope_params([1.0] * 32), torch.zeros(1, 2, 0, dtype=torch.int32, device="cuda")
     x, w, dw = torch.zeros(2, 0, 3, 64, dtype=BF16, device="cuda"), torch.ones(3, 64, device="cuda"), torch.full((3, 64), 9.0, device="cuda")

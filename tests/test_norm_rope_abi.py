@@ -86,6 +86,15 @@ def test_gradient_refusals(L):
     assert call(t=0, dw=None, ws=None, pos=None) == OK
 
 
+def test_an_eps_too_small_for_sums_of_squares_is_refused(L):
+    """Below the least normal number squares that leave fp32's range would matter beside it."""
+    fwd = (mkv.mkv_norm_rope_tensor * 1)(mkv.mkv_norm_rope_tensor(mkv.mkv_rope_tensor(FAKE, FAKE, 2, 0, 256, 128, 0, 256, 128), FAKE, 0, 0))
+    bwd = (mkv.mkv_norm_rope_grad_tensor * 1)(mkv.mkv_norm_rope_grad_tensor(FAKE, FAKE, FAKE, 2, *(0, 256, 128) * 3, FAKE, 0, 0, None))
+    for eps, tokens, want in ((2.0 ** -126, 0, OK), (2.0 ** -126 - 2.0 ** -149, 4, INVALID), (1e-40, 4, INVALID), (2.0 ** -149, 4, INVALID)):
+        assert L.mkv_norm_rope(1, tokens, 128, FAKE, 0, 0, _params(), eps, 1, fwd, None) == want
+        assert L.mkv_norm_rope_grad(1, tokens, 128, FAKE, 0, 0, _params(), eps, 1, bwd, FAKE, 1 << 40, None) == want
+
+
 def test_binding_refusals():
     pos, p = torch.zeros(1, 1, 4, dtype=torch.int32), _params(64)
     x = torch.zeros(1, 4, 2, 64, dtype=torch.bfloat16)
