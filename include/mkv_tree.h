@@ -204,14 +204,16 @@ typedef struct {
  * Everything is fp32 between x and the one rounding to bf16; sums of squares
  * that pass fp32's range are taken of smaller values, so that any finite x has
  * its norm.  Arguments, layouts and requirements as in mkv_rope, with
- * p->inverse 0 and eps a normal number above 0 (2^-126 or more: below fp32's range squares lose their digits).
+ * p->inverse 0, no two tensors with one out, and eps a normal number above 0
+ * (2^-126 or more: below fp32's range squares lose their digits).
  */
 MKV_API mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const int32_t* pos, int64_t pos_axis,
                                  int64_t pos_batch, const mkv_rope_params* p, float eps, int32_t n_tensors,
                                  const mkv_norm_rope_tensor* tensors, void* stream);
 
 /* A tensor of mkv_norm_rope_grad: bf16 [b, tokens, heads, d] each with the strides given.  dx may be x or dy
- * with the same strides (in place); else it must not overlap them. */
+ * with the same strides (in place); else it must not overlap them.  No two tensors have one dx or dweight
+ * (the gradient of weights that tensors share is the sum of theirs, the caller's to add). */
 typedef struct {
   const void* x;        /* what mkv_norm_rope read                                            */
   const void* dy;       /* the gradient of what it wrote                                     */

@@ -73,6 +73,11 @@ bool rope_strides_ok(const void* at, int32_t batch, int32_t tokens, int32_t head
     if (s % 8 != 0 || s < 0) return false;
   return !written || ((batch == 1 || s_batch != 0) && (tokens == 1 || s_token != 0) && (heads == 1 || s_head != 0));
 }
+// A tensor that is written where one is read is read with the same strides (those over extents of one are not used).
+bool in_place_ok(const void* in, const void* out, int32_t batch, int32_t tokens, int32_t heads, const int64_t (&a)[3],
+                 const int64_t (&b)[3]) {
+  return in != out || ((batch == 1 || a[0] == b[0]) && (tokens == 1 || a[1] == b[1]) && (heads == 1 || a[2] == b[2]));
+}
 // At or above the least normal number: what sums of squares lose below fp32's range is less than its rounding.
 bool norm_eps_ok(float eps) { return eps >= FLT_MIN && eps <= FLT_MAX; }
 bool norm_weight_ok(const void* weight, int64_t head, int32_t f32, int32_t head_dim, NormWeight* w) {
@@ -254,6 +259,14 @@ mkv_status mkv_norm_rope(int32_t batch, int32_t tokens, int32_t head_dim, const 
                         t.out_batch, t.out_token, t.out_head, t.heads};
   }
   if (heads > 65536) return MKV_ERR_SHAPE;
+  for (int i = 0; i < n_tensors; ++i) {
+    const mkv_rope_tensor& t = tensors[i].t;
+    if (!in_place_ok(t.in, t.out, batch, tokens, t.heads, {t.in_batch, t.in_token, t.in_head},
+                     {t.out_batch, t.out_token, t.out_head}))
+      return MKV_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)
+      if (t.out == tensors[k].t.out) return MKV_ERR_INVALID_ARG;
+  }
   a.heads = static_cast<int32_t>(heads);
   a.eps = eps;
   return cuda_status(launch_norm_rope(a, head_dim, num_sms_current(), static_cast<cudaStream_t>(stream)));
@@ -318,6 +331,18 @@ mkv_status mkv_norm_rope_grad(int32_t batch, int32_t tokens, int32_t head_dim, c
   }
   const int blocks = norm_rope_grad_blocks(a, batch, tokens, head_dim, n_tensors, tensors);
   if (blocks == 0) return MKV_ERR_SHAPE;
+  for (int i = 0; i < n_tensors; ++i) {
+    const mkv_norm_rope_grad_tensor& t = tensors[i];
+    for (int k = 0; k < i; ++k)
+      if (t.dweight && t.dweight == tensors[k].dweight) return MKV_ERR_INVALID_ARG;
+    if (tokens == 0) continue;  // (empty tensors may have no address)
+    const int64_t dx[3] = {t.dx_batch, t.dx_token, t.dx_head};
+    if (!in_place_ok(t.x, t.dx, batch, tokens, t.heads, {t.x_batch, t.x_token, t.x_head}, dx) ||
+        !in_place_ok(t.dy, t.dx, batch, tokens, t.heads, {t.dy_batch, t.dy_token, t.dy_head}, dx))
+      return MKV_ERR_INVALID_ARG;
+    for (int k = 0; k < i; ++k)
+      if (t.dx == tensors[k].dx) return MKV_ERR_INVALID_ARG;
+  }
   if (tokens == 0 && !wanted) return MKV_OK;
   if (!workspace || workspace_bytes < kHeaderBytes + (size_t)blocks * head_dim * sizeof(float) ||
       !aligned(workspace, 256))

@@ -95,6 +95,33 @@ def test_an_eps_too_small_for_sums_of_squares_is_refused(L):
         assert L.mkv_norm_rope_grad(1, tokens, 128, FAKE, 0, 0, _params(), eps, 1, bwd, FAKE, 1 << 40, None) == want
 
 
+def test_outputs_in_one_place_are_refused(L):
+    """Two tensors written to one place (each would leave parts of its own there), and a place that is read with other strides."""
+    def fwd(*xs, t=4):
+        arr = (mkv.mkv_norm_rope_tensor * len(xs))(*(mkv.mkv_norm_rope_tensor(mkv.mkv_rope_tensor(*x), FAKE, 0, 0) for x in xs))
+        return L.mkv_norm_rope(1, t, 128, FAKE, 0, 0, _params(), 1e-6, len(xs), arr, None)
+
+    def bwd(*xs, t=4):
+        arr = (mkv.mkv_norm_rope_grad_tensor * len(xs))(*(mkv.mkv_norm_rope_grad_tensor(*x) for x in xs))
+        return L.mkv_norm_rope_grad(1, t, 128, FAKE, 0, 0, _params(), 1e-6, len(xs), arr, None, 0, None)  # (no workspace: not launched)
+    far, s = [FAKE * i for i in range(2, 8)], (0, 256, 128)
+    assert fwd((FAKE, far[0], 2, *s, *s), (FAKE, far[0], 2, *s, *s)) == INVALID
+    assert fwd((FAKE, FAKE, 2, *s, 0, 512, 128)) == INVALID and fwd((FAKE, FAKE, 2, *s, 0, 256, 256)) == INVALID
+
+    def grad(x=FAKE, dy=far[0], dx=far[1], sx=s, sdy=s, sdx=s, heads=2, dw=far[2]):
+        return x, dy, dx, heads, *sx, *sdy, *sdx, FAKE, 0, 0, dw
+    other = dict(dx=far[3], dw=far[4])
+    assert bwd(grad(), grad(**other)) == bwd(grad(dw=None), grad(dx=far[3])) == WORKSPACE
+    assert bwd(grad(dw=None), grad(dx=far[3], dw=None), t=0) == OK
+    assert bwd(grad(), grad(**{**other, "dx": far[1]})) == INVALID and bwd(grad(), grad(**{**other, "dw": far[2]})) == INVALID
+    assert bwd(grad(), grad(**{**other, "dw": far[2]}), t=0) == INVALID  # (both would be zeros, but that is a caller's mistake too)
+    for same in ("x", "dy"):
+        place = {same: far[1]}
+        assert bwd(grad(**place)) == bwd(grad(**place, heads=1, sdx=(0, 256, 0))) == WORKSPACE  # in place; a stride that is not used
+        for strides in ((0, 512, 128), (0, 256, 136)):
+            assert bwd(grad(**place, sdx=strides)) == INVALID
+
+
 def test_binding_refusals():
     pos, p = torch.zeros(1, 1, 4, dtype=torch.int32), _params(64)
     x = torch.zeros(1, 4, 2, 64, dtype=torch.bfloat16)
