@@ -43,7 +43,6 @@ struct PrefixArgs {
   int32_t batch;
   int32_t n_kv;
   int32_t group;
-  int32_t early;
   uint32_t polls;
   void* ws;
   // filled by the launcher: parts of every query row, row-major as out's rows

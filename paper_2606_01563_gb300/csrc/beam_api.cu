@@ -98,7 +98,6 @@ mkv_status mkv_prefix_step(mkv_geom geom, const mkv_seqs* seqs, const void* q, c
   a.batch = geom.batch;
   a.n_kv = geom.n_kv_heads;
   a.group = geom.group;
-  a.early = p->early_load;
   a.ws = workspace;
   return cuda_status(launch_prefix_step(a, geom, sms, static_cast<cudaStream_t>(stream)));
 }
