@@ -88,7 +88,7 @@ MKV_API size_t mkv_prefix_workspace_size(mkv_geom geom, int32_t n_seqs, int32_t 
  * length outside 0..capacity is recorded as MKV_ERR_CAPACITY and taken as the
  * nearer end.  Scores, statistics and sums are fp32; the softmax weights enter
  * the product with the values rounded to bf16 (about a normaliser of the
- * rounded weights), as the output is, and the order-1 product takes an fp32 C'
+ * rounded weights; mkv_decode_step has them in two parts, and an fp32 output), as the output is, and the order-1 product takes an fp32 C'
  * as two bf16 parts.
  * Requirements: q, k_new, v_new and out 16-byte aligned, lse 4; p as in
  * mkv_decode_step.

@@ -27,10 +27,14 @@
 // The log of the joined sum and the scores are fp64: which of two continuations is
 // better is decided to a few 1e-7 whatever the vocabulary, and the scores that come back are rounded once.
 //
-// Each logit is read once; what bounds it over many beams is issue, 18
-// instructions a logit and a barrier a chunk (32 x 8 beams of 150001 bf16 logits: 43-46 us,
-// HBM's floor 9.6; with blocks of 512 threads 72), over few the two launches'
-// chains (4 beams of 32000: 9.5 us).
+// Each logit is read once.  What bounds it over many beams is waiting more than
+// issue (32 x 8 of 150001 bf16 logits: 44 us, HBM's floor 9.6; with blocks of 512 threads
+// 72): an SM that has blocks issues in 0.58 of its cycles, 20 instructions a logit,
+// and of the 8.8 cycles from one of a warp's issues to its next 2.3 go to the
+// chunk's barrier and 1.8 to the instruction before; the join, 11 us, has a block an item.
+// Over few it is the two launches' chains (4 beams of 32000: 9.8-10.3 us).  Of the
+// same logits fp32 take 46 us, rows of an odd length that are not padded to 16 bytes 56 (bf16)
+// and 46 (fp32); one item of 64 beams 74 us (n_out 64), of 8 beams 21.
 #include <algorithm>
 
 #include "beam.h"

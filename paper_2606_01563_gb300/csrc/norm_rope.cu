@@ -21,8 +21,8 @@
 //
 // Bounded by HBM at 4 bytes a value forward and 6 backward, in so far as enough
 // rows are in flight: a row's sum stands between its loads and its stores, so
-// the forward kernel is held to 64 registers, four blocks an SM (4 x 32768 tokens,
-// 40 heads of 128 dims: 494 us, 0.80 of 6.8 TB/s; 526 with 72 registers and three; 505 with the next
+// the forward kernel is held to 64 registers, four blocks an SM, at the cost of
+// 24 spilled bytes (4 x 32768 tokens, 40 heads of 128 dims: 494 us, 0.80 of 6.8 TB/s; 526 with 72 registers and three; 505 with the next
 // head's values loaded ahead and 80; 516 with weight times cosine and sine
 // kept in pairs for two operations an instruction, and 80).  The gradient, 127
 // registers and two blocks: 16382 tokens 122 us, 0.61.

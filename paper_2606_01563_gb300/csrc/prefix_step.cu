@@ -9,29 +9,35 @@
 // moment term is a state too: m = log2 n + scale log2 e q.mu_k, l = 1, O = mu_v +
 // scale C' q; and so is the new token.
 //
-// Two launches.  prefix_parts_kernel leaves states ("parts") of every query row in
+// Two launches, or three to four.  prefix_parts_kernel leaves states ("parts") of every query row in
 // the workspace: a block takes a run of the shared rows for up to 8 NT query
 // rows of a unit (all sequences' heads side by side, so that a shared row is read
 // once for all of them), or 64 dims of the moment term for as many, or tails, one
 // a warp.  prefix_join_kernel joins each row's parts and the new token and
 // appends that token to its tail.  For many query rows over many shared rows the kernels of
-// tree_step.cu take the shared rows, between the two.
+// tree_step.cu (one, and a second where it cuts items) take the shared rows, between the two.
 //
 // A run: a warp issues 64-row TMA copies into a ring; four warps work on every
 // tile together.  Each takes the logits of 16 of its rows, S^T = K q^T with the keys on
 // the 16-row side and the query rows on the 8-column side, and writes their
 // weights, rounded to bf16, to shared memory; then each takes a quarter of the
 // value dims over all 64 rows, O^T += V^T P^T.  So a query row's O is held once (8 NT registers a thread at
-// 128 dims), up to 64 query rows share a shared row's one trip, and no states of
+// 128 dims), up to 32 query rows share a shared row's one trip, and no states of
 // warps are merged.  One barrier a tile: the weights have two buffers.  A reference
-// moves when a score exceeds it by more than 8 (log2), which every warp learns
+// lies 32 (log2) above the score that set it and moves when a score exceeds it, which every warp learns
 // at that barrier.  O is scaled by the ratio of the unrounded weights' sum to the
-// rounded ones', so that roundings that are common cancel.
+// rounded ones', so that roundings that are common cancel; those that are not
+// leave the output off by up to 2^-8 of the values' mean magnitude, half a step of its own
+// type (measured against 64 bits 0.0017, a form with weights in 32 bits 0.0016-0.0017).
 //
 // What bounds it: HBM with few query rows over a long prompt (4 sequences of 8 x 4
 // heads, 65536 rows: 43.5-45 us, 0.88-0.91 of 6.8 TB/s); with 32 the chain of a tile, 1
-// us (8 sequences, 65536 rows: 50 us); short prompts the two launches' chains
+// us (8 sequences, 65536 rows: 50 us; its kernel, with four column tiles at 128 dims,
+// has 168 registers and spills 80 bytes); short prompts the two launches' chains
 // (4 sequences, 128 rows: 6.0 us; 8 sequences of 4 prompts, 1024 rows, tails of 100: 15).
+// Splits follow capacities, since the host does not know the lengths: tails of
+// capacity 1024 or 4096 that hold 4 rows cost those 8 sequences 16.6-16.9 us, of
+// capacity 8 11.3 (13 sequences of 8 prompts, 4001 rows: 49.6 and 42.8).
 #include <algorithm>
 #include <cmath>
 
@@ -57,7 +63,9 @@ constexpr int kMaxTails = 8;   // tails of a warp
 // rows 26 and 34 us (14), 24 over 8192 23 and 26 (10), 32 x 2 prompts over 2048 21
 // and 26 (7); 64 over 4096 32 and 28 (14), 64 x 4 over 1024 44 and 39 (14), 32 x 2
 // over 8192 55 and 38 (27), 24 over 32768 61 and 45 (40).  A unit's only block
-// keeps its rows: 8 sequences over 65536 49 and 59 (27).
+// keeps its rows: 8 sequences over 65536 49 and 59 (27).  The first of these cases is on
+// the wrong side: visits alone do not tell two blocks of a unit, which do well here
+// for longer, from eight.
 constexpr long kVisits = 12;
 constexpr float kSlack = 32.f;  // log2 headroom of a reference above the score that set it (weights at most 1)
 constexpr float kNegInf = -INFINITY;
